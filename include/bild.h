@@ -279,6 +279,156 @@ int bild_head_stats(const bild_model* m, const float* x_dev, int rows, const int
 int bild_head_stats_static(const bild_model* m, const float* x_dev, int rows, const int32_t* targets_dev,
                            bild_row_stats* out_dev, void* hip_stream);
 
+/* ======================================================================= operators on rows
+ * Like bild_head_stats these work on rows that the caller holds: x, y, src, dst, logits and every other array of a call's struct is
+ * DEVICE memory of the caller, read and written by kernels on hip_stream (NULL: the default stream) behind what is on that stream
+ * already.  The calls allocate nothing, do not wait for the stream and may be captured into a graph; what the struct points to then
+ * has to stay where it is.  They run on the device of their handle, or of the stream (bild_rotary_apply), and leave the caller's
+ * current device as it was.  Strides are in elements, may be anything that keeps the rows apart, and ask for no alignment beyond the type's
+ * (rows whose addresses are multiples of 16 bytes are faster).  Unless an entry says that it may be, what a call writes must not overlap what it reads. */
+#define BILD_DT_F16 2 /* rows and scales of the operators, besides BILD_DT_F32 and BILD_DT_BF16; no model has it */
+
+/* ---- products with a matrix in 4 bits ----
+ * w[n][k] = (code[n][k] - zero[n][k / group]) * scale[n][k / group], zero = 8 where there are no zeros.  The last group of a feature may be short. */
+typedef struct bild_quant bild_quant; /* the matrix on the device, immutable */
+
+/* Rounds an fp32 matrix (HOST memory, [n][k]; inputs_first: [k][n], the order of bild_model_create's matrices) to such a matrix: codes [n][(k + 1) / 2],
+ * input 2j in the low and 2j + 1 in the high half of byte j (an odd k leaves the last half zero); scales [n][groups], groups = ceil(k / group), of type
+ * scale_dtype (BILD_DT_F16 or BILD_DT_BF16); zeros [n][groups], one of 0..15 a byte, or NULL.  Without zeros the scale is the group's largest magnitude / 7,
+ * with zeros the group's range (widened to hold 0) / 15; codes and zeros are the nearest.  No value moves by more than half a scale, but for what the scale's own rounding adds
+ * at the ends of the range.  BILD_EINVAL for a value that is not finite or a scale beyond the type. */
+int bild_quant_round(const float* host_w, int n, int k, int inputs_first, int group, int scale_dtype, uint8_t* host_codes, void* host_scales,
+                     uint8_t* host_zeros /* nullable */);
+/* Uploads a matrix given as above.  The arrays may be in host or in device memory (whatever wrote them there has to be done) and are copied.  group is 32, 64 or 128.
+ * BILD_EINVAL for another group, a scale type that is not 16 bits wide or a zero above 15; the matrix lies on the current device. */
+int bild_quant_create(int n, int k, int group, const uint8_t* codes, const void* scales, int scale_dtype, const uint8_t* zeros /* nullable */,
+                      bild_quant** out);
+int bild_quant_destroy(bild_quant* w); /* nothing that uses it may still run */
+
+/* y[r][n] = scale * sum over k of xh[r][k] * w[n][k], xh = x, or with gain x[r][k] * gain[k] / sqrt(mean over k of x[r][k]^2 + eps): the RMSNorm in front of
+ * a projection or an LM head.  Products are those of the values themselves (none is rounded on the way, but x * gain to 24 bits), sums are
+ * fp32, y is rounded once.  rows >= 1; made for the rows of a decoder pass (up to BILD_MAX_ROWS), longer blocks are taken as they are. */
+typedef struct bild_quant_call {
+    const void* x;      /* [rows][k], row r at x + r * x_stride               */
+    int64_t x_stride;
+    void* y;            /* [rows][n]                                          */
+    int64_t y_stride;
+    const float* gain;  /* [k], nullable: no norm                             */
+    int32_t rows;
+    int32_t x_dtype;    /* BILD_DT_F32, BILD_DT_BF16 or BILD_DT_F16           */
+    int32_t y_dtype;
+    float eps;
+    float scale;
+} bild_quant_call;
+int bild_quant_matmul(const bild_quant* w, const bild_quant_call* call, void* hip_stream);
+
+/* ---- rotary positions ----
+ * The first rot_dim dimensions of a head are pairs that turn by position * f_i, i = 0 .. rot_dim / 2 - 1; the others are copied.
+ *   layout   BILD_ROTARY_PAIRS: pair i is (2i, 2i + 1); BILD_ROTARY_HALVES: (i, i + rot_dim / 2)
+ *   scaling  f_i = base^(-2i / rot_dim), and for long contexts
+ *     LINEAR  f_i / factor
+ *     BASE    with base * factor^(rot_dim / (rot_dim - 2)) for base
+ *     BANDS   by the turns t_i = original * f_i / 2 pi in the original context: f_i from `high` turns on, f_i / factor up to `low`,
+ *             in between the mean weighted by (t_i - low) / (high - low)
+ *     YARN    f_i below the pair that makes `high` turns in the original context, f_i / factor above the one that makes `low`, a ramp over the
+ *             pairs' index in between; cos and sin are multiplied by `magnitude`, 0: 0.1 ln(factor) + 1
+ * original, low, high and magnitude are read by the last two alone (magnitude by YARN); low = high = 0 stands for 1 and 4 (BANDS), 1 and 32 (YARN). */
+#define BILD_ROTARY_PAIRS  0
+#define BILD_ROTARY_HALVES 1
+#define BILD_ROTARY_NONE   0
+#define BILD_ROTARY_LINEAR 1
+#define BILD_ROTARY_BASE   2
+#define BILD_ROTARY_BANDS  3
+#define BILD_ROTARY_YARN   4
+typedef struct bild_rotary_config {
+    int32_t layout;
+    int32_t rot_dim;    /* even, 2 .. 256  */
+    int32_t scaling;
+    int32_t original;   /* positions the unscaled frequencies were made for */
+    float   base;
+    float   factor;     /* >= 1 */
+    float   low, high;
+    float   magnitude;
+} bild_rotary_config;
+typedef struct bild_rotary bild_rotary; /* the frequencies, in host memory: one handle serves any stream and device, and several threads */
+
+/* The frequencies f_i (HOST memory, rot_dim / 2 doubles) and the factor on cos and sin (nullable). */
+int bild_rotary_frequencies(const bild_rotary_config* cfg, double* frequencies, double* magnitude);
+int bild_rotary_create(const bild_rotary_config* cfg, bild_rotary** out);
+int bild_rotary_destroy(bild_rotary* r);
+
+/* Turns the rows of up to two arrays (queries and keys, each with heads of its own) by the positions of their tokens: dst[t][h] =
+ * turned src[t][h].  inverse turns back (without dividing by the magnitude): the gradient of src from that of dst.  dst may be src with the same strides.  Angles are
+ * formed in 64 bits, the products in fp32, results are rounded once. */
+typedef struct bild_rotary_rows {
+    const void* src;       /* head h of token t at src + t * src_token + h * src_head, its d_head dimensions side by side */
+    void* dst;
+    int64_t src_token, src_head, dst_token, dst_head;
+    int32_t heads;         /* 0: the array is not there */
+    int32_t reserved;      /* 0 */
+} bild_rotary_rows;
+typedef struct bild_rotary_call {
+    bild_rotary_rows q, k;
+    const int32_t* positions;  /* [tokens], nullable: first, first + 1, .. */
+    int32_t first;
+    int32_t tokens;
+    int32_t d_head;            /* rot_dim .. 1024 */
+    int32_t dtype;
+    int32_t inverse;
+    int32_t reserved;          /* 0 */
+} bild_rotary_call;
+int bild_rotary_apply(const bild_rotary* r, const bild_rotary_call* call, void* hip_stream);
+
+/* bild_model_create for a network (pos = BILD_POS_ROPE) whose positions are those of `rotary` (rot_dim <= d_head; cfg->rope_base is not read but has to be
+ * valid).  Every pass of such a model turns queries and keys accordingly. */
+int bild_model_create_rotary(const bild_model_config* cfg, const bild_rotary_config* rotary, const float* const* host_tensors, int n_tensors,
+                             bild_model** out);
+
+/* ---- rules on logits ----
+ * For each row, in this order and in fp32:
+ *   an id that the row's tokens hold:            z = z > 0 ? z / repetition : z * repetition
+ *   one they hold c > 0 times from `starts` on:  z = z - frequency * c, then z = z - presence
+ *   an id with a bias:                           z = z + bias (the entry that stands last, if there are several)
+ *   an id whose mask bit is 0:                   z = -infinity, whatever stood there
+ * and the statistics of what is left, as bild_head_stats gives them, of the values before they are rounded to the rows' type: zmax, lse, argmax (lowest id among equal maxima; -1 where no id is
+ * above -infinity, zmax and lse are -infinity then) and z_target (NaN without targets or for an id outside the vocabulary).  A NaN that the rules leave makes lse NaN, zmax and
+ * argmax are those of the numbers; +infinity makes lse +infinity. */
+typedef struct bild_penalties {
+    float repetition;  /* 1: none */
+    float frequency;   /* 0: none */
+    float presence;    /* 0: none */
+} bild_penalties;
+typedef struct bild_rules_call {
+    const void* logits;              /* [rows][vocab]                                                            */
+    int64_t logits_stride;
+    void* out;                       /* [rows][vocab] of the same type; may be logits (same stride); NULL: statistics only */
+    int64_t out_stride;
+    const int32_t* targets;          /* [rows], nullable                                                         */
+    bild_row_stats* stats;           /* [rows], nullable: logits only                                            */
+    const int32_t* tokens;           /* row r's tokens at tokens + r * tokens_stride (0: the rows share them); nullable: no penalties */
+    int64_t tokens_stride;
+    const int32_t* lengths;          /* [rows]: how many of them count; limited to 0 .. max_tokens. Ids outside the vocabulary are passed over. */
+    const int32_t* starts;           /* [rows], nullable (0): the first that frequency and presence count        */
+    const bild_penalties* penalties; /* [rows], or one for all rows (penalties_stride 0); needed with tokens     */
+    int64_t penalties_stride;        /* 0 or 1                                                                   */
+    const int32_t* bias_ids;         /* row r's ids at bias_ids + r * bias_stride (0: shared); nullable: no biases. Ids outside the vocabulary are passed over. */
+    const float* bias;               /* their values, laid out the same; needed with bias_ids                    */
+    int64_t bias_stride;
+    const int32_t* bias_counts;      /* [rows], nullable (max_bias): how many of them count; limited to 0 .. max_bias */
+    const uint32_t* mask;            /* bit id % 32 of word id / 32, row r's words at mask + r * mask_stride (0: shared); nullable: all allowed */
+    int64_t mask_stride;
+    int32_t rows;                    /* 1 .. the handle's max_rows                                               */
+    int32_t dtype;
+    int32_t max_tokens;              /* up to 1048575 */
+    int32_t max_bias;                /* up to 1023    */
+} bild_rules_call;
+typedef struct bild_rules bild_rules; /* device memory for the statistics of rows that several workgroups share */
+/* A handle's calls have to follow each other (one stream, or ordered by the caller): two streams, or two captured graphs, that may
+ * run at the same time take a handle each. */
+int bild_rules_create(int vocab, int max_rows, bild_rules** out);
+int bild_rules_destroy(bild_rules* r);
+int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_stream);
+
 /* Introspection (host copies of the control block). */
 int bild_get_lengths(bild_state* s, int32_t* y_len, int32_t* draft_start, int32_t* len_small, int32_t* len_large);
 int bild_get_sequence(bild_state* s, int32_t* out, int cap, int32_t* n);

@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(_PKG, "libbild.so")
 OK, EINVAL, ESTATE, ECAP, EHIP, ENOMEM = 0, -1, -2, -3, -4, -5
 MAX_ROWS = 32
 SMALL, LARGE, BOTH = 1, 2, 3
+DT_F32, DT_BF16, DT_F16 = 0, 1, 2
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_YARN = 0, 1, 2, 3, 4
 ACCEPT_THRESHOLD, ACCEPT_REJECTION = 0, 1
 
 
@@ -40,6 +42,38 @@ class Profile(C.Structure):
                 ("dropped", C.c_int32)]
 
 
+class QuantCall(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64), ("gain", C.c_void_p),
+                ("rows", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("eps", C.c_float), ("scale", C.c_float)]
+
+
+class RotaryConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layout", "rot_dim", "scaling", "original")] + [
+        (n, C.c_float) for n in ("base", "factor", "low", "high", "magnitude")]
+
+
+class RotaryRows(C.Structure):
+    """RotaryRows(src, dst, heads, src_token, src_head, dst_token, dst_head): device pointers, strides in elements."""
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("src_token", C.c_int64), ("src_head", C.c_int64), ("dst_token", C.c_int64),
+                ("dst_head", C.c_int64), ("heads", C.c_int32), ("reserved", C.c_int32)]
+
+    def __init__(self, src=None, dst=None, heads=0, src_token=0, src_head=0, dst_token=0, dst_head=0):
+        super().__init__(src, dst, src_token, src_head, dst_token, dst_head, heads, 0)
+
+
+class RotaryCall(C.Structure):
+    _fields_ = [("q", RotaryRows), ("k", RotaryRows), ("positions", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("first", "tokens", "d_head", "dtype", "inverse", "reserved")]
+
+
+class RulesCall(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64), ("targets", C.c_void_p),
+                ("stats", C.c_void_p), ("tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("lengths", C.c_void_p), ("starts", C.c_void_p),
+                ("penalties", C.c_void_p), ("penalties_stride", C.c_int64), ("bias_ids", C.c_void_p), ("bias", C.c_void_p),
+                ("bias_stride", C.c_int64), ("bias_counts", C.c_void_p), ("mask", C.c_void_p), ("mask_stride", C.c_int64),
+                ("rows", C.c_int32), ("dtype", C.c_int32), ("max_tokens", C.c_int32), ("max_bias", C.c_int32)]
+
+
 class BildError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {code} ({strerror(code)})")
@@ -51,6 +85,7 @@ _lib = None
 _SIGS = {
     "bild_model_num_tensors": (C.c_int, [C.POINTER(ModelConfig)]),
     "bild_model_create": (C.c_int, [C.POINTER(ModelConfig), C.POINTER(C.c_void_p), C.c_int, C.POINTER(C.c_void_p)]),
+    "bild_model_create_rotary": (C.c_int, [C.POINTER(ModelConfig), C.POINTER(RotaryConfig), C.POINTER(C.c_void_p), C.c_int, C.POINTER(C.c_void_p)]),
     "bild_model_destroy": (C.c_int, [C.c_void_p]),
     "bild_pair_create": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p)]),
     "bild_pair_create_early_exit": (C.c_int, [C.c_void_p, C.c_int, C.c_float, C.POINTER(C.c_void_p)]),
@@ -73,6 +108,17 @@ _SIGS = {
                               C.POINTER(C.c_int32)]),
     "bild_head_stats": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
     "bild_head_stats_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_quant_round": (C.c_int, [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p] * 3),
+    "bild_quant_create": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_void_p)]),
+    "bild_quant_destroy": (C.c_int, [C.c_void_p]),
+    "bild_quant_matmul": (C.c_int, [C.c_void_p, C.POINTER(QuantCall), C.c_void_p]),
+    "bild_rotary_frequencies": (C.c_int, [C.POINTER(RotaryConfig), C.c_void_p, C.POINTER(C.c_double)]),
+    "bild_rotary_create": (C.c_int, [C.POINTER(RotaryConfig), C.POINTER(C.c_void_p)]),
+    "bild_rotary_destroy": (C.c_int, [C.c_void_p]),
+    "bild_rotary_apply": (C.c_int, [C.c_void_p, C.POINTER(RotaryCall), C.c_void_p]),
+    "bild_rules_create": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_void_p)]),
+    "bild_rules_destroy": (C.c_int, [C.c_void_p]),
+    "bild_rules_apply": (C.c_int, [C.c_void_p, C.POINTER(RulesCall), C.c_void_p]),
     "bild_get_lengths": (C.c_int, [C.c_void_p] + [C.POINTER(C.c_int32)] * 4),
     "bild_get_sequence": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.POINTER(C.c_int32)]),
     "bild_debug_enable_logits": (C.c_int, [C.c_void_p, C.c_int]),
@@ -149,11 +195,15 @@ def config_from_shape(shape) -> ModelConfig:
 class Model:
     h = None
 
-    def __init__(self, cfg: ModelConfig, tensors: Sequence[np.ndarray]):
+    def __init__(self, cfg: ModelConfig, tensors: Sequence[np.ndarray], rotary: Optional[RotaryConfig] = None):
+        """rotary: the positions of a network with pos = BILD_POS_ROPE (None: pairs (2i, 2i + 1) of the whole head, cfg.rope_base)."""
         arrs = [np.ascontiguousarray(t, dtype=np.float32) for t in tensors]
         ptrs = (C.c_void_p * len(arrs))(*[a.ctypes.data for a in arrs])
         h = C.c_void_p()
-        _check(lib().bild_model_create(C.byref(cfg), ptrs, len(arrs), C.byref(h)), "bild_model_create")
+        if rotary is None:
+            _check(lib().bild_model_create(C.byref(cfg), ptrs, len(arrs), C.byref(h)), "bild_model_create")
+        else:
+            _check(lib().bild_model_create_rotary(C.byref(cfg), C.byref(rotary), ptrs, len(arrs), C.byref(h)), "bild_model_create_rotary")
         self.h, self.cfg = h, cfg
 
     def close(self):
@@ -172,6 +222,98 @@ def head_stats(model: Model, x_dev_ptr: int, rows: int, targets_dev_ptr: Optiona
     """Device pointers in, device pointer out (rows records of ROW_STATS_DTYPE); see bild.h."""
     _check(getattr(lib(), entry)(model.h, C.c_void_p(x_dev_ptr), rows, C.c_void_p(targets_dev_ptr or 0),
                                  C.c_void_p(out_dev_ptr), C.c_void_p(stream or 0)), entry)
+
+
+def _where(a) -> Optional[int]:
+    """Address of a host array, or a device pointer as it is."""
+    return a.ctypes.data if isinstance(a, np.ndarray) else a
+
+
+def quant_round(w: np.ndarray, group: int, scale_dtype: int = DT_F16, zeros: bool = False, inputs_first: bool = False):
+    """Rounds an fp32 matrix ([n][k]; inputs_first: [k][n]) to 4 bits; (codes, scales as 16-bit words, zeros or None), see bild.h."""
+    a = np.ascontiguousarray(w, dtype=np.float32)
+    n, k = a.shape[::-1] if inputs_first else a.shape
+    groups = -(-k // group) if group > 0 else 0
+    codes, scales = np.zeros((n, (k + 1) // 2), np.uint8), np.zeros((n, groups), np.uint16)
+    z = np.zeros((n, groups), np.uint8) if zeros else None
+    _check(lib().bild_quant_round(a.ctypes.data, n, k, int(inputs_first), group, scale_dtype, codes.ctypes.data, scales.ctypes.data,
+                                  z.ctypes.data if zeros else None), "bild_quant_round")
+    return codes, scales, z
+
+
+class Quant:
+    """A matrix in 4 bits on the device.  codes, scales, zeros: host arrays (uint8, 16-bit, uint8) or device pointers."""
+    h = None
+
+    def __init__(self, n: int, k: int, group: int, codes, scales, scale_dtype: int, zeros=None):
+        h = C.c_void_p()
+        codes, scales, zeros = [np.ascontiguousarray(a) if isinstance(a, np.ndarray) else a for a in (codes, scales, zeros)]
+        _check(lib().bild_quant_create(n, k, group, _where(codes), _where(scales), scale_dtype, _where(zeros), C.byref(h)), "bild_quant_create")
+        self.h, self.n, self.k = h, n, k
+
+    def matmul(self, x: int, x_dtype: int, rows: int, y: int, y_dtype: int, x_stride: Optional[int] = None, y_stride: Optional[int] = None,
+               gain: Optional[int] = None, eps: float = 0.0, scale: float = 1.0, stream: Optional[int] = None):
+        """Device pointers; strides in elements (None: rows side by side)."""
+        call = QuantCall(x, self.k if x_stride is None else x_stride, y, self.n if y_stride is None else y_stride, gain, rows, x_dtype, y_dtype, eps, scale)
+        _check(lib().bild_quant_matmul(self.h, C.byref(call), stream), "bild_quant_matmul")
+
+    def close(self):
+        if self.h:
+            lib().bild_quant_destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+
+class Rotary:
+    h = None
+
+    def __init__(self, rot_dim: int, halves: bool = False, base: float = 10000.0, scaling: int = ROTARY_NONE, factor: float = 1.0,
+                 original: int = 0, low: float = 0.0, high: float = 0.0, magnitude: float = 0.0):
+        self.cfg = RotaryConfig(int(halves), rot_dim, scaling, original, base, factor, low, high, magnitude)
+        h = C.c_void_p()
+        _check(lib().bild_rotary_create(C.byref(self.cfg), C.byref(h)), "bild_rotary_create")
+        self.h = h
+
+    def frequencies(self):
+        f, m = np.zeros(self.cfg.rot_dim // 2, np.float64), C.c_double()
+        _check(lib().bild_rotary_frequencies(C.byref(self.cfg), f.ctypes.data, C.byref(m)), "bild_rotary_frequencies")
+        return f, m.value
+
+    def apply(self, d_head: int, dtype: int, tokens: int, q: RotaryRows, k: Optional[RotaryRows] = None, positions: Optional[int] = None,
+              first: int = 0, inverse: bool = False, stream: Optional[int] = None):
+        call = RotaryCall(q, k if k is not None else RotaryRows(), positions, first, tokens, d_head, dtype, int(inverse), 0)
+        _check(lib().bild_rotary_apply(self.h, C.byref(call), stream), "bild_rotary_apply")
+
+    def close(self):
+        if self.h:
+            lib().bild_rotary_destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+
+class Rules:
+    h = None
+
+    def __init__(self, vocab: int, max_rows: int):
+        h = C.c_void_p()
+        _check(lib().bild_rules_create(vocab, max_rows, C.byref(h)), "bild_rules_create")
+        self.h, self.vocab = h, vocab
+
+    def apply(self, logits: int, dtype: int, rows: int, out: Optional[int] = None, stats: Optional[int] = None, targets: Optional[int] = None,
+              logits_stride: Optional[int] = None, out_stride: Optional[int] = None, stream: Optional[int] = None, **rules):
+        """Device pointers; strides in elements (None: rows side by side).  rules: the other fields of bild_rules_call by name."""
+        call = RulesCall(logits=logits, logits_stride=self.vocab if logits_stride is None else logits_stride, out=out,
+                         out_stride=self.vocab if out_stride is None else out_stride, targets=targets, stats=stats, rows=rows, dtype=dtype, **rules)
+        _check(lib().bild_rules_apply(self.h, C.byref(call), stream), "bild_rules_apply")
+
+    def close(self):
+        if self.h:
+            lib().bild_rules_destroy(self.h)
+            self.h = None
+
+    __del__ = close
 
 
 class Pair:

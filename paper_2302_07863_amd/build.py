@@ -31,6 +31,9 @@ UNITS = [
     ("head.hip", "head.o", []),
     ("head_stats.hip", "head_stats.o", []),
     ("bench_api.hip", "bench_api.o", []),
+    ("quant.hip", "quant.o", []),
+    ("rotary.hip", "rotary.o", []),
+    ("rules.hip", "rules.o", []),
     ("layout.cpp", "layout.o", []),
 ]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-pthread",

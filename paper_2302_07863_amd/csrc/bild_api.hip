@@ -137,25 +137,48 @@ extern "C" int bild_model_num_tensors(const bild_model_config* c) {
 extern "C" int bild_model_destroy(bild_model* m) {
     if (!m) return BILD_EINVAL;
     for (void* p : m->allocs) (void)hipFree(p);
+    (void)bild_rotary_destroy(m->rotary);
     delete m;
     return BILD_OK;
 }
 
-extern "C" int bild_model_create(const bild_model_config* cfg, const float* const* t, int n_tensors,
-                                 bild_model** out) {
-    if (!cfg || !t || !out) return BILD_EINVAL;
-    if (!config_ok(*cfg)) return BILD_EINVAL;
-    if (n_tensors != bild_model_num_tensors(cfg)) return BILD_EINVAL;
+namespace {
+
+// Where dimension j of a head lies for models whose pairs are (i, i + rot_dim / 2): the kernels turn (2i, 2i + 1), and scores do
+// not change where queries and keys change their order alike.
+int turned_at(const bild_rotary* r, int j) {
+    const int half = r && r->cfg.layout == BILD_ROTARY_HALVES ? r->cfg.rot_dim / 2 : 0;
+    return j >= 2 * half ? j : j < half ? 2 * j : 2 * (j - half) + 1;
+}
+
+// The columns of a [d][heads * d_head] projection in that order (`to`: memory for them).
+const float* turned_columns(const bild_model* m, const float* w, std::vector<float>& to) {
+    if (!m->rotary || m->rotary->cfg.layout != BILD_ROTARY_HALVES) return w;
+    const int dh = m->cfg.d_head, I = m->inner();
+    to.resize((size_t)m->cfg.d_model * I);
+    for (int r = 0; r < m->cfg.d_model; ++r)
+        for (int h = 0; h < m->cfg.n_heads; ++h)
+            for (int j = 0; j < dh; ++j) to[(size_t)r * I + h * dh + turned_at(m->rotary, j)] = w[(size_t)r * I + h * dh + j];
+    return to.data();
+}
+
+int model_create(const bild_model_config* cfg, const bild_rotary_config* rotary, const float* const* t, int n_tensors, bild_model** out) {
     for (int i = 0; i < n_tensors; ++i)
         if (!t[i]) return BILD_EINVAL;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return BILD_EHIP;
     bild_model* m = new (std::nothrow) bild_model();
     if (!m) return BILD_ENOMEM;
+    if (rotary)
+        if (const int rc = bild_rotary_create(rotary, &m->rotary)) {
+            bild_model_destroy(m);
+            return rc;
+        }
     m->cfg = *cfg;
     m->cfg.tie_shift %= cfg->vocab;  // (kernels take the row below vocab with one subtraction)
     const int d = cfg->d_model, I = m->inner(), F = cfg->d_ff, V = cfg->vocab;
     int i = 0, rc = BILD_OK;
+    std::vector<float> tq, tk;
 #define UP(call)                         \
     do {                                 \
         rc = (call);                     \
@@ -179,7 +202,7 @@ extern "C" int bild_model_create(const bild_model_config* cfg, const float* cons
     m->enc.resize(cfg->n_enc_layers);
     for (auto& L : m->enc) {
         UP(upload_vec(m, t[i], d, &L.ln1));
-        UP(upload_concat(m, {t[i + 1], t[i + 2], t[i + 3]}, I, d, &L.wqkv));
+        UP(upload_concat(m, {turned_columns(m, t[i + 1], tq), turned_columns(m, t[i + 2], tk), t[i + 3]}, I, d, &L.wqkv));
         UP(upload_matrix(m, t[i + 4], true, d, I, &L.wo));
         UP(upload_vec(m, t[i + 5], d, &L.ln2));
         i += 6;
@@ -200,7 +223,7 @@ extern "C" int bild_model_create(const bild_model_config* cfg, const float* cons
     }
     for (auto& L : m->dec) {
         UP(upload_vec(m, t[i], d, &L.ln1));
-        UP(upload_concat(m, {t[i + 1], t[i + 2], t[i + 3]}, I, d, &L.wqkv));
+        UP(upload_concat(m, {turned_columns(m, t[i + 1], tq), turned_columns(m, t[i + 2], tk), t[i + 3]}, I, d, &L.wqkv));
         UP(upload_matrix(m, t[i + 4], true, d, I, &L.wo));
         i += 5;
         if (cfg->cross_attn) {
@@ -219,6 +242,26 @@ extern "C" int bild_model_create(const bild_model_config* cfg, const float* cons
 #undef UP
     *out = m;
     return BILD_OK;
+}
+
+}  // namespace
+
+extern "C" int bild_model_create(const bild_model_config* cfg, const float* const* t, int n_tensors,
+                                 bild_model** out) {
+    if (!cfg || !t || !out) return BILD_EINVAL;
+    if (!config_ok(*cfg)) return BILD_EINVAL;
+    if (n_tensors != bild_model_num_tensors(cfg)) return BILD_EINVAL;
+    return model_create(cfg, nullptr, t, n_tensors, out);
+}
+
+extern "C" int bild_model_create_rotary(const bild_model_config* cfg, const bild_rotary_config* rotary, const float* const* t, int n_tensors,
+                                        bild_model** out) {
+    if (!cfg || !rotary || !t || !out) return BILD_EINVAL;
+    if (!config_ok(*cfg) || cfg->pos != BILD_POS_ROPE || rotary->rot_dim > cfg->d_head) return BILD_EINVAL;
+    if (n_tensors != bild_model_num_tensors(cfg)) return BILD_EINVAL;
+    double f[256];
+    if (const int rc = bild_rotary_frequencies(rotary, f, nullptr)) return rc;
+    return model_create(cfg, rotary, t, n_tensors, out);
 }
 
 extern "C" int bild_pair_create(bild_model* s, bild_model* l, bild_pair** out) {
@@ -264,6 +307,7 @@ extern "C" int bild_pair_create_early_exit(bild_model* l, int k, float small_log
     v->head = l->head;
     v->dec_final = l->dec_final;
     v->dec_rel = l->dec_rel;
+    v->rotary = l->rotary;
     v->dec.assign(l->dec.begin(), l->dec.begin() + k);
     v->cwkv_all = l->cwkv_all;  // (a view's cross K/V are the large model's: never projected for the view)
     p->m[0] = v;
@@ -512,7 +556,9 @@ extern "C" int bild_state_create(const bild_pair* p, int max_src, int max_len, i
         const bild_model_config& c = p->m[w]->cfg;
         M.x2 = M.x + (size_t)M.rows_cap * c.d_model;
         if (M.pe) e = launch_pe_table(M.pe, positions, c.d_model, s->stream);
-        if (M.rope && e == hipSuccess) e = launch_rope_table(M.rope, positions, c.d_head, c.rope_base, s->stream);
+        if (M.rope && e == hipSuccess)
+            e = p->m[w]->rotary ? launch_rotary_table(M.rope, positions, c.d_head, *p->m[w]->rotary, s->stream)
+                                : launch_rope_table(M.rope, positions, c.d_head, c.rope_base, s->stream);
     }
     if (p->trunk_layers > 0) {
         s->ms[0].kcache = s->ms[1].kcache;
@@ -2299,7 +2345,10 @@ extern "C" int bild_debug_kv(bild_state* s, int which, int layer, int is_v, int 
         return f;
     };
     for (int t = 0; t < n; ++t)
-        for (size_t i = 0; i < I; ++i) out[(size_t)t * I + i] = is_v ? widen(i * cap + pos0 + t) : widen((size_t)t * I + i);
+        for (size_t i = 0; i < I; ++i) {
+            const size_t dh = m->cfg.d_head;
+            out[(size_t)t * I + i] = is_v ? widen(i * cap + pos0 + t) : widen((size_t)t * I + i / dh * dh + turned_at(m->rotary, (int)(i % dh)));
+        }
     return BILD_OK;
 }
 

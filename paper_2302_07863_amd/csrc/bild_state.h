@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "bild_internal.h"
+#include "operators.h"
 
 #define HIPC(expr)                                   \
     do {                                             \
@@ -111,6 +112,7 @@ struct bild_model {
     const float* dec_rel = nullptr;  // encoder's / decoder's self-attention, shared by all layers of the stack
     std::vector<LayerW> enc, dec;
     TMat cwkv_all;                   // the cross K/V projections of all decoder layers side by side (dec[l].cwkv points into it)
+    bild_rotary* rotary = nullptr;   // bild_model_create_rotary: the positions (a view's are its model's)
     std::vector<void*> allocs;
     mutable HeadPool head_pool;
     size_t device_bytes = 0;

@@ -1,0 +1,79 @@
+// What the operators on rows (quant.hip, rotary.hip, rules.hip) share with each other and with the decoder passes.
+#pragma once
+#include "bild_internal.h"
+
+// A matrix in 4 bits: tiles of 16 features x 128 inputs in the order the matrix cores take them.
+struct bild_quant {
+    int n = 0, k = 0, group = 0;
+    int tn = 0, tk = 0;        // feature tiles, input tiles
+    int bf16_scales = 0;
+    void* mem = nullptr;       // one allocation
+    const uint4* codes = nullptr;     // [tn][tk][64 lanes]: see quant.hip
+    const uint16_t* scales = nullptr; // [tn][tk][4 feature quads][128 / group][4 features]
+    const uint8_t* zeros = nullptr;   // the same order; null: 8 everywhere
+    int device = 0;
+};
+
+struct bild_rotary {
+    bild_rotary_config cfg;
+    double frequency[128];
+    double magnitude;
+};
+
+namespace bild {
+
+// Runs what follows on `device` and puts the caller's current device back.
+class OnDevice {
+    int was = -1;
+
+public:
+    bool ok;
+    explicit OnDevice(int device) {
+        int now = -1;
+        ok = hipGetDevice(&now) == hipSuccess;
+        if (ok && now != device) {
+            ok = hipSetDevice(device) == hipSuccess;
+            if (ok) was = now;
+        }
+    }
+    ~OnDevice() {
+        if (was >= 0) (void)hipSetDevice(was);
+    }
+    OnDevice(const OnDevice&) = delete;
+};
+
+inline int row_bytes(int dtype) { return dtype == BILD_DT_F32 ? 4 : 2; }
+inline bool row_type(int dtype) { return dtype == BILD_DT_F32 || dtype == BILD_DT_BF16 || dtype == BILD_DT_F16; }
+
+// cos and sin of the positions from 0 on, times the magnitude, as the passes' kernels read them: [position][d_head / 2] pairs, those
+// behind rot_dim not turned.
+hipError_t launch_rotary_table(double2* table, int positions, int d_head, const bild_rotary& r, hipStream_t st);
+
+int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st);
+
+// Rules on the logits of a row (bild_rules_call), as kernel arguments.
+struct RulesArgs {
+    const void* logits;
+    void* out;
+    int64_t ld, ldo;
+    const int* targets;
+    bild_row_stats* stats;
+    const int* tokens;
+    int64_t tokens_stride;
+    const int *lengths, *starts;
+    const bild_penalties* penalties;
+    int64_t penalties_stride;
+    const int* bias_ids;
+    const float* bias;
+    int64_t bias_stride;
+    const int* bias_counts;
+    const uint32_t* mask;
+    int64_t mask_stride;
+    int rows, vocab, dtype, max_tokens, max_bias;
+    int parts, range;   // workgroups of a row, ids of each
+    StatPart* part;     // [row][parts]
+    unsigned* arrived;  // [row]: zero between launches
+};
+hipError_t launch_rules(RulesArgs a, hipStream_t st);
+
+}  // namespace bild

@@ -1,0 +1,190 @@
+"""Products with matrices in 4 bits against the definition in 64 bits: types, groups, ragged sizes, strides, norms, streams, graphs."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import paper_2302_07863_amd as pkg
+from paper_2302_07863_amd import binding as b
+from tests.hipmem import DeviceArray, hip
+from tests.rows import BF16, F16, F32, HALF_STEP, TINY, U32, Graph, Rows, Stream, close, normed, pack, scale_words, scales_of, unpack, weights
+
+pytestmark = pytest.mark.gpu
+
+
+def matrix(rng, n, k, group, zeros=False, scale_dtype=F16):
+    groups = -(-k // group)
+    codes = rng.integers(0, 256, (n, (k + 1) // 2)).astype(np.uint8)
+    scales = scale_words(0.01 * (0.5 + rng.random((n, groups))) * rng.choice([-1.0, 1.0], (n, groups)), scale_dtype)
+    z = rng.integers(0, 16, (n, groups)).astype(np.uint8) if zeros else None
+    return codes, scales, z, pkg.Quant(n, k, group, codes, scales, scale_dtype, z), weights(codes, scales_of(scales, scale_dtype), z, k, group), \
+        np.abs(scales_of(scales, scale_dtype))[:, np.arange(k) // group]
+
+
+def tolerance(xh, scale, y, y_dtype):
+    """A step of 32 inputs adds two products of at most 2 * 16 * scale * |x| each (in up to three parts, whose sizes add up to |x|), into a
+    sum that never holds more than all of them: at most 6 roundings a step if the matrix cores round once an instruction,
+    33 times as many if after every product.  Groups, waves and the norm add a rounding of the sum each."""
+    most = 64.0 * np.abs(xh) @ scale.T
+    steps = -(-xh.shape[1] // 32)
+    return (6 * 33 + 2 * steps + 16) * U32 * most + HALF_STEP[y_dtype] * np.abs(y) + TINY[y_dtype]
+
+
+def check(rng, n, k, group, rows, x_dtype, y_dtype, zeros=False, scale_dtype=F16, norm=False, scale=1.0, x_stride=None, y_stride=None, first=0,
+          stream=None, mean=0.0):
+    *_, q, w, s = matrix(rng, n, k, group, zeros, scale_dtype)
+    words = pack(rng.standard_normal((rows, k)) + mean, x_dtype)
+    x = Rows(words, x_stride, first)
+    y = Rows(pack(np.zeros((rows, n)), y_dtype), y_stride, first)
+    gain = (1.0 + 0.2 * rng.standard_normal(k)).astype(np.float32) if norm else None
+    g = DeviceArray(gain) if norm else None
+    q.matmul(x.ptr, x_dtype, rows, y.ptr, y_dtype, x.stride, y.stride, g.ptr.value if norm else None, 1e-6, scale, stream)
+    xh = normed(unpack(words, x_dtype), None if gain is None else gain.astype(np.float64), 1e-6)
+    want = scale * (xh @ w.T)
+    got = unpack(y.get(), y_dtype)
+    close(got, want, abs(scale) * tolerance(xh, s, want / scale, y_dtype))
+
+
+@pytest.mark.parametrize("x_dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows", [1, 2, 11, 16, 17, 32, 33, 70])
+def test_rows_and_groups(x_dtype, group, rows):
+    rng = np.random.default_rng(rows * 1000 + group + x_dtype)
+    check(rng, 80, 512, group, rows, x_dtype, x_dtype, zeros=group == 64, scale_dtype=BF16 if rows % 2 else F16)
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 128), (16, 2), (15, 33), (17, 31), (33, 127), (47, 129), (100, 257), (5, 1000), (250, 1153), (2049, 96)])
+@pytest.mark.parametrize("x_dtype,y_dtype", [(F32, F32), (BF16, F32), (F16, BF16), (BF16, F16)])
+def test_ragged_sizes(n, k, x_dtype, y_dtype):
+    rng = np.random.default_rng(n * 7 + k)
+    for rows, group, zeros in ((1, 32, True), (3, 128, False), (19, 64, True)):
+        check(rng, n, k, group, rows, x_dtype, y_dtype, zeros=zeros)
+
+
+@pytest.mark.parametrize("x_dtype", [F32, BF16, F16])
+def test_norm_in_front(x_dtype):
+    rng = np.random.default_rng(5 + x_dtype)
+    for rows, n, k in ((1, 64, 512), (1, 31, 77), (4, 48, 1024), (29, 20, 640), (40, 33, 384)):
+        check(rng, n, k, 64, rows, x_dtype, F32, norm=True, scale=0.7, mean=0.5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_strides_and_addresses(dtype):
+    """Rows apart, rows whose addresses are multiples of their type alone, nothing written beside them."""
+    rng = np.random.default_rng(9)
+    for rows, x_stride, y_stride, first in ((5, 300, 90, 0), (5, 301, 91, 1), (18, 257, 83, 3), (1, 0, 0, 1)):
+        check(rng, 83, 257, 32, rows, dtype, dtype, x_stride=x_stride, y_stride=y_stride, first=first)
+    # one row of x for all rows of y
+    *_, q, w, s = matrix(rng, 40, 96, 32)
+    x, y = Rows(pack(rng.standard_normal((1, 96)), dtype)), Rows(pack(np.zeros((6, 40)), F32))
+    q.matmul(x.ptr, dtype, 6, y.ptr, F32, x_stride=0)
+    got = y.get()
+    assert np.all(got == got[0])
+
+
+def test_values_far_from_zero_lose_nothing():
+    """Inputs around 50 (what a code's offset adds is taken off step by step), inputs of very different sizes in a row, subnormal ones."""
+    rng = np.random.default_rng(10)
+    check(rng, 64, 4096, 128, 2, F32, F32, mean=50.0)
+    codes, scales, z, q, w, s = matrix(rng, 64, 256, 32, True)
+    x = rng.standard_normal((3, 256)) * 10.0 ** rng.integers(-30, 20, (3, 256))
+    x[2] = 1e-40
+    for dtype in (F32, BF16):
+        words = pack(x, dtype)
+        xd, y = Rows(words), Rows(pack(np.zeros((3, 64)), F32))
+        q.matmul(xd.ptr, dtype, 3, y.ptr, F32)
+        xv = unpack(words, dtype)
+        want = xv @ w.T
+        close(y.get()[:2], want[:2], tolerance(xv, s, want, F32)[:2])
+
+
+def test_long_rows():
+    rng = np.random.default_rng(11)
+    check(rng, 24, 40000, 128, 3, BF16, F32, zeros=True)
+    check(rng, 7000, 64, 32, 2, F16, F16)
+
+
+def test_a_row_that_is_not_finite_stays_alone():
+    rng = np.random.default_rng(12)
+    *_, q, w, s = matrix(rng, 50, 200, 32)
+    for dtype in (F32, BF16, F16):
+        x = rng.standard_normal((4, 200))
+        clean = Rows(pack(x, dtype))
+        y0, y1 = Rows(pack(np.zeros((4, 50)), F32)), Rows(pack(np.zeros((4, 50)), F32))
+        q.matmul(clean.ptr, dtype, 4, y0.ptr, F32)
+        x[1, 17], x[2, 199] = np.inf, np.nan
+        dirty = Rows(pack(x, dtype))
+        q.matmul(dirty.ptr, dtype, 4, y1.ptr, F32)
+        a, c = y0.get(), y1.get()
+        assert np.array_equal(a[[0, 3]], c[[0, 3]])
+        assert not np.any(np.isfinite(c[1:3]))
+
+
+def test_rows_do_not_depend_on_their_company():
+    """A row's result is the same bits alone and in any block that runs through the same kernel."""
+    rng = np.random.default_rng(13)
+    *_, q, w, s = matrix(rng, 96, 640, 64, True)
+    x = pack(rng.standard_normal((16, 640)), BF16)
+    whole = Rows(pack(np.zeros((16, 96)), F32))
+    xd = Rows(x)
+    q.matmul(xd.ptr, BF16, 16, whole.ptr, F32)
+    again = Rows(pack(np.zeros((16, 96)), F32))
+    q.matmul(xd.ptr, BF16, 16, again.ptr, F32)
+    assert np.array_equal(whole.get(), again.get())
+    part = Rows(pack(np.zeros((9, 96)), F32))
+    q.matmul(xd.ptr + 5 * 640 * 2, BF16, 9, part.ptr, F32)
+    assert np.array_equal(whole.get()[5:14], part.get())
+
+
+def test_from_device_memory_and_rounded_from_fp32():
+    rng = np.random.default_rng(14)
+    w = (0.02 * rng.standard_normal((48, 200))).astype(np.float32)
+    x = Rows(pack(rng.standard_normal((3, 200)), F32))
+    for zeros in (False, True):
+        codes, scales, z = pkg.quant_round(w, 64, BF16, zeros)
+        devs = [DeviceArray(a) for a in (codes, scales)] + ([DeviceArray(z)] if zeros else [])
+        a = pkg.Quant(48, 200, 64, codes, scales, BF16, z)
+        c = pkg.Quant(48, 200, 64, devs[0].ptr.value, devs[1].ptr.value, BF16, devs[2].ptr.value if zeros else None)
+        ya, yc = Rows(pack(np.zeros((3, 48)), F32)), Rows(pack(np.zeros((3, 48)), F32))
+        a.matmul(x.ptr, F32, 3, ya.ptr, F32)
+        c.matmul(x.ptr, F32, 3, yc.ptr, F32)
+        assert np.array_equal(ya.get(), yc.get())
+        wq = weights(codes, scales_of(scales, BF16), z, 200, 64)
+        s = np.abs(scales_of(scales, BF16))[:, np.arange(200) // 64]
+        xv = unpack(x.get(), F32)
+        close(ya.get(), xv @ wq.T, tolerance(xv, s, xv @ wq.T, F32))
+
+
+def test_streams_and_captured_launches():
+    rng = np.random.default_rng(15)
+    *_, q, w, s = matrix(rng, 128, 512, 128, True)
+    xs = [pack(rng.standard_normal((7, 512)), BF16) for _ in range(4)]
+    x = Rows(xs[0])
+    stream = Stream()
+    y, eager = Rows(pack(np.zeros((7, 128)), F32)), Rows(pack(np.zeros((7, 128)), F32))
+    graph = Graph(stream, lambda st: q.matmul(x.ptr, BF16, 7, y.ptr, F32, stream=st))
+    for words in xs:
+        stream.sync()
+        assert hip().hipMemcpy(x.dev.ptr, np.ascontiguousarray(words).ctypes.data, words.nbytes, 1) == 0
+        graph.replay()
+        stream.sync()
+        q.matmul(x.ptr, BF16, 7, eager.ptr, F32)
+        x.host[:words.size] = words.ravel()
+        assert np.array_equal(y.get(), eager.get())
+
+
+def test_refusals_leave_y_alone():
+    rng = np.random.default_rng(16)
+    *_, q, w, s = matrix(rng, 40, 96, 32)
+    x, y = Rows(pack(rng.standard_normal((2, 96)), F32)), Rows(pack(np.zeros((2, 40)), F32))
+    for kw in (dict(rows=0), dict(rows=-3), dict(x=None), dict(y=None), dict(x_dtype=3), dict(y_dtype=-1), dict(eps=-1.0), dict(eps=float("nan"))):
+        a = dict(x=x.ptr, x_dtype=F32, rows=2, y=y.ptr, y_dtype=F32)
+        a.update(kw)
+        with pytest.raises(pkg.BildError) as e:
+            q.matmul(**a)
+        assert e.value.code == b.EINVAL
+    assert np.all(y.get() == 0)
+    codes, scales = np.zeros((4, 16), np.uint8), np.zeros((4, 1), np.uint16)
+    with pytest.raises(pkg.BildError) as e:
+        pkg.Quant(4, 32, 32, codes, scales, F16, np.full((4, 1), 16, np.uint8))
+    assert e.value.code == b.EINVAL
