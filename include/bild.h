@@ -300,7 +300,8 @@ typedef struct bild_quant bild_quant; /* the matrix on the device, immutable */
 int bild_quant_round(const float* host_w, int n, int k, int inputs_first, int group, int scale_dtype, uint8_t* host_codes, void* host_scales,
                      uint8_t* host_zeros /* nullable */);
 /* Uploads a matrix given as above.  The arrays may be in host or in device memory (whatever wrote them there has to be done) and are copied.  group is 32, 64 or 128.
- * BILD_EINVAL for another group, a scale type that is not 16 bits wide or a zero above 15; the matrix lies on the current device. */
+ * BILD_EINVAL for another group, a scale type that is not 16 bits wide, a zero above 15, or bf16 scales so far apart that no power of two makes all of
+ * them fp16 (a factor of 2^32 between the largest and the smallest that is not zero always fits); the matrix lies on the current device. */
 int bild_quant_create(int n, int k, int group, const uint8_t* codes, const void* scales, int scale_dtype, const uint8_t* zeros /* nullable */,
                       bild_quant** out);
 int bild_quant_destroy(bild_quant* w); /* nothing that uses it may still run */

@@ -6,11 +6,11 @@
 struct bild_quant {
     int n = 0, k = 0, group = 0;
     int tn = 0, tk = 0;        // feature tiles, input tiles
-    int bf16_scales = 0;
+    int scale_exponent = 0;    // the scales are those stored times 2^this
     void* mem = nullptr;       // one allocation
     const uint4* codes = nullptr;     // [tn][tk][64 lanes]: see quant.hip
-    const uint16_t* scales = nullptr; // [tn][tk][4 feature quads][128 / group][4 features]
-    const uint8_t* zeros = nullptr;   // the same order; null: 8 everywhere
+    const uint16_t* scales = nullptr; // fp16, [tn][tk][4 feature quads][128 / group][4 features]
+    const uint8_t* zeros = nullptr;   // [tn][tk][16 features], four bits a group (a byte, two with groups of 32)
     int device = 0;
 };
 

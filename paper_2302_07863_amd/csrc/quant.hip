@@ -9,11 +9,13 @@
 // larger than 32 inputs' sum; scales are applied to the accumulators once a group.  No weight is ever rounded.
 //
 // Layout: tiles of 16 features x 128 inputs, 1 KiB, in the order of the matrix cores' A operand: lane l has feature l % 16, its word j
-// the inputs 32 j + 8 (l / 16) + 0 .. 7.  Of these, pair p (2p, 2p + 1) lies in the nibbles p and p + 4, the two halves of the word.  Scales (and
-// zeros) of a tile: the four features of an accumulator's lane side by side, one such group per group of inputs.
+// the inputs 32 j + 8 (l / 16) + 0 .. 7.  Of these, pair p (2p, 2p + 1) lies 4 p bits above the places where bf16 takes it (bits 3 .. 6 and 19 .. 22), the
+// last pair round the end of the word.  Scales of a tile: for the four features of an accumulator's lane side by side, group by group, as fp16 (which goes into
+// the products as it is) times a power of two of the whole matrix; zeros: feature by feature, four bits a group.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -29,10 +31,18 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTileK = 128;   // inputs of a tile
-constexpr int kMaxWaves = 8;
+constexpr int kTileK = 128;    // inputs of a tile
+constexpr int kMaxWaves = 16;
+// Waves that may share a feature tile: what their registers leave room for.
+constexpr int most_waves(int tiles) { return tiles <= 2 ? kMaxWaves : 8; }
+constexpr int kPartRows = 32;  // most rows of a workgroup
+// Tiles that a wave has under way (with a group per step of 32 inputs the scales take two thirds of a tile's registers).
+constexpr int ahead(int group) { return group == 32 ? 3 : 4; }
+constexpr int kChipUnits = 256;  // compute units
+constexpr int kLdsLimit = 160 * 1024;
 
-// Rows as the matrix cores take them: bf16 and fp16 as they are; fp32, and rows with a norm's gain, as three bf16 parts.
+// Rows as the matrix cores take them.  bf16 and fp16 rows as they are; fp32 rows, and rows with a norm's gain, as three bf16 parts each, whose
+// sum is the value to 24 bits.  A part is a row of its own to the matrix cores: up to five such rows cost no more instructions than one.
 enum RowsAs : int { AS_BF16 = 0, AS_F16 = 1, AS_PARTS = 2 };
 
 struct QuantArgs {
@@ -44,8 +54,15 @@ struct QuantArgs {
     const float* gain;
     int64_t ldx, ldy;
     int n, k, tn, tk, rows;
-    int x_dtype, y_dtype, bf16_scales;
-    float eps, scale;
+    int x_dtype, y_dtype;
+    float eps, scale;  // (the scale with what codes and scales are short of)
+    int rows_per;  // rows of a workgroup
+    int wk, lwk;   // waves that share a feature tile's inputs (a power of two)
+    int per;       // feature tiles of a wave, one after the other (1 where there are several chunks)
+    int chunk;     // input tiles staged at a time
+    int chunks;
+    int turns;     // of a wave over them (several chunks: a multiple of ahead())
+    int sums_at;   // where in LDS the sums lie: behind the rows, or (per 1) in their place
 };
 
 template <int AS>
@@ -54,79 +71,40 @@ __device__ __forceinline__ f32x4 mac(const uint4& a, const uint4& b, const f32x4
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// What turns codes into numbers, in registers: an and-or has room for one constant that is none.
+struct CodeBits {
+    uint32_t mask, one;
+};
+template <int AS>
+__device__ __forceinline__ CodeBits code_bits() {
+    CodeBits b = AS == AS_F16 ? CodeBits{0x03C003C0u, 0x3C003C00u} : CodeBits{0x00780078u, 0x3F803F80u};
+    asm("" : "+s"(b.mask));
+    asm("" : "+v"(b.one));
+    return b;
+}
 // Eight codes as 1 + q / 16.
 template <int AS>
-__device__ __forceinline__ uint4 codes_up(uint32_t w) {
-    if constexpr (AS == AS_F16) {
-        constexpr uint32_t m = 0x03C003C0u, one = 0x3C003C00u;
-        return make_uint4(((w << 6) & m) | one, ((w << 2) & m) | one, ((w >> 2) & m) | one, ((w >> 6) & m) | one);
-    } else {
-        constexpr uint32_t m = 0x00780078u, one = 0x3F803F80u;
-        return make_uint4(((w << 3) & m) | one, ((w >> 1) & m) | one, ((w >> 5) & m) | one, ((w >> 9) & m) | one);
-    }
+__device__ __forceinline__ uint4 codes_up(uint32_t w, const CodeBits& b) {
+    if constexpr (AS == AS_F16)
+        return make_uint4(((w << 3) & b.mask) | b.one, ((w >> 1) & b.mask) | b.one, ((w >> 5) & b.mask) | b.one,
+                          (__builtin_amdgcn_alignbit(w, w, 9) & b.mask) | b.one);
+    else
+        return make_uint4((w & b.mask) | b.one, ((w >> 4) & b.mask) | b.one, ((w >> 8) & b.mask) | b.one,
+                          (__builtin_amdgcn_alignbit(w, w, 12) & b.mask) | b.one);
 }
 // -(1 + z / 16), twice
 template <int AS>
 __device__ __forceinline__ uint32_t zero_up(uint32_t z) {
-    const uint32_t h = AS == AS_F16 ? 0xBC00u | (z << 6) : 0xBF80u | (z << 3);
-    return h | (h << 16);
+    return AS == AS_F16 ? 0xBC00BC00u + z * 0x00400040u : 0xBF80BF80u + z * 0x00080008u;
 }
 
-// Eight values of a row in up to three parts that the matrix cores take.
-template <int AS>
-struct Frag {
-    uint4 part[AS == AS_PARTS ? 3 : 1];
-};
-
-__device__ __forceinline__ void split3(const float (&v)[8], Frag<AS_PARTS>& f) {
-    uint32_t p[3][4];
+// Two values' three bf16 parts.
+__device__ __forceinline__ void split3(float a, float b, uint32_t (&p)[3]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a = v[2 * i], b = v[2 * i + 1];
-#pragma unroll
-        for (int j = 0; j < 3; ++j) {
-            const uint32_t h = pack_bf16x2(a, b);
-            p[j][i] = h;
-            a -= __uint_as_float(h << 16);
-            b -= __uint_as_float(h & 0xFFFF0000u);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 3; ++j) f.part[j] = make_uint4(p[j][0], p[j][1], p[j][2], p[j][3]);
-}
-
-template <class R>
-__device__ __forceinline__ void up8(const R*, const void* row, int k0, int k, float (&v)[8]) {
-    RowVec<R, 8> r;
-    const typename R::type* p = (const typename R::type*)row + k0;
-    if (k0 + 8 <= k) r.load(p); else r.load_some(p, k - k0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = R::up(r.v[i]);
-}
-
-// Inputs k0 .. k0 + 7 of a row (zero from the k-th on); AS_PARTS: times the gain, squares added to ss.
-template <int AS>
-__device__ __forceinline__ void load_frag(const QuantArgs& a, const char* row, int k0, Frag<AS>& f, float& ss) {
-    if constexpr (AS == AS_PARTS) {
-        float v[8];
-        if (a.x_dtype == BILD_DT_F32) up8((const RowF32*)nullptr, row, k0, a.k, v);
-        else if (a.x_dtype == BILD_DT_BF16) up8((const RowBf16*)nullptr, row, k0, a.k, v);
-        else up8((const RowF16*)nullptr, row, k0, a.k, v);
-        if (a.gain) {
-            float g[8];
-            up8((const RowF32*)nullptr, a.gain, k0, a.k, g);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                ss = __builtin_fmaf(v[i], v[i], ss);
-                v[i] *= g[i];
-            }
-        }
-        split3(v, f);
-    } else {
-        RowVec<RowBf16, 8> r;  // (16 bits are 16 bits)
-        const uint16_t* p = (const uint16_t*)row + k0;
-        if (k0 + 8 <= a.k) r.load(p); else r.load_some(p, a.k - k0);
-        __builtin_memcpy(&f.part[0], r.v, 16);
+    for (int j = 0; j < 3; ++j) {
+        p[j] = pack_bf16x2(a, b);
+        a -= __uint_as_float(p[j] << 16);
+        b -= __uint_as_float(p[j] & 0xFFFF0000u);
     }
 }
 
@@ -147,87 +125,307 @@ __device__ __forceinline__ void store_y(const QuantArgs& a, int row, int n0, con
     else put(RowF16());
 }
 
-// NT row tiles of 16; the workgroup's waves share a feature tile, each takes every nw-th input tile of it.
-template <int AS, int G, int NT>
-__global__ __launch_bounds__(64 * kMaxWaves) void quant_kernel(const QuantArgs a) {
+// Eight inputs of row r, as they are or times the gain in three parts, to their place in the operand; their squares (with a gain).
+template <class R, bool PARTS>
+__device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&g)[8], bool gain, char* to, int rows, bool real) {
+    if constexpr (!PARTS) {
+        uint4 q;
+        __builtin_memcpy(&q, x.v, 16);
+        if (real) *(uint4*)to = q;
+        return 0.f;
+    } else {
+        float ss = 0.f;
+        uint32_t q[4][3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float a = R::up(x.v[2 * j]), b = R::up(x.v[2 * j + 1]);
+            if (gain) {
+                ss = __builtin_fmaf(a, a, __builtin_fmaf(b, b, ss));
+                a *= g[2 * j];
+                b *= g[2 * j + 1];
+            }
+            split3(a, b, q[j]);
+        }
+        if (real) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *(uint4*)(to + (size_t)p * rows * 64) = make_uint4(q[0][p], q[1][p], q[2][p], q[3][p]);
+        }
+        return ss;
+    }
+}
+
+// The workgroup's rows, inputs of the tiles t0 .. t1 - 1, to LDS in the order of the matrix cores' B operand:
+// [step of 32 inputs][row of the operand][4 pieces of 8].  Row v of the operand is part v / rows of row v % rows.  Inputs from the k-th on are zero.
+// A wave's 64 pieces belong to one row; with a norm it adds up their squares.  `between` runs behind the requests of the first U pieces a thread
+// (loads come back in order: what it requests does not keep these waiting).
+template <class R, bool PARTS, int U, class Between>
+__device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (*squares)[kPartRows], int r0, int rows, int t0, int t1, Between&& between) {
+    const int nthr = blockDim.x, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int k0 = t0 * kTileK, pieces = (t1 - t0) * (kTileK / 8), span = (pieces + 63) & ~63;
+    const int full = min(max((a.k - k0) / 8, 0), pieces);  // pieces that are there as a whole
+    const bool tail = (a.k & 7) != 0 && full < pieces;     // one more is there in part
+    const int v = PARTS ? 3 * rows : rows;                 // rows of the operand
+    const bool gain = PARTS && a.gain;
+    const auto place = [&](int p, int r) { return xs + ((size_t)((p >> 2) * v + r) * 4 + (p & 3)) * 16; };
+    RowVec<R, 8> x[U];
+    float g[U][8];
+    const auto load = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * nthr + tid, r = min(__builtin_amdgcn_readfirstlane((i & ~63) / span), rows - 1), p = i - r * span;
+            __builtin_memset(x[u].v, 0, sizeof(x[u].v));
+            if (full > 0) {  // (past the end: a valid address, replaced below)
+                const int k = k0 + min(p, full - 1) * 8;
+                x[u].load((const typename R::type*)a.x + (int64_t)(r0 + r) * a.ldx + k);
+                if (gain) {
+                    RowVec<RowF32, 8> t;
+                    t.load(a.gain + k);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[u][j] = t.v[j];
+                }
+            }
+        }
+    };
+    const auto put = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * nthr + tid, r = __builtin_amdgcn_readfirstlane((i & ~63) / span), p = i - r * span;
+            if (r >= rows) break;
+            if (p >= full) __builtin_memset(x[u].v, 0, sizeof(x[u].v));
+            const float ss = put_piece<R, PARTS>(x[u], g[u], gain, place(p, r), rows, p < pieces && !(tail && p == full));
+            if (gain) {
+                const float all = wave_sum(ss);
+                if ((tid & 63) == 0) squares[wave][r] += all;
+            }
+        }
+    };
+    load(0);
+    __builtin_amdgcn_sched_barrier(0);
+    between();
+    __builtin_amdgcn_sched_barrier(0);
+    put(0);
+    for (int i0 = U * nthr; i0 < rows * span; i0 += U * nthr) {
+        load(i0);
+        put(i0);
+    }
+    // the piece that the last input lies in (nobody else writes it)
+    if (!tail || tid >= rows) return;
+    RowVec<R, 8> y;
+    RowVec<RowF32, 8> h;
+    const int n = a.k & 7, k = a.k - n;
+    y.load_some((const typename R::type*)a.x + (int64_t)(r0 + tid) * a.ldx + k, n);
+    h.load_some(a.gain ? a.gain + k : nullptr, gain ? n : 0);
+    const float ss = put_piece<R, PARTS>(y, h.v, gain, place(full, tid), rows, true);
+    if (gain) squares[0][tid] += ss;
+}
+
+// What a wave has requested of one tile.
+template <int GT>
+struct Unit {
+    uint4 codes;
+    uint2 scales[GT];
+    uint32_t zeros;
+};
+
+// A workgroup has up to rows_per rows (NT tiles of 16 rows of the operand) and stages them once, or (CHUNKED) chunk by chunk of the inputs where they do
+// not fit.  wk of its waves share a feature tile, each takes every wk-th of the input tiles; a wave goes through `per` feature tiles (CHUNKED: one).  It streams their
+// tiles of codes one behind the other, ahead() of them under way.  Nothing is stored before the last one: stores would be counted among the loads that the waves
+// wait for.  The sums meet in LDS.
+template <int AS, int G, int NT, bool CHUNKED>
+__global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantArgs a) {
     constexpr int GT = kTileK / G;  // groups of a tile
     constexpr int SG = G / 32;      // steps of a group
-    __shared__ f32x4 part[kMaxWaves][NT][64];
-    __shared__ float squares[kMaxWaves][NT][64];
+    constexpr int kAhead = ahead(G);
+    constexpr int PARTS = AS == AS_PARTS ? 3 : 1;
+    constexpr int CH = NT == 1 && SG > 1 ? 2 : 1;  // chains of products: of one row tile the odd steps have their own
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float squares[kMaxWaves][kPartRows];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
-    const int ft = blockIdx.x, r0 = blockIdx.y * (16 * NT);
-    const int xb = a.x_dtype == BILD_DT_F32 ? 4 : 2;
-    const char* row[NT];
+    const int wk = a.wk, wkid = wave & (wk - 1), wfid = wave >> a.lwk, wf = nw >> a.lwk;
+    const int r0 = blockIdx.y * a.rows_per, rows = min(a.rows_per, a.rows - r0), v = PARTS * rows;
+    const int f0 = (int)blockIdx.x * wf * a.per + wfid;  // the wave's feature tiles: every wf-th from here (some of the last workgroup's are not there: they load the last one's)
+    const int turns = a.turns, segments = CHUNKED ? a.chunks : a.per;
+    f32x4* sums = (f32x4*)(lds + a.sums_at);  // [feature tile of a wave][wave][row tile][lane]
+
+    // the tile of a segment's turn (past the end: the last one there is)
+    int ps = 0, pj = 0;
+    const auto request = [&](Unit<GT>& u) {
+        const int f = min(f0 + (CHUNKED ? 0 : ps) * wf, a.tn - 1), kt = min((CHUNKED ? ps * a.chunk : 0) + wkid + pj * wk, a.tk - 1);
+        const size_t tile = (size_t)f * a.tk + kt;
+        u.codes = a.codes[tile * 64 + lane];
+        const uint2* s = (const uint2*)a.scales + (tile * 4 + (lane >> 4)) * GT;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) row[t] = (const char*)a.x + (int64_t)min(r0 + t * 16 + (lane & 15), a.rows - 1) * a.ldx * xb;
+        for (int i = 0; i < GT; ++i) u.scales[i] = s[i];
+        if constexpr (GT == 4) u.zeros = ((const uint16_t*)a.zeros)[tile * 16 + (lane & 15)];
+        else u.zeros = a.zeros[tile * 16 + (lane & 15)];
+        if (++pj == turns) {
+            pj = 0;
+            ps = min(ps + 1, segments - 1);
+        }
+    };
+    Unit<GT> ring[kAhead];
+    const auto first = [&] {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (CHUNKED || i < segments * turns) request(ring[i]);
+    };
+    const auto stage = [&](int t0, auto&& between) {
+        const int t1 = min(t0 + a.chunk, a.tk);
+        if constexpr (AS == AS_PARTS) {
+            if (a.x_dtype == BILD_DT_F32) stage_rows<RowF32, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            else if (a.x_dtype == BILD_DT_BF16) stage_rows<RowBf16, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            else stage_rows<RowF16, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
+        } else {  // (16 bits are 16 bits)
+            if (rows * ((t1 - t0) * (kTileK / 8)) <= (int)blockDim.x) stage_rows<RowBf16, false, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            else stage_rows<RowBf16, false, 4>(a, lds, squares, r0, rows, t0, t1, between);
+        }
+    };
+    const CodeBits bits = code_bits<AS>();
     f32x4 total[NT];
-    float ss[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        total[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        ss[t] = 0.f;
-    }
-    for (int kt = wave; kt < a.tk; kt += nw) {
-        const size_t tile = (size_t)ft * a.tk + kt;
-        const uint4 c = a.codes[tile * 64 + lane];
-        const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+    for (int t = 0; t < NT; ++t) total[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int col[NT];  // the lane's row of the operand (past the last: that one again, its results are nobody's)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) col[t] = min(t * 16 + (lane & 15), v - 1) * 64 + (lane >> 4) * 16;
+
+    const auto process = [&](const Unit<GT>& u, int at) {  // tile `at` of those staged
+        const uint32_t cw[4] = {u.codes.x, u.codes.y, u.codes.z, u.codes.w};
+        int xs = at * 4 * v * 64;
+        asm volatile("" : "+v"(xs));  // (else the compiler keeps an address for every operand of the tiles ahead in a register)
 #pragma unroll
         for (int g = 0; g < GT; ++g) {
-            uint32_t zw = zero_up<AS>(8);
-            if (a.zeros) zw = zero_up<AS>(a.zeros[((tile * 4 + ((lane & 15) >> 2)) * GT + g) * 4 + (lane & 3)]);
+            const uint32_t zw = zero_up<AS>(GT == 1 ? u.zeros : u.zeros >> (4 * g) & 15u);
             const uint4 za = make_uint4(zw, zw, zw, zw);
-            const uint2 sw = *(const uint2*)(a.scales + ((tile * 4 + (lane >> 4)) * GT + g) * 4);
-            f32x4 acc[NT];
+            f32x4 acc[NT][CH];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < SG; ++s) {
                 const int j = g * SG + s;
-                const uint4 ca = codes_up<AS>(cw[j]);
+                const uint4 ca = codes_up<AS>(cw[j], bits);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    Frag<AS> f;
-                    load_frag<AS>(a, row[t], kt * kTileK + j * 32 + 8 * (lane >> 4), f, ss[t]);
-#pragma unroll
-                    for (int p = (int)(sizeof(f) / 16) - 1; p >= 0; --p) {
-                        acc[t] = mac<AS>(ca, f.part[p], acc[t]);
-                        acc[t] = mac<AS>(za, f.part[p], acc[t]);
-                    }
+                    const uint4 b = *(const uint4*)(lds + col[t] + (xs + j * v * 64));
+                    acc[t][s % CH] = mac<AS>(ca, b, acc[t][s % CH]);
+                    acc[t][s % CH] = mac<AS>(za, b, acc[t][s % CH]);
                 }
             }
-            const uint32_t sh[4] = {sw.x & 0xFFFFu, sw.x >> 16, sw.y & 0xFFFFu, sw.y >> 16};
+            typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+            const f16x4 sv = __builtin_bit_cast(f16x4, u.scales[g]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float sv = a.bf16_scales ? bf2f(sh[i]) : RowF16::up((uint16_t)sh[i]);
+            for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) total[t][i] = __builtin_fmaf(sv, acc[t][i], total[t][i]);
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf((float)sv[i], acc[t][c][i], total[t][i]);
+                asm volatile("" : "+v"(total[t]));  // (now: four registers less than a group that waits)
             }
         }
-    }
+    };
+    const auto keep = [&](int s) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        part[wave][t][lane] = total[t];
-        squares[wave][t][lane] = ss[t];
-    }
-    __syncthreads();
-    for (int t = wave; t < NT; t += nw) {
-        f32x4 sum = part[0][t][lane];
-        for (int w = 1; w < nw; ++w) sum += part[w][t][lane];
-        float f = 16.f * a.scale;
-        if (a.gain) {  // (four lanes have a row's inputs)
-            float q = 0.f;
-            for (int w = 0; w < nw; ++w)
-                for (int i = 0; i < 4; ++i) q += squares[w][t][(lane & 15) + 16 * i];
-            f *= 1.f / sqrtf(q / (float)a.k + a.eps);
+        for (int t = 0; t < NT; ++t) {
+            sums[((s * nw + wave) * NT + t) * 64 + lane] = total[t];
+            total[t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int r = r0 + t * 16 + (lane & 15);
-        if (r < a.rows) store_y(a, r, ft * 16 + 4 * (lane >> 4), sum * f);
+    };
+
+    if (AS == AS_PARTS && lane < kPartRows) squares[wave][lane] = 0.f;
+    stage(0, first);
+    lds_barrier();
+    if constexpr (CHUNKED) {  // (turns: a multiple of kAhead, what is too much is skipped)
+        for (int s = 0; s < segments; ++s) {
+            const int t0 = s * a.chunk, n = min(a.chunk, a.tk - t0);
+            if (s) {
+                lds_barrier();
+                stage(t0, [] {});
+                lds_barrier();
+            }
+            for (int j = 0; j < turns; j += kAhead) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int at = wkid + (j + i) * wk;
+                    if (at < n) process(ring[i], at);
+                    request(ring[i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        lds_barrier();  // (the sums take the rows' place)
+        keep(0);
+    } else {
+        const int all = segments * turns;
+        int s = 0, j = 0;
+        const auto turn = [&](const Unit<GT>& u) {
+            const int at = wkid + j * wk;
+            if (at < a.tk) process(u, at);
+            if (++j < turns) return;
+            if (a.per > 1) keep(s);
+            j = 0;
+            s += 1;
+        };
+        int q = 0;
+        for (; all - q > kAhead; q += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                turn(ring[i]);
+                request(ring[i]);  // (past the end: the last one again)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (q + i < all) turn(ring[i]);
+        if (a.per == 1) {
+            lds_barrier();
+            keep(0);
+        }
     }
+    lds_barrier();
+    // What the waves have of a row's four features, over its parts, to y.
+    const int items = a.per * wf * rows * 4;
+    for (int it = threadIdx.x; it < items; it += blockDim.x) {
+        const int q = it & 3, fr = it >> 2, fl = fr / rows, r = fr - fl * rows;  // feature tile fl of the workgroup's
+        const int p = fl / wf, w0 = (fl - p * wf) << a.lwk;
+        f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; --part) {
+            const int c = part * rows + r;
+            const f32x4* from = sums + ((p * nw + w0) * NT + (c >> 4)) * 64 + q * 16 + (c & 15);
+#pragma unroll 4
+            for (int w = 0; w < wk; ++w) sum += from[w * NT * 64];
+        }
+        float s = a.scale;
+        if (AS == AS_PARTS && a.gain) {
+            float ss = 0.f;
+#pragma unroll 8
+            for (int w = 0; w < nw; ++w) ss += squares[w][r];
+            s *= 1.f / sqrtf(ss / (float)a.k + a.eps);
+        }
+        store_y(a, r0 + r, ((int)blockIdx.x * wf * a.per + fl) * 16 + q * 4, sum * s);
+    }
+}
+
+// What bf16 scales ask of the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
+__global__ __launch_bounds__(256) void quant_range_kernel(const uint16_t* scales, size_t count, int* range) {
+    int most = -1024, least = 1024;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
+        const uint32_t h = scales[i] & 0x7FFFu, e = h >> 7, m = h & 0x7Fu;
+        if (h == 0 || e == 255) continue;  // (zero, and what is not finite, go through any)
+        const uint32_t bits = e ? 0x80u | m : m;
+        const int unit = (int)(e ? e : 1) - 127 - 7;
+        most = max(most, unit + 31 - __builtin_clz(bits));
+        least = min(least, unit + __builtin_ctz(bits));
+    }
+    atomicMax(range, most);
+    atomicMin(range + 1, least);
 }
 
 // From rows of codes (two a byte), scales and zeros to tiles.  A thread per lane and tile; `bad`: a zero above 15.
 __global__ __launch_bounds__(256) void quant_layout_kernel(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, int k, int group, int tk, size_t lanes,
-                                                           uint32_t* to_codes, uint16_t* to_scales, uint8_t* to_zeros, unsigned* bad) {
+                                                           int bf16_shift, int bf16, uint32_t* to_codes, uint16_t* to_scales, uint8_t* to_zeros, unsigned* bad) {
     const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (at >= lanes) return;
     const int lane = (int)(at & 63);
@@ -240,34 +438,60 @@ __global__ __launch_bounds__(256) void quant_layout_kernel(const uint8_t* codes,
         for (int p = 0; p < 4; ++p) {
             const int kk = k0 + 2 * p;
             const uint32_t b = f < n && kk < k ? codes[(size_t)f * bytes + kk / 2] : 0u;
-            w |= (b & 15u) << (4 * p) | (b >> 4) << (4 * p + 16);
+            const uint32_t pair = (b & 15u) << 3 | (b >> 4) << 19;  // where bf16 takes them
+            w |= p == 0 ? pair : p == 3 ? pair << 12 | pair >> 20 : pair << (4 * p);
         }
         to_codes[at * 4 + j] = w;
     }
     const int gt = kTileK / group, groups = (k + group - 1) / group;
-    if (lane < 16)  // feature `lane` of the tile
-        for (int g = 0; g < gt; ++g) {
-            const int gg = kt * gt + g;
-            const bool in = f < n && gg < groups;
-            const size_t to = ((tile * 4 + (lane >> 2)) * gt + g) * 4 + (lane & 3);
-            to_scales[to] = in ? scales[(size_t)f * groups + gg] : (uint16_t)0;
-            if (!zeros) continue;
-            const unsigned z = in ? zeros[(size_t)f * groups + gg] : 0u;
-            if (z > 15u) *bad = 1u;
-            to_zeros[to] = (uint8_t)(z & 15u);
-        }
+    if (lane >= 16) return;  // feature `lane` of the tile
+    unsigned nibbles = 0;
+    for (int g = 0; g < gt; ++g) {
+        const int gg = kt * gt + g;
+        const bool in = f < n && gg < groups;
+        uint16_t s = in ? scales[(size_t)f * groups + gg] : (uint16_t)0;
+        if (bf16) s = RowF16::down(ldexpf(bf2f(s), bf16_shift));  // (exact: the caller has seen to it)
+        to_scales[((tile * 4 + (lane >> 2)) * gt + g) * 4 + (lane & 3)] = s;
+        const unsigned z = in && zeros ? zeros[(size_t)f * groups + gg] : 8u;
+        if (z > 15u) *bad = 1u;
+        nibbles |= (z & 15u) << (4 * g);
+    }
+    if (gt == 4) ((uint16_t*)to_zeros)[tile * 16 + lane] = (uint16_t)nibbles;
+    else to_zeros[tile * 16 + lane] = (uint8_t)nibbles;
 }
 
+template <void (*KERNEL)(QuantArgs)>
+hipError_t launch_kernel(const QuantArgs& a, dim3 grid, int waves, size_t lds, int device, hipStream_t st) {
+    if (lds > 64 * 1024) {  // (more than a workgroup gets without asking)
+        static std::atomic<uint64_t> asked{0};  // by device
+        const uint64_t bit = 1ull << (device & 63);
+        if (device > 63 || !(asked.load(std::memory_order_relaxed) & bit)) {
+            const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsLimit - 4096);
+            if (e != hipSuccess) return e;
+            asked.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    hipLaunchKernelGGL(KERNEL, grid, dim3(64 * waves), lds, st, a);
+    return hipGetLastError();
+}
 template <int AS, int G>
-void launch_rows(const QuantArgs& a, int waves, hipStream_t st) {
-    if (a.rows <= 16) hipLaunchKernelGGL((quant_kernel<AS, G, 1>), dim3(a.tn), dim3(64 * waves), 0, st, a);
-    else hipLaunchKernelGGL((quant_kernel<AS, G, 2>), dim3(a.tn, (a.rows + 31) / 32), dim3(64 * waves), 0, st, a);
+hipError_t launch_rows(const QuantArgs& a, int tiles, dim3 grid, int waves, size_t lds, int device, hipStream_t st) {
+#define BILD_Q(NT) \
+    return a.chunks > 1 ? launch_kernel<quant_kernel<AS, G, NT, true>>(a, grid, waves, lds, device, st) : launch_kernel<quant_kernel<AS, G, NT, false>>(a, grid, waves, lds, device, st)
+    if (tiles == 1) BILD_Q(1);
+    if (tiles == 2) BILD_Q(2);
+    if constexpr (AS == AS_PARTS) {
+        if (tiles == 3) BILD_Q(3);
+        BILD_Q(6);
+    }
+#undef BILD_Q
+    return hipErrorInvalidValue;
 }
 template <int AS>
-void launch_group(const QuantArgs& a, int group, int waves, hipStream_t st) {
-    if (group == 32) launch_rows<AS, 32>(a, waves, st);
-    else if (group == 64) launch_rows<AS, 64>(a, waves, st);
-    else launch_rows<AS, 128>(a, waves, st);
+hipError_t launch_group(const QuantArgs& a, int group, int tiles, dim3 grid, int waves, size_t lds, int device, hipStream_t st) {
+    if (group == 32) return launch_rows<AS, 32>(a, tiles, grid, waves, lds, device, st);
+    if (group == 64) return launch_rows<AS, 64>(a, tiles, grid, waves, lds, device, st);
+    return launch_rows<AS, 128>(a, tiles, grid, waves, lds, device, st);
 }
 
 bool shape_ok(int n, int k, int group) { return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 20) && (group == 32 || group == 64 || group == 128); }
@@ -324,14 +548,52 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
     a.rows = c.rows;
     a.x_dtype = c.x_dtype;
     a.y_dtype = c.y_dtype;
-    a.bf16_scales = w->bf16_scales;
     a.eps = c.eps;
-    a.scale = c.scale;
-    const int waves = std::max(1, std::min(kMaxWaves, w->tk));
-    if (c.gain || c.x_dtype == BILD_DT_F32) launch_group<AS_PARTS>(a, w->group, waves, st);
-    else if (c.x_dtype == BILD_DT_F16) launch_group<AS_F16>(a, w->group, waves, st);
-    else launch_group<AS_BF16>(a, w->group, waves, st);
-    return hipGetLastError() == hipSuccess ? BILD_OK : BILD_EHIP;
+    a.scale = (float)(16.0 * c.scale * std::ldexp(1.0, w->scale_exponent));
+    const bool parts = c.gain || c.x_dtype == BILD_DT_F32;
+    a.rows_per = std::min(c.rows, kPartRows);
+    const int v = a.rows_per * (parts ? 3 : 1);
+    const int tiles = v <= 16 ? 1 : v <= 32 ? 2 : v <= 48 ? 3 : 6;
+    const int row_blocks = (c.rows + a.rows_per - 1) / a.rows_per, tile_bytes = v * kTileK * 2;
+    const int turn = ahead(w->group), most = most_waves(tiles), wave_sums = tiles * 1024;
+    const int room = kLdsLimit - 4096;  // (beside the squares)
+    const int units = std::max(1, kChipUnits / row_blocks);
+    // How many waves share a feature tile, and how many tiles a workgroup has beside each other (no more than gives one to every compute unit) and one after the other.
+    const bool fits = w->tk * tile_bytes + wave_sums <= room;
+    int wf = 1, best = 0;
+    for (int wk = 1, l = 0; wk <= most && wk <= w->tk; wk *= 2, ++l) {
+        if (!fits && wk * tile_bytes > room) break;  // (of so few input tiles at a time every wave is to have one)
+        const int side = std::min(most / wk, (w->tn + units - 1) / units), waves = side * wk;
+        const int sums_room = fits ? std::max(1, (room - w->tk * tile_bytes) / (waves * wave_sums)) : 1;
+        const int per = std::max(1, std::min((w->tn + units * side - 1) / (units * side), sums_room));
+        const int rounds = (w->tn + units * side * per - 1) / (units * side * per);
+        // clocks of a compute unit: rows at 64 bytes each, a tile as fast as memory brings it or the matrix cores take it, the sums
+        const int cost = rounds * (v * w->k / 32 + per * (10 * ((w->tk + wk - 1) / wk) + 6) * std::max(waves, 12) * std::max(10, 6 * tiles));
+        if (best && cost >= best) continue;
+        best = cost;
+        a.wk = wk;
+        a.lwk = l;
+        a.per = per;
+        wf = side;
+    }
+    const int waves = wf * a.wk;
+    // The rows in LDS, all of them or as many input tiles as there is room for, in chunks of equal turns.
+    a.chunk = w->tk;
+    if (!fits) {
+        a.chunk = room / (a.wk * tile_bytes) * a.wk;
+        const int n = (w->tk + a.chunk - 1) / a.chunk;
+        a.chunk = ((w->tk + n - 1) / n + a.wk - 1) / a.wk * a.wk;
+    }
+    a.chunks = (w->tk + a.chunk - 1) / a.chunk;
+    a.turns = (a.chunk + a.wk - 1) / a.wk;
+    if (a.chunks > 1) a.turns = (a.turns + turn - 1) / turn * turn;
+    a.sums_at = a.per > 1 ? a.chunk * tile_bytes : 0;
+    const size_t sums = (size_t)a.per * waves * wave_sums, lds = a.per > 1 ? a.sums_at + sums : std::max((size_t)a.chunk * tile_bytes, sums);
+    const dim3 grid((w->tn + wf * a.per - 1) / (wf * a.per), row_blocks);
+    const hipError_t err = parts ? launch_group<AS_PARTS>(a, w->group, tiles, grid, waves, lds, w->device, st)
+                           : c.x_dtype == BILD_DT_F16 ? launch_group<AS_F16>(a, w->group, tiles, grid, waves, lds, w->device, st)
+                                                      : launch_group<AS_BF16>(a, w->group, tiles, grid, waves, lds, w->device, st);
+    return err == hipSuccess ? BILD_OK : BILD_EHIP;
 }
 
 }  // namespace bild
@@ -379,11 +641,10 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
     q->group = group;
     q->tn = (n + 15) / 16;
     q->tk = (k + kTileK - 1) / kTileK;
-    q->bf16_scales = scale_dtype == BILD_DT_BF16;
     const size_t tiles = (size_t)q->tn * q->tk, tile_scales = 16 * (size_t)(kTileK / group);
     const size_t groups = (size_t)(k + group - 1) / group;
     // what stays, and behind it what was given
-    const size_t code_bytes = tiles * 1024, scale_bytes = (tiles * tile_scales * 2 + 255) / 256 * 256, zero_bytes = zeros ? (tiles * tile_scales + 255) / 256 * 256 : 0;
+    const size_t code_bytes = tiles * 1024, scale_bytes = (tiles * tile_scales * 2 + 255) / 256 * 256, zero_bytes = (tiles * 16 * (group == 32 ? 2 : 1) + 255) / 256 * 256;
     const size_t raw_codes = (size_t)n * ((k + 1) / 2), raw_scales = (size_t)n * groups * 2, raw_zeros = zeros ? (size_t)n * groups : 0;
     const size_t scales_at = (raw_codes + 255) / 256 * 256, zeros_at = scales_at + (raw_scales + 255) / 256 * 256, bad_at = zeros_at + (raw_zeros + 255) / 256 * 256;
     char* raw = nullptr;
@@ -394,14 +655,29 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
     if (rc == BILD_OK) {
         q->codes = (const uint4*)q->mem;
         q->scales = (const uint16_t*)((char*)q->mem + code_bytes);
-        q->zeros = zeros ? (const uint8_t*)q->mem + code_bytes + scale_bytes : nullptr;
+        q->zeros = (const uint8_t*)q->mem + code_bytes + scale_bytes;
         unsigned bad = 0;
         bool ok = hipMemcpy(raw, codes, raw_codes, hipMemcpyDefault) == hipSuccess && hipMemcpy(raw + scales_at, scales, raw_scales, hipMemcpyDefault) == hipSuccess &&
                   (!zeros || hipMemcpy(raw + zeros_at, zeros, raw_zeros, hipMemcpyDefault) == hipSuccess) && hipMemset(raw + bad_at, 0, sizeof(unsigned)) == hipSuccess;
-        if (ok) {
-            const size_t lanes = tiles * 64;
+        const size_t lanes = tiles * 64;
+        const int bf16 = scale_dtype == BILD_DT_BF16;
+        if (ok && bf16) {  // fp16 times a power of two: its 11 bits and 40 binary places hold all of them, or the matrix is refused
+            int range[2] = {-1024, 1024};
+            int* at = (int*)(raw + bad_at + 16);
+            ok = hipMemcpy(at, range, sizeof(range), hipMemcpyHostToDevice) == hipSuccess;
+            if (ok) {
+                const size_t count = (size_t)n * groups;
+                hipLaunchKernelGGL(quant_range_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 1024)), dim3(256), 0, nullptr, (const uint16_t*)(raw + scales_at), count, at);
+                ok = hipGetLastError() == hipSuccess && hipMemcpy(range, at, sizeof(range), hipMemcpyDeviceToHost) == hipSuccess;
+            }
+            if (ok && range[0] >= range[1]) {
+                q->scale_exponent = range[0] - 15;
+                bad = range[1] - q->scale_exponent < -24;
+            }
+        }
+        if (ok && !bad) {
             hipLaunchKernelGGL(quant_layout_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, nullptr, (const uint8_t*)raw, (const uint16_t*)(raw + scales_at),
-                               zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, (uint32_t*)q->codes, (uint16_t*)q->scales,
+                               zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, -q->scale_exponent, bf16, (uint32_t*)q->codes, (uint16_t*)q->scales,
                                (uint8_t*)q->zeros, (unsigned*)(raw + bad_at));
             ok = hipGetLastError() == hipSuccess && hipMemcpy(&bad, raw + bad_at, sizeof(bad), hipMemcpyDeviceToHost) == hipSuccess;
         }
