@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -52,17 +53,25 @@ class RotaryConfig(C.Structure):
         (n, C.c_float) for n in ("base", "factor", "low", "high", "magnitude")]
 
 
-class RotaryRows(C.Structure):
-    """RotaryRows(src, dst, heads, src_token, src_head, dst_token, dst_head): device pointers, strides in elements."""
+class RotaryRowsStruct(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("src_token", C.c_int64), ("src_head", C.c_int64), ("dst_token", C.c_int64),
                 ("dst_head", C.c_int64), ("heads", C.c_int32), ("reserved", C.c_int32)]
 
-    def __init__(self, src=None, dst=None, heads=0, src_token=0, src_head=0, dst_token=0, dst_head=0):
-        super().__init__(src, dst, src_token, src_head, dst_token, dst_head, heads, 0)
+
+class RotaryRows:
+    """Rows that Rotary.apply turns: device pointers, strides in elements."""
+    __slots__ = ("fields",)
+
+    def __init__(self, src: Optional[int] = None, dst: Optional[int] = None, heads: int = 0, src_token: int = 0, src_head: int = 0, dst_token: int = 0,
+                 dst_head: int = 0):
+        self.fields = (src or 0, dst or 0, src_token, src_head, dst_token, dst_head, heads, 0)
+
+
+_NO_ROWS = RotaryRows()
 
 
 class RotaryCall(C.Structure):
-    _fields_ = [("q", RotaryRows), ("k", RotaryRows), ("positions", C.c_void_p)] + [
+    _fields_ = [("q", RotaryRowsStruct), ("k", RotaryRowsStruct), ("positions", C.c_void_p)] + [
         (n, C.c_int32) for n in ("first", "tokens", "d_head", "dtype", "inverse", "reserved")]
 
 
@@ -72,6 +81,13 @@ class RulesCall(C.Structure):
                 ("penalties", C.c_void_p), ("penalties_stride", C.c_int64), ("bias_ids", C.c_void_p), ("bias", C.c_void_p),
                 ("bias_stride", C.c_int64), ("bias_counts", C.c_void_p), ("mask", C.c_void_p), ("mask_stride", C.c_int64),
                 ("rows", C.c_int32), ("dtype", C.c_int32), ("max_tokens", C.c_int32), ("max_bias", C.c_int32)]
+
+
+# The calls' structs as bytes: one packing costs less than setting a ctypes structure field by field.
+_QUANT_CALL = struct.Struct("@PqPqPiiiff4x")
+_ROTARY_CALL = struct.Struct("@PPqqqqiiPPqqqqiiPiiiiii")
+_RULES_CALL = struct.Struct("@PqPqPPPqPPPqPPqPPqiiii")
+assert _QUANT_CALL.size == C.sizeof(QuantCall) and _ROTARY_CALL.size == C.sizeof(RotaryCall) and _RULES_CALL.size == C.sizeof(RulesCall)
 
 
 class BildError(RuntimeError):
@@ -111,14 +127,14 @@ _SIGS = {
     "bild_quant_round": (C.c_int, [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p] * 3),
     "bild_quant_create": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_void_p)]),
     "bild_quant_destroy": (C.c_int, [C.c_void_p]),
-    "bild_quant_matmul": (C.c_int, [C.c_void_p, C.POINTER(QuantCall), C.c_void_p]),
+    "bild_quant_matmul": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "bild_rotary_frequencies": (C.c_int, [C.POINTER(RotaryConfig), C.c_void_p, C.POINTER(C.c_double)]),
     "bild_rotary_create": (C.c_int, [C.POINTER(RotaryConfig), C.POINTER(C.c_void_p)]),
     "bild_rotary_destroy": (C.c_int, [C.c_void_p]),
-    "bild_rotary_apply": (C.c_int, [C.c_void_p, C.POINTER(RotaryCall), C.c_void_p]),
+    "bild_rotary_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "bild_rules_create": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_void_p)]),
     "bild_rules_destroy": (C.c_int, [C.c_void_p]),
-    "bild_rules_apply": (C.c_int, [C.c_void_p, C.POINTER(RulesCall), C.c_void_p]),
+    "bild_rules_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "bild_get_lengths": (C.c_int, [C.c_void_p] + [C.POINTER(C.c_int32)] * 4),
     "bild_get_sequence": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.POINTER(C.c_int32)]),
     "bild_debug_enable_logits": (C.c_int, [C.c_void_p, C.c_int]),
@@ -254,8 +270,9 @@ class Quant:
     def matmul(self, x: int, x_dtype: int, rows: int, y: int, y_dtype: int, x_stride: Optional[int] = None, y_stride: Optional[int] = None,
                gain: Optional[int] = None, eps: float = 0.0, scale: float = 1.0, stream: Optional[int] = None):
         """Device pointers; strides in elements (None: rows side by side)."""
-        call = QuantCall(x, self.k if x_stride is None else x_stride, y, self.n if y_stride is None else y_stride, gain, rows, x_dtype, y_dtype, eps, scale)
-        _check(lib().bild_quant_matmul(self.h, C.byref(call), stream), "bild_quant_matmul")
+        call = _QUANT_CALL.pack(x or 0, self.k if x_stride is None else x_stride, y or 0, self.n if y_stride is None else y_stride, gain or 0, rows,
+                                x_dtype, y_dtype, eps, scale)
+        _check(lib().bild_quant_matmul(self.h, call, stream), "bild_quant_matmul")
 
     def close(self):
         if self.h:
@@ -282,8 +299,8 @@ class Rotary:
 
     def apply(self, d_head: int, dtype: int, tokens: int, q: RotaryRows, k: Optional[RotaryRows] = None, positions: Optional[int] = None,
               first: int = 0, inverse: bool = False, stream: Optional[int] = None):
-        call = RotaryCall(q, k if k is not None else RotaryRows(), positions, first, tokens, d_head, dtype, int(inverse), 0)
-        _check(lib().bild_rotary_apply(self.h, C.byref(call), stream), "bild_rotary_apply")
+        call = _ROTARY_CALL.pack(*q.fields, *(k or _NO_ROWS).fields, positions or 0, first, tokens, d_head, dtype, int(inverse), 0)
+        _check(lib().bild_rotary_apply(self.h, call, stream), "bild_rotary_apply")
 
     def close(self):
         if self.h:
@@ -302,11 +319,15 @@ class Rules:
         self.h, self.vocab = h, vocab
 
     def apply(self, logits: int, dtype: int, rows: int, out: Optional[int] = None, stats: Optional[int] = None, targets: Optional[int] = None,
-              logits_stride: Optional[int] = None, out_stride: Optional[int] = None, stream: Optional[int] = None, **rules):
-        """Device pointers; strides in elements (None: rows side by side).  rules: the other fields of bild_rules_call by name."""
-        call = RulesCall(logits=logits, logits_stride=self.vocab if logits_stride is None else logits_stride, out=out,
-                         out_stride=self.vocab if out_stride is None else out_stride, targets=targets, stats=stats, rows=rows, dtype=dtype, **rules)
-        _check(lib().bild_rules_apply(self.h, C.byref(call), stream), "bild_rules_apply")
+              logits_stride: Optional[int] = None, out_stride: Optional[int] = None, tokens: Optional[int] = None, tokens_stride: int = 0,
+              lengths: Optional[int] = None, starts: Optional[int] = None, penalties: Optional[int] = None, penalties_stride: int = 0,
+              bias_ids: Optional[int] = None, bias: Optional[int] = None, bias_stride: int = 0, bias_counts: Optional[int] = None,
+              mask: Optional[int] = None, mask_stride: int = 0, max_tokens: int = 0, max_bias: int = 0, stream: Optional[int] = None):
+        """The fields of bild_rules_call by name: device pointers, strides in elements (None: rows side by side)."""
+        call = _RULES_CALL.pack(logits or 0, self.vocab if logits_stride is None else logits_stride, out or 0, self.vocab if out_stride is None else out_stride,
+                                targets or 0, stats or 0, tokens or 0, tokens_stride, lengths or 0, starts or 0, penalties or 0, penalties_stride,
+                                bias_ids or 0, bias or 0, bias_stride, bias_counts or 0, mask or 0, mask_stride, rows, dtype, max_tokens, max_bias)
+        _check(lib().bild_rules_apply(self.h, call, stream), "bild_rules_apply")
 
     def close(self):
         if self.h:

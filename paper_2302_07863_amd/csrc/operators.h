@@ -72,7 +72,7 @@ struct RulesArgs {
     int rows, vocab, dtype, max_tokens, max_bias;
     int parts, range;   // workgroups of a row, ids of each
     StatPart* part;     // [row][parts]
-    unsigned* arrived;  // [row]: zero between launches
+    unsigned* arrived;  // a line per row, zero between launches
 };
 hipError_t launch_rules(RulesArgs a, hipStream_t st);
 

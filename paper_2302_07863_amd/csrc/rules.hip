@@ -1,10 +1,10 @@
 // Rules on logits (bild_rules_apply): penalties for tokens that were there, biases, bit masks, and the softmax statistics of
 // what is left, in one pass over the logits.
 //
-// Bound: memory, every logit read and written once.  A workgroup takes a range of a row's ids.  What the row's tokens and
-// biases say about its ids it collects in a table in LDS, a word per id, from the whole list: a list of some thousand tokens
-// comes from the L2 faster than a table of counts for the whole vocabulary could be cleared and filled in memory, and counts
-// are whole numbers, so the order of the LDS atomics shows nowhere.  The last workgroup of a row joins the ranges' statistics.
+// Bound: memory, every logit read and written once.  A workgroup takes a range of a row's ids and requests all of its logits at once.  What the row's
+// tokens and biases say about its ids it collects in a table in LDS, a word per id, from the whole list: a list of some thousand tokens comes from the L2 faster
+// than a table of counts for the whole vocabulary could be cleared and filled in memory, and counts are whole numbers, so the order of the LDS atomics
+// shows nowhere.  A thread keeps the maximum and the sum of its ids as they come by; the last workgroup of a row joins those of its ranges.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -18,13 +18,16 @@
 
 using namespace bild;
 
-// A word of the table: how often the id occurs from `starts` on, whether it occurs at all, which of the biases is its last.
 namespace {
+// A word of the table: how often the id occurs from `starts` on, whether it occurs at all, which of the biases is its last.
 constexpr unsigned kCountBits = 20, kSeen = 1u << kCountBits, kBiasAt = kCountBits + 1;
 constexpr unsigned kCountMask = kSeen - 1;
 constexpr int kMaxTokens = (1 << kCountBits) - 1, kMaxBias = (1 << (32 - kBiasAt)) / 2 - 1;  // (1023)
 constexpr int kThreads = 256;
-constexpr int kMaxRange = 8192;  // ids of a workgroup: 32 KiB of table
+constexpr int kMaxRange = kThreads * 16;  // ids of a workgroup, 16 a thread: 16 KiB of table
+constexpr int kCountStride = 32;          // words between two rows' counts of arrivals: a line each (side by side, a thousand arrivals took 20 us)
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 struct Penalty {
     float rep, freq, pres;
@@ -44,17 +47,23 @@ __device__ __forceinline__ float apply(float z, unsigned w, const Penalty& p, co
     return z;
 }
 
+// Sums of exponentials are kept as sums of 2^(z log2 e - M), M the whole number above the largest z log2 e: two products and the
+// hardware's exponential a term, and what M takes off is exact.  The low part of log2 e keeps the argument to half a step.
+constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596299e-8f;
+constexpr float kFar = 1e30f;  // (the type's lowest value as a mask: there a difference of logits is what is left)
+__device__ __forceinline__ float whole_above(float m) { return m == -INFINITY || m == INFINITY ? 0.f : ceilf(m * kLog2e); }
+__device__ __forceinline__ float term(float z, float whole) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2eLow, __builtin_fmaf(z, kLog2e, -whole))); }
+// such a sum as one of e^(z - m)
+__device__ __forceinline__ float to_base(float s, float m) {
+    return !(fabsf(m) < kFar) ? s : s * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, kLog2eLow, __builtin_fmaf(-m, kLog2e, whole_above(m))));
+}
+
 // Statistics of two sets of ids.  (A sum that is NaN stays NaN beside any other; what lies infinitely far below counts nothing.)
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
     Stat r;
     r.m = fmaxf(a.m, b.m);
     r.s = a.s * (a.m == r.m ? 1.f : fexp_full(a.m - r.m)) + b.s * (b.m == r.m ? 1.f : fexp_full(b.m - r.m));
     r.idx = a.m > b.m || (a.m == b.m && a.idx < b.idx) ? a.idx : b.idx;
-    return r;
-}
-__device__ __forceinline__ Stat join_wave(Stat r) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) r = join(r, stat_shfl_xor(r, o));
     return r;
 }
 
@@ -67,115 +76,254 @@ __device__ __forceinline__ void put_stats(const RulesArgs& a, int row, const Sta
     a.stats[row] = o;
 }
 
-template <class R>
-__global__ __launch_bounds__(kThreads) void rules_kernel(const RulesArgs a) {
-    constexpr int E = 16 / R::kBytes;
-    typedef typename R::type V;
-    extern __shared__ unsigned table[];  // [range] where there are tokens or biases
-    __shared__ StatPart share[kThreads / 64];
-    __shared__ unsigned word;
-    __shared__ float at_target;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = blockIdx.y, v0 = (int)blockIdx.x * a.range, v1 = min(v0 + a.range, a.vocab);
-    const bool tabled = a.tokens || a.bias_ids;
-    Penalty pen = {1.f, 0.f, 0.f};
-    const float* bias = nullptr;
-    if (tabled) {
-        for (int i = tid; i < v1 - v0; i += kThreads) table[i] = 0u;
-        __syncthreads();
-        if (a.bias_ids) {
-            const int n = a.bias_counts ? min(max(a.bias_counts[row], 0), a.max_bias) : a.max_bias;
-            const int* ids = a.bias_ids + (int64_t)row * a.bias_stride;
-            bias = a.bias + (int64_t)row * a.bias_stride;
-            for (int i = tid; i < n; i += kThreads) {
-                const int v = ids[i];
-                if (v >= v0 && v < v1) atomicMax(&table[v - v0], (unsigned)(i + 1) << kBiasAt);
+// last_in (last_in.h) for workgroups whose one wave has stored their partial results.
+__device__ __forceinline__ bool last_wave_in(unsigned* counter, unsigned n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned before = 0;
+    if ((threadIdx.x & 63) == 0) {
+        before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == n - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    return __builtin_amdgcn_readfirstlane((int)before) == (int)n - 1;
+}
+
+// The first n of a row's tokens, dealt to the threads by fours, two of these requested at a time: request(0), then each(f) with f(i, token).
+struct Tokens {
+    typedef Piece<16, 4> Four;
+    static constexpr int U = 2;
+    const int* ids;
+    int n;
+    Four p[U];
+    __device__ __forceinline__ void request(int i0) {
+        const int full = n >> 2;
+        if (full == 0) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u) p[u] = *(const Four*)(ids + 4 * (int64_t)min(i0 + u * kThreads + (int)threadIdx.x, full - 1));
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F&& f) {
+        const int tid = threadIdx.x, full = n >> 2;
+        for (int i0 = 0; i0 < full; i0 += U * kThreads) {
+            if (i0) request(i0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kThreads + tid;
+                if (i < full) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f(4 * i + e, (int)p[u].w[e]);
+                }
             }
-            __syncthreads();
         }
+        if (tid < (n & 3)) f((full << 2) + tid, ids[(full << 2) + tid]);
+    }
+};
+
+// EACH ids a thread, in pieces of 16 bytes that lie a workgroup's width apart.
+template <class R, int EACH>
+__global__ __launch_bounds__(kThreads) void rules_kernel(const RulesArgs a) {
+    constexpr int E = 16 / R::kBytes, P = EACH / E, W = kThreads / 64;
+    typedef typename R::type V;
+    extern __shared__ __attribute__((aligned(16))) unsigned table[];  // [range], then the biases, where there are tokens or biases
+    __shared__ float tops[W], sums[W];
+    __shared__ int ids_at[W];
+    static_assert(W == 4, "joined by hand");
+    __shared__ float at_target;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nthr = kThreads;
+    const int row = blockIdx.y, v0 = (int)blockIdx.x * a.range, v1 = min(v0 + a.range, a.vocab), n = v1 - v0;
+    const bool tabled = a.tokens || a.bias_ids;
+    const int n_tokens = a.tokens ? min(max(a.lengths[row], 0), a.max_tokens) : 0, from = a.tokens && a.starts ? a.starts[row] : 0;
+    const int n_bias = !a.bias_ids ? 0 : a.bias_counts ? min(max(a.bias_counts[row], 0), a.max_bias) : a.max_bias;
+    const int target = a.targets ? a.targets[row] : -1, ti = target - v0;
+    const V* in = (const V*)a.logits + (int64_t)row * a.ld + v0;
+    V* out = a.out ? (V*)a.out + (int64_t)row * a.ldo + v0 : nullptr;
+    const uint32_t* mask = a.mask ? a.mask + (int64_t)row * a.mask_stride + (v0 >> 5) : nullptr;
+    float* bias = (float*)(table + a.range);
+
+    struct Slot {
+        RowVec<R, E> x;
+        uint32_t allowed;
+    };
+    Slot pieces[P];
+    const auto request = [&](Slot& q, int turn) {  // (past the end: ids that are there, for nobody)
+        const int i = (turn * nthr + tid) * E;
+        if (n >= E) q.x.load(in + min(i, n - E));
+        if (i < n && i + E > n) q.x.load_some(in + i, n - i);
+        q.allowed = ~0u;
+        if (mask) q.allowed = mask[min(i, n - 1) >> 5];  // (a range starts with a word of the mask, and no piece has ids of two words)
+    };
+    // (loads come back in order, and the logits, which need nothing, take longest: everything is requested before anything is waited for)
+#pragma unroll
+    for (int p = 0; p < P; ++p) request(pieces[p], p);
+    Penalty pen = {1.f, 0.f, 0.f};
+    if (tabled) {
+        const int* bias_ids = a.bias_ids + (int64_t)row * a.bias_stride;
+        const float* values = a.bias + (int64_t)row * a.bias_stride;
+        int b_id = -1;
+        float b_value = 0.f;
+        if (tid < n_bias) {
+            b_id = bias_ids[tid];
+            b_value = values[tid];
+        }
+        Tokens said = {a.tokens + (int64_t)row * a.tokens_stride, n_tokens, {}};
+        said.request(0);
         if (a.tokens) {
-            const int n = min(max(a.lengths[row], 0), a.max_tokens), from = a.starts ? a.starts[row] : 0;
-            const int* ids = a.tokens + (int64_t)row * a.tokens_stride;
-            for (int i = tid; i < n; i += kThreads) {
-                const int v = ids[i];
-                if (v < v0 || v >= v1) continue;
-                if (i >= from) atomicAdd(&table[v - v0], 1u);
-                else atomicOr(&table[v - v0], kSeen);
-            }
             const bild_penalties p = a.penalties[(int64_t)row * a.penalties_stride];
             pen = {p.repetition, p.frequency, p.presence};
-            __syncthreads();
         }
-    }
-    const V* in = (const V*)a.logits + (int64_t)row * a.ld;
-    V* out = a.out ? (V*)a.out + (int64_t)row * a.ldo : nullptr;
-    const uint32_t* mask = a.mask ? a.mask + (int64_t)row * a.mask_stride : nullptr;
-    const int target = a.targets ? a.targets[row] : -1;
-    float m = -INFINITY, s = 0.f;
-    int idx = 0x7FFFFFFF;
-    for (int v = v0 + tid * E; v < v1; v += kThreads * E) {
-        const int n = v1 - v;
-        RowVec<R, E> x;
-        if (n >= E) x.load(in + v); else x.load_some(in + v, n);
-        const uint32_t allowed = mask ? mask[v >> 5] >> (v & 31) : ~0u;  // (a range starts with a word, so do eight ids not cross one)
-        float z[E];
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            z[i] = R::up(x.v[i]);
-            if (tabled) z[i] = apply(z[i], i < n ? table[v + i - v0] : 0u, pen, bias);
-            if (!(allowed >> i & 1u) || i >= n) z[i] = -INFINITY;
-            if (i < n && v + i == target) at_target = z[i];
-            x.v[i] = R::down(z[i]);
-            if (z[i] > top) top = z[i];
-        }
-        if (out) {
-            if (n >= E) x.store(out + v); else x.store_some(out + v, n);
-        }
-        if (a.stats) {  // (equal maxima keep the lower id: ids come in increasing order)
-            if (top > m) {
-                s = s * fexp_full(m - top);
-                m = top;
-#pragma unroll
-                for (int i = E - 1; i >= 0; --i)
-                    if (z[i] == top) idx = v + i;
+        for (int i = tid * 4; i < a.range; i += kThreads * 4) *(uint4*)(table + i) = make_uint4(0, 0, 0, 0);
+        lds_barrier();
+        if (n_bias > 0) {
+            for (int i = tid; i < n_bias; i += kThreads) {
+                if (i != tid) {
+                    b_id = bias_ids[i];
+                    b_value = values[i];
+                }
+                const unsigned v = (unsigned)b_id - (unsigned)v0;
+                bias[i] = b_value;
+                if (v < (unsigned)n) atomicMax(&table[v], (unsigned)(i + 1) << kBiasAt);
             }
-            const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int i = 0; i < E; ++i) s += fexp_full(z[i] - base);
+            lds_barrier();
         }
+        said.each([&](int i, int t) {
+            const unsigned v = (unsigned)t - (unsigned)v0;
+            if (v >= (unsigned)n) return;
+            if (i >= from) atomicAdd(&table[v], 1u);
+            else atomicOr(&table[v], kSeen);
+        });
+        lds_barrier();
     }
+
+    float z[P][E];
+    float top = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int i = (p * kThreads + tid) * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[p][e] = R::up(pieces[p].x.v[e]);
+        if (tabled) {
+            uint32_t w[E], any = 0u;
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                const uint4 q = *(const uint4*)(table + min(i, a.range - E) + e);
+                w[e] = q.x; w[e + 1] = q.y; w[e + 2] = q.z; w[e + 3] = q.w;
+                any |= q.x | q.y | q.z | q.w;
+            }
+            if (i < n && any) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (w[e]) z[p][e] = apply(z[p][e], w[e], pen, bias);
+            }
+        }
+        uint32_t allowed = pieces[p].allowed >> (i & 31);
+        const bool edge = i + E > n;
+        if (edge) allowed &= i < n ? (1u << (n - i)) - 1u : 0u;
+        if (mask || edge) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const uint32_t keep = (uint32_t)((int)(allowed << (31 - e)) >> 31);
+                z[p][e] = __uint_as_float((__float_as_uint(z[p][e]) & keep) | (0xFF800000u & ~keep));
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = __builtin_amdgcn_fmed3f(top, z[p][e], INFINITY);
+    }
+    const auto put = [&] {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (p * kThreads + tid) * E;
+            RowVec<R, E> y;
+#pragma unroll
+            for (int e = 0; e < E; ++e) y.v[e] = R::down(z[p][e]);
+            if (i + E <= n) y.store(out + i); else y.store_some(out + i, n - i);
+        }
+    };
+    // (the wave that tells of the workgroup's arrival waits for its stores first: its own logits come behind that)
+    const bool tells = wave == 0 && a.parts > 1 && a.stats;
+    if (out && !tells) put();
     if (!a.stats) return;
-    Stat r = join_wave(Stat{m, s, idx});
-    if (lane == 0) share[wave] = StatPart{r.m, r.s, r.idx, 0};
-    __syncthreads();
-    r = Stat{share[0].m, share[0].s, share[0].idx};
-    for (int w = 1; w < kThreads / 64; ++w) r = join(r, Stat{share[w].m, share[w].s, share[w].idx});
+    const float mine = top;
+    top = wave_max(top);
+    if (lane == 0) tops[wave] = top;
+    // the target's logit is with one thread
+    if (ti >= 0 && ti < n && ti / E % kThreads == tid) {
+        float zt = 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if ((p * kThreads + tid) * E + e == ti) zt = z[p][e];
+        at_target = zt;
+    }
+    lds_barrier();
+    Stat r;
+    r.m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    float s = 0.f;
+    if (fabsf(r.m) < kFar || r.m == -INFINITY) {
+        const float whole = whole_above(r.m);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += term(z[p][e], whole);
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += fexp_full(z[p][e] - r.m);
+    }
+    s = wave_sum(s);
+    int idx = 0x7FFFFFFF;
+    if (top == r.m && r.m != -INFINITY) {  // (a wave that has the maximum)
+        if (mine == r.m) {
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                for (int e = E - 1; e >= 0; --e)
+                    if (z[p][e] == r.m) idx = v0 + (p * kThreads + tid) * E + e;
+        }
+        for (int o = 32; o > 0; o >>= 1) idx = min(idx, __shfl_xor(idx, o, 64));
+    }
+    if (lane == 0) {
+        sums[wave] = s;
+        ids_at[wave] = idx;
+    }
+    lds_barrier();
+    if (wave != 0) return;
+    r.s = to_base(sums[0] + sums[1] + sums[2] + sums[3], r.m);
+    r.idx = min(min(ids_at[0], ids_at[1]), min(ids_at[2], ids_at[3]));
     const bool has = target >= 0 && target < a.vocab;
     float zt = has ? at_target : NAN;  // (where the target is not this range's: not read)
     if (a.parts > 1) {
-        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
         const auto parts = make_rsrc(a.part + (size_t)row * a.parts, sizeof(StatPart) * (size_t)a.parts);
-        if (tid == 0)
+        if (lane == 0)
             __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(r.m), __float_as_uint(r.s), (unsigned)r.idx, __float_as_uint(zt)}, parts,
                                                    (int)blockIdx.x * 16, 0, kPartAux);
-        if (!last_in(a.arrived + row, (unsigned)a.parts, &word)) return;
-        if (wave != 0) return;
+        const bool last = last_wave_in(a.arrived + (size_t)row * kCountStride, (unsigned)a.parts);
+        if (out) put();
+        if (!last) return;
         r = stat_neutral();
         for (int p = lane; p < a.parts; p += 64) {
             const u32x4 q = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, p * 16, 0, kPartAux));
             r = join(r, Stat{__uint_as_float(q[0]), __uint_as_float(q[1]), (int)q[2]});
         }
-        r = join_wave(r);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) r = join(r, stat_shfl_xor(r, o));
         if (has) zt = __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b32(parts, target / a.range * 16 + 12, 0, kPartAux));
     }
-    if (tid == 0) put_stats(a, row, r, zt);
+    if (lane == 0) put_stats(a, row, r, zt);
 }
 
-// Workgroups of a row: about a thousand in all, none with more ids than its table holds or with less than one piece a thread.
+// Workgroups of a row: two thousand in all, none with more ids than its threads hold or with less than one piece a thread.  (Ranges of up to 4096 / 8192
+// ids, us: 512 x 50257 fp16 29.1 / 32.2, with 1000 tokens a row 40.4 / 46.2, 256 x 128000 bf16 with 1000 53.5 / 65.9; two thousand / one
+// thousand workgroups: 11 x 250112 fp32 with 700 tokens 12.6 / 13.6, 64 x 32000 bf16 with 8192 12.9 / 13.1.)
 int parts_of(int rows, int vocab) {
     const int least = (vocab + kMaxRange - 1) / kMaxRange, most = std::max(least, (vocab + 2047) / 2048);
-    return std::max(least, std::min(most, (1024 + rows - 1) / rows));
+    return std::max(least, std::min(most, (2048 + rows - 1) / rows));
+}
+template <class R>
+void launch(const RulesArgs& a, size_t lds, hipStream_t st) {
+    const dim3 grid(a.parts, a.rows), block(kThreads);
+    if (a.range <= kThreads * 8) hipLaunchKernelGGL((rules_kernel<R, 8>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((rules_kernel<R, 16>), grid, block, lds, st, a);
 }
 size_t parts_cap(int max_rows, int vocab) { return (size_t)max_rows * ((vocab + kMaxRange - 1) / kMaxRange) + 2048 + max_rows; }
 
@@ -191,14 +339,13 @@ struct bild_rules {
 namespace bild {
 
 hipError_t launch_rules(RulesArgs a, hipStream_t st) {
-    // whole words of the mask
-    a.range = ((a.vocab + a.parts - 1) / a.parts + 31) / 32 * 32;
+    a.parts = parts_of(a.rows, a.vocab);
+    a.range = ((a.vocab + a.parts - 1) / a.parts + 31) / 32 * 32;  // whole words of the mask
     a.parts = (a.vocab + a.range - 1) / a.range;
-    const size_t lds = a.tokens || a.bias_ids ? sizeof(unsigned) * (size_t)a.range : 0;
-    const dim3 grid(a.parts, a.rows), block(kThreads);
-    if (a.dtype == BILD_DT_F32) hipLaunchKernelGGL(rules_kernel<RowF32>, grid, block, lds, st, a);
-    else if (a.dtype == BILD_DT_BF16) hipLaunchKernelGGL(rules_kernel<RowBf16>, grid, block, lds, st, a);
-    else hipLaunchKernelGGL(rules_kernel<RowF16>, grid, block, lds, st, a);
+    const size_t lds = a.tokens || a.bias_ids ? sizeof(unsigned) * ((size_t)a.range + (a.bias_ids ? a.max_bias : 0)) : 0;
+    if (a.dtype == BILD_DT_F32) launch<RowF32>(a, lds, st);
+    else if (a.dtype == BILD_DT_BF16) launch<RowBf16>(a, lds, st);
+    else launch<RowF16>(a, lds, st);
     return hipGetLastError();
 }
 
@@ -210,7 +357,7 @@ extern "C" int bild_rules_create(int vocab, int max_rows, bild_rules** out) {
     if (!r) return BILD_ENOMEM;
     r->vocab = vocab;
     r->max_rows = max_rows;
-    const size_t counts = (sizeof(unsigned) * (size_t)max_rows + 255) / 256 * 256;
+    const size_t counts = (sizeof(unsigned) * kCountStride * (size_t)max_rows + 255) / 256 * 256;
     int rc = BILD_OK;
     if (hipGetDevice(&r->device) != hipSuccess) rc = BILD_EHIP;
     else if (hipMalloc(&r->mem, counts + sizeof(StatPart) * parts_cap(max_rows, vocab)) != hipSuccess) r->mem = nullptr, rc = BILD_ENOMEM;
@@ -268,7 +415,6 @@ extern "C" int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void
     a.max_bias = c.max_bias;
     a.part = r->part;
     a.arrived = r->arrived;
-    a.parts = parts_of(c.rows, r->vocab);
     const OnDevice on(r->device);
     if (!on.ok) return BILD_EHIP;
     return launch_rules(a, (hipStream_t)hip_stream) == hipSuccess ? BILD_OK : BILD_EHIP;
