@@ -33,6 +33,7 @@ struct RotaryArgs {
     int half, rot, d_head;
     int pair_units, units;  // pieces of a head: of its turned part, of all that is written
     int tokens_per, heads_per;
+    int again;              // values may be written twice
     unsigned units_m, slab_m;  // of units and units * heads_per (see divide)
     float sign;
     double magnitude;
@@ -42,78 +43,124 @@ struct RotaryArgs {
 // u / d by a product with m = 2^32 / d rounded up (0: d is 1); exact for u and d below 2^16, since u * (m * d - 2^32) < 2^32.
 __device__ __forceinline__ int divide(int u, unsigned m) { return m ? (int)__umulhi((unsigned)u, m) : u; }
 
+// Cosine and sine in 64 bits, good to some 2^-36 (the results are rounded to fp32): the quarter turn nearest to the angle is taken off in two
+// steps, each with one rounding, and what is left, at most pi / 4, goes into the Taylor series.  A third of the library's
+// instructions, in a chain that every workgroup waits for.
+__device__ __forceinline__ void turn_of(double angle, double& cs, double& sn) {
+    const double k = rint(angle * 0.63661977236758134308);  // 2 / pi
+    const double r = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489661923, angle)), q = r * r;
+    double s = fma(q, -2.50521083854417187751e-8, 2.75573192239858906526e-6);  // 1 / 11!, 1 / 9!
+    s = fma(q, s, -1.98412698412698412698e-4);
+    s = fma(q, s, 8.33333333333333333333e-3);
+    s = fma(q, s, -0.166666666666666666667);
+    s = fma(q * r, s, r);
+    double c = fma(q, 2.08767569878680989792e-9, -2.75573192239858906526e-7);  // 1 / 12!, 1 / 10!
+    c = fma(q, c, 2.48015873015873015873e-5);
+    c = fma(q, c, -1.38888888888888888889e-3);
+    c = fma(q, c, 4.16666666666666666667e-2);
+    c = fma(q, c, -0.5);
+    c = fma(q, c, 1.0);
+    const int quarter = (int)(long long)k;
+    const double x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+    cs = (quarter + 1) & 2 ? -x : x;
+    sn = quarter & 2 ? -y : y;
+}
+
+// A piece of a head are two times 16 bytes: of first and of second halves, of pairs side by side, or of what lies behind the turned part.
 template <class R, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
     constexpr int E = 16 / R::kBytes;
     typedef typename R::type V;
+    typedef RowVec<R, E> Vec;
     __shared__ float2 turn[kMaxTokens * kMaxHalf];
     const int t0 = (int)blockIdx.x * a.tokens_per, nt = min(a.tokens_per, a.tokens - t0);
     const int h0 = (int)blockIdx.y * a.heads_per, nh = min(a.heads_per, a.heads - h0);
+    const int slab = a.units * a.heads_per, count = nt * slab;
+    struct Unit {
+        Vec x, y;
+        V* dst;
+        int p;  // which of the head's
+        int t;  // token; -1: nothing
+    };
+    // Where the two vectors of a piece begin and how many values they have (of neighbouring lanes either lie side by side).  The last vector of a part whose
+    // length is no multiple of one begins earlier, and what it shares with its neighbour is written twice, the same both times; in place it is cut short.
+    struct Place {
+        int x, y, nx, ny;
+    };
+    const auto place = [&](int p) {
+        int base = 0, len = a.rot, x = p * E, y = (p + a.pair_units) * E;
+        if (p >= a.pair_units) {
+            base = a.rot;
+            len = a.d_head - a.rot;
+            x -= a.pair_units * E;
+            y = x + (a.units - a.pair_units) * E;
+        } else if (HALVES) {
+            len = a.half;
+            y = x;
+        }
+        if (a.again && len >= E) {
+            x = min(x, len - E);
+            y = min(y, len - E);
+        }
+        return Place{base + x, base + y + (HALVES && base == 0 ? a.half : 0), len - x, len - y};
+    };
+    const auto request = [&](Unit& q, int u) {
+        const int t = divide(u, a.slab_m), r = u - t * slab, hh = divide(r, a.units_m);
+        q.t = -1;
+        if (u >= count || hh >= nh) return;
+        q.p = r - hh * a.units;
+        q.t = t;
+        const int head = h0 + hh, which = head >= a.heads_q, h = which ? head - a.heads_q : head;
+        const V* src = (const V*)a.src[which] + (int64_t)(t0 + t) * a.src_token[which] + (int64_t)h * a.src_head[which];
+        q.dst = (V*)a.dst[which] + (int64_t)(t0 + t) * a.dst_token[which] + (int64_t)h * a.dst_head[which];
+        const Place at = place(q.p);
+        if (at.ny >= E) {
+            q.x.load(src + at.x);
+            q.y.load(src + at.y);
+        } else {
+            q.x.load_some(src + at.x, at.nx);
+            q.y.load_some(src + at.y, at.ny);
+        }
+    };
+    const auto finish = [&](Unit& q) {
+        if (q.t < 0) return;
+        const Place at = place(q.p);
+        if (q.p < a.pair_units) {
+            const float2* tn = turn + q.t * a.half;
+            const auto pair = [&](typename R::type& u, typename R::type& v, int i) {
+                const float2 c = tn[min(i, a.half - 1)];
+                const float fu = R::up(u), fv = R::up(v);
+                u = R::down(fu * c.x - fv * c.y);
+                v = R::down(fu * c.y + fv * c.x);
+            };
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (HALVES) pair(q.x.v[i], q.y.v[i], at.x + i);
+                else if (i < E / 2) pair(q.x.v[2 * i], q.x.v[2 * i + 1], at.x / 2 + i);
+                else pair(q.y.v[2 * i - E], q.y.v[2 * i - E + 1], at.y / 2 + i - E / 2);
+            }
+        }
+        if (at.ny >= E) {
+            q.x.store(q.dst + at.x);
+            q.y.store(q.dst + at.y);
+        } else {
+            q.x.store_some(q.dst + at.x, at.nx);
+            q.y.store_some(q.dst + at.y, at.ny);
+        }
+    };
+    Unit unit;
+    request(unit, (int)threadIdx.x);
+    __builtin_amdgcn_sched_barrier(0);
+    // the rows are on their way meanwhile
     for (int e = threadIdx.x; e < nt * a.half; e += kThreads) {
         const int t = e / a.half, i = e - t * a.half;
         const int pos = a.positions ? a.positions[t0 + t] : a.first + t0 + t;
         double sn, cs;
-        sincos((double)pos * a.frequency[i], &sn, &cs);
+        turn_of((double)pos * a.frequency[i], cs, sn);
         turn[e] = make_float2((float)(cs * a.magnitude), (float)(sn * a.magnitude) * a.sign);
     }
-    __syncthreads();
-    const int slab = a.units * a.heads_per;
-    for (int u = threadIdx.x; u < nt * slab; u += kThreads) {
-        const int t = divide(u, a.slab_m), r = u - t * slab;
-        const int hh = divide(r, a.units_m), p = r - hh * a.units;
-        if (hh >= nh) continue;
-        const int head = h0 + hh, which = head >= a.heads_q, h = which ? head - a.heads_q : head;
-        const V* src = (const V*)a.src[which] + (int64_t)(t0 + t) * a.src_token[which] + (int64_t)h * a.src_head[which];
-        V* dst = (V*)a.dst[which] + (int64_t)(t0 + t) * a.dst_token[which] + (int64_t)h * a.dst_head[which];
-        const float2* tn = turn + t * a.half;
-        if (p >= a.pair_units) {  // behind the turned part
-            const int at = a.rot + (p - a.pair_units) * E, n = a.d_head - at;
-            RowVec<R, E> v;
-            if (n >= E) {
-                v.load(src + at);
-                v.store(dst + at);
-            } else {
-                v.load_some(src + at, n);
-                v.store_some(dst + at, n);
-            }
-        } else if (HALVES) {
-            const int at = p * E, n = a.half - at;
-            RowVec<R, E> x, y;
-            if (n >= E) {
-                x.load(src + at);
-                y.load(src + a.half + at);
-            } else {
-                x.load_some(src + at, n);
-                y.load_some(src + a.half + at, n);
-            }
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float2 c = tn[min(at + i, a.half - 1)];
-                const float fx = R::up(x.v[i]), fy = R::up(y.v[i]);
-                x.v[i] = R::down(fx * c.x - fy * c.y);
-                y.v[i] = R::down(fx * c.y + fy * c.x);
-            }
-            if (n >= E) {
-                x.store(dst + at);
-                y.store(dst + a.half + at);
-            } else {
-                x.store_some(dst + at, n);
-                y.store_some(dst + a.half + at, n);
-            }
-        } else {
-            const int at = p * E, n = a.rot - at;
-            RowVec<R, E> x;
-            if (n >= E) x.load(src + at); else x.load_some(src + at, n);
-#pragma unroll
-            for (int i = 0; i < E; i += 2) {
-                const float2 c = tn[min((at + i) / 2, a.half - 1)];
-                const float fx = R::up(x.v[i]), fy = R::up(x.v[i + 1]);
-                x.v[i] = R::down(fx * c.x - fy * c.y);
-                x.v[i + 1] = R::down(fx * c.y + fy * c.x);
-            }
-            if (n >= E) x.store(dst + at); else x.store_some(dst + at, n);
-        }
-    }
+    lds_barrier();
+    finish(unit);
 }
 
 __global__ __launch_bounds__(64) void rotary_table_kernel(double2* table, int pairs, const bild_rotary r) {
@@ -227,7 +274,7 @@ extern "C" int bild_rotary_apply(const bild_rotary* r, const bild_rotary_call* c
     RotaryArgs a;
     std::memset((void*)&a, 0, sizeof(a));
     const bild_rotary_rows* rows[2] = {&c.q, &c.k};
-    bool in_place = true;
+    bool in_place = true, any_in_place = false;
     for (int i = 0; i < 2; ++i) {
         const bild_rotary_rows& x = *rows[i];
         a.src[i] = x.src;
@@ -237,6 +284,8 @@ extern "C" int bild_rotary_apply(const bild_rotary* r, const bild_rotary_call* c
         a.dst_token[i] = x.dst_token;
         a.dst_head[i] = x.dst_head;
         in_place = in_place && (x.heads == 0 || (x.src == x.dst && x.src_token == x.dst_token && x.src_head == x.dst_head));
+        any_in_place = any_in_place || (x.heads > 0 && x.src == x.dst);
+        if (x.heads > 0 && x.src == x.dst && ((c.tokens > 1 && x.src_token != x.dst_token) || (x.heads > 1 && x.src_head != x.dst_head))) return BILD_EINVAL;
     }
     a.positions = c.positions;
     a.first = c.first;
@@ -248,12 +297,13 @@ extern "C" int bild_rotary_apply(const bild_rotary* r, const bild_rotary_call* c
     a.d_head = c.d_head;
     const int e = 16 / row_bytes(c.dtype);
     const bool halves = r->cfg.layout == BILD_ROTARY_HALVES;
-    a.pair_units = ((halves ? a.half : rot) + e - 1) / e;
-    a.units = a.pair_units + (in_place ? 0 : (c.d_head - rot + e - 1) / e);  // (in place the rest is there already)
-    a.heads_per = std::min((int)heads, std::max(1, 2048 / a.units));
-    a.tokens_per = std::min({c.tokens, kMaxTokens, std::max(1, 2048 / (a.units * a.heads_per))});
-    if (c.tokens / a.tokens_per > 0x7FFFFFFE) return BILD_EINVAL;
-    const auto magic = [](int d) { return d == 1 ? 0u : (unsigned)((0xFFFFFFFFull + d) / d); };  // (at most 2048 and a head's 258 pieces: see divide)
+    a.pair_units = (rot + 2 * e - 1) / (2 * e);
+    a.units = a.pair_units + (in_place ? 0 : (c.d_head - rot + 2 * e - 1) / (2 * e));  // (in place the rest is there already)
+    // a piece a thread (two of them: 26.2 against 25.4 us for 134 MB in halves, 3.5 against 2.8 for eleven tokens)
+    a.again = !any_in_place;
+    a.heads_per = std::min((int)heads, std::max(1, kThreads / a.units));
+    a.tokens_per = std::min({c.tokens, kMaxTokens, std::max(1, kThreads / (a.units * a.heads_per))});
+    const auto magic = [](int d) { return d == 1 ? 0u : (unsigned)((0xFFFFFFFFull + d) / d); };  // (at most a workgroup's 256 pieces and a head's 130: see divide)
     a.units_m = magic(a.units);
     a.slab_m = magic(a.units * a.heads_per);
     a.sign = c.inverse ? -1.f : 1.f;

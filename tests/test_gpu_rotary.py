@@ -167,7 +167,8 @@ def test_refusals():
     good = dict(d_head=64, dtype=F32, tokens=2, q=pkg.RotaryRows(src.ptr, src.ptr, 2, 128, 64, 128, 64))
     r.apply(**good)
     for kw in (dict(tokens=0), dict(d_head=62), dict(d_head=1025), dict(dtype=3), dict(q=pkg.RotaryRows()), dict(q=pkg.RotaryRows(None, src.ptr, 1)),
-               dict(q=pkg.RotaryRows(src.ptr, None, 1)), dict(q=pkg.RotaryRows(src.ptr, src.ptr, -1)), dict(first=2 ** 31 - 2, tokens=3)):
+               dict(q=pkg.RotaryRows(src.ptr, None, 1)), dict(q=pkg.RotaryRows(src.ptr, src.ptr, -1)), dict(first=2 ** 31 - 2, tokens=3),
+               dict(q=pkg.RotaryRows(src.ptr, src.ptr, 2, 128, 64, 129, 64)), dict(q=pkg.RotaryRows(src.ptr, src.ptr, 2, 128, 64, 128, 32))):
         with pytest.raises(pkg.BildError) as e:
             r.apply(**{**good, **kw})
         assert e.value.code == b.EINVAL
