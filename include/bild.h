@@ -430,6 +430,22 @@ int bild_rules_create(int vocab, int max_rows, bild_rules** out);
 int bild_rules_destroy(bild_rules* r);
 int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_stream);
 
+/* ---- the operators inside a state's passes ----
+ * The LM head of model `which` (1 small, 2 large) of this state's passes becomes `head` (n = vocab, k = d_model, else BILD_EINVAL), behind the model's final
+ * norm and times its logit scale; NULL: the model's own again.  Everything that is read off the logits (policies, draws, acceptance) follows.  The matrix is
+ * borrowed and has to outlive the state or the next call.  The passes then keep their logits in device memory (32 x vocabulary floats a model). */
+int bild_set_quant_head(bild_state* s, int which, const bild_quant* head /* nullable */);
+/* Penalties (NULL: none) and biases (n 0: none; id i gets bias[i], the last entry of an id counts; finite, at most 1023, ids in the vocabulary) for every token that
+ * either model of the state proposes from now on, as bild_rules_apply has them: the row's tokens are the sequence up to the row, drafts
+ * included; frequency and presence count from the first generated token on.  repetition > 0.  HOST memory, copied.  Both none: back to unchanged logits (masks stay).
+ * bild_small_step's max_prob, the fallback and rollback tests, draws and bild_debug_logits are those of the changed logits.  BILD_ECAP for penalties where
+ * max_len is above 1048575. */
+int bild_set_rules(bild_state* s, const bild_penalties* penalties /* nullable */, const int32_t* bias_ids, const float* bias, int n_bias);
+/* Masks for the tokens at positions first .. first + n - 1 of the sequence (0 <= first, first + n <= max_len): bit id % 32 of word id / 32 of a row of ceil(vocab / 32) words
+ * says whether the id may stand there.  masks [n][words]: HOST memory, copied; NULL: all ids may.  They hold until changed, also for later requests.  BILD_EINVAL for
+ * a row that allows no id.  The first call allocates (max_len + 1) rows of device memory. */
+int bild_set_masks(bild_state* s, int first, int n, const uint32_t* masks);
+
 /* Introspection (host copies of the control block). */
 int bild_get_lengths(bild_state* s, int32_t* y_len, int32_t* draft_start, int32_t* len_small, int32_t* len_large);
 int bild_get_sequence(bild_state* s, int32_t* out, int cap, int32_t* n);

@@ -115,6 +115,9 @@ _SIGS = {
                                     C.POINTER(C.c_int32), C.c_void_p]),
     "bild_set_sampling": (C.c_int, [C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_int]),
     "bild_set_acceptance": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int]),
+    "bild_set_quant_head": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p]),
+    "bild_set_rules": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
+    "bild_set_masks": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_void_p]),
     "bild_kv_truncate": (C.c_int, [C.c_void_p, C.c_int, C.c_int]),
     "bild_seq_truncate": (C.c_int, [C.c_void_p, C.c_int]),
     "bild_force_tokens": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int]),
@@ -423,6 +426,24 @@ class State:
             return
         a = np.ascontiguousarray(u_accept, dtype=np.float32)
         _check(lib().bild_set_acceptance(self.h, int(rule), a.ctypes.data, len(a)), "bild_set_acceptance")
+
+    def set_quant_head(self, which: int, head: Optional["Quant"]):
+        """A 4-bit matrix in place of the LM head of model `which` (None: the model's own)."""
+        _check(lib().bild_set_quant_head(self.h, which, head.h if head is not None else None), "bild_set_quant_head")
+        self._heads = {**getattr(self, "_heads", {}), which: head}   # (borrowed by the state)
+
+    def set_rules(self, penalties=None, bias=None):
+        """penalties: (repetition, frequency, presence) or None; bias: {id: value} or None."""
+        p = np.asarray(penalties, dtype=np.float32) if penalties is not None else None
+        bias = bias or {}
+        ids, values = _i32(list(bias.keys())), np.asarray(list(bias.values()), dtype=np.float32)
+        _check(lib().bild_set_rules(self.h, p.ctypes.data if p is not None else None, ids.ctypes.data if len(ids) else None,
+                                    values.ctypes.data if len(ids) else None, len(ids)), "bild_set_rules")
+
+    def set_masks(self, first: int, masks=None, n: int = 0):
+        """masks [n][ceil(vocab / 32)] uint32 for the tokens at positions first .. first + n - 1; None: all ids at n positions."""
+        a = np.ascontiguousarray(masks, dtype=np.uint32) if masks is not None else None
+        _check(lib().bild_set_masks(self.h, first, len(a) if a is not None else n, a.ctypes.data if a is not None else None), "bild_set_masks")
 
     def force_tokens(self, first: int, tokens, draft_start: int):
         a = _i32(tokens)

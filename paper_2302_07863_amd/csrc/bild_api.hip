@@ -1473,6 +1473,8 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
     float* xfin = M.x;  // the residual stream after the last layer ...
     int thin_parts = 0;  // > 0: the final hidden state lies in M.xb as tile planes (times the final norm's gain)
     bool parts = false; // ... to which the partial results in M.px are still to be added (split FFN output projection)
+    const bild_quant* quant = s->gemm_only || lm_rows == 0 ? nullptr : s->quant_head[w];  // the LM head
+    const bool ruled = !s->gemm_only && lm_rows > 0 && s->ruled();
     if (one) {
         const int trunk = s->pair->trunk_layers, layer0 = w == 1 ? trunk : 0;
         PassArgs p;
@@ -1508,7 +1510,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         p.two = two_tiles(s, w, T);
         p.rope = M.rope;
         PassHead in;
-        const bool inside = die && T == 1 && lm_rows == 1 && mode != 3 && !s->debug_logits && s->top_p == 0.f;  // (pass_head.h)
+        const bool inside = die && T == 1 && lm_rows == 1 && mode != 3 && !s->debug_logits && s->top_p == 0.f && !quant && !ruled;  // (pass_head.h)
         if (inside) {
             std::memset((void*)&in, 0, sizeof(in));
             in.w = m->head.w;
@@ -1535,7 +1537,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         // Rows wider than the sweep of the vocabulary takes, from five on: as tile planes for the thin GEMM.  (The entry points, whose call is the head alone, ask
         // for 16 MB of matrix with five to eight rows, see head_route; a review of eight rows of two layers with that line / with none, us:
         // 2560 wide, 700, 1500, 2500 ids 131.3, 131.6, 132.1 / 130.1, 130.2, 131.4, 4096 wide 201.0, 200.7, 202.7 / 200.1, 199.0, 200.9.)
-        if (lm_rows > 4 && d > 2048 && dt == BILD_DT_BF16) {
+        if (lm_rows > 4 && d > 2048 && dt == BILD_DT_BF16 && !quant) {
             RowCopyArgs r;
             std::memset((void*)&r, 0, sizeof(r));
             r.src = M.x;
@@ -1554,7 +1556,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         if (rc) return rc;
     } else {
         // a single-row pass whose LM head is the one-row kernel with one feature tile per wave can add them itself
-        const bool head_reads_parts = T == 1 && lm_rows == 1 && s->pair->trunk_layers == 0 && m->head.tn < 8192;
+        const bool head_reads_parts = T == 1 && lm_rows == 1 && s->pair->trunk_layers == 0 && m->head.tn < 8192 && !quant;
         int rc = emit_layers(s, w, T, key_hint, lm_rows > 0, head_reads_parts, &xb_parts, &xfin, &parts);
         if (rc) return rc;
     }
@@ -1570,7 +1572,23 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         f.sync = s->pass_sync;
         f.turn = pass_turn(s, w, T);
     }
-    if (lm_rows > 0 && thin_parts > 0) {
+    // A head in 4 bits and rules take kernels of their own, whose logits go through memory.  us per pass of two layers, 1, 4, 11 rows, the model's own head (bf16) /
+    // with rules / in 4 bits, groups of 64 / both: 512 wide, 32 128 ids 46.6, 57.6, 64.5 / 51.9, 63.3, 70.2 / 45.1, 55.1, 64.4 / 46.6, 56.3, 65.8; 1024 wide, 250 112
+    // 135, 149, 159 / 139, 159, 177 / 75.8, 87.3, 136 / 75.2, 89.7, 139; 4096 wide, 32 000 219, 223, 229 / 223, 230, 243 / 186, 192, 222 / 193, 198, 228.
+    if (quant) {
+        bild_quant_call q;
+        std::memset((void*)&q, 0, sizeof(q));
+        q.x = xfin + (size_t)(T - lm_rows) * d;
+        q.x_stride = d;
+        q.y = M.dbg;
+        q.y_stride = c.vocab;
+        q.gain = m->dec_final;
+        q.rows = lm_rows;
+        q.eps = c.norm_eps;
+        q.scale = c.logit_scale;
+        s->stage_count += 1;
+        if (const int rc = launch_quant(quant, q, s->stream)) return rc;
+    } else if (lm_rows > 0 && thin_parts > 0) {
         ThinArgs g = thin_base(s, w, T, m->head, M.xb, thin_parts);
         g.epi = EPI_LMHEAD;
         g.first = T - lm_rows;
@@ -1581,7 +1599,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         g.part = M.part;
         g.part_ld = M.nparts_cap;
         g.zt = M.zt;
-        g.dbg = (s->debug_logits || s->top_p > 0.f) ? M.dbg : nullptr;
+        g.dbg = (s->debug_logits || s->top_p > 0.f || ruled) ? M.dbg : nullptr;
         f.nparts = thin_shape(g.W, g.epi, g.act, T).groups;
         if (f.nparts > M.nparts_cap) return BILD_ECAP;
         const int rc = run_thin(s, m, g);
@@ -1604,7 +1622,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         h.part = M.part;
         h.part_ld = M.nparts_cap;
         h.zt = M.zt;
-        h.dbg = (s->debug_logits || s->top_p > 0.f) ? M.dbg : nullptr;  // the draw of the sampling variant reads the logits
+        h.dbg = (s->debug_logits || s->top_p > 0.f || ruled) ? M.dbg : nullptr;  // the draw of the sampling variant reads the logits
         if (groups > M.nparts_cap) return BILD_ECAP;
         const int rc = launch_profiled(s, m, h.W, EPI_LMHEAD, [&] { return launch_head(h, s->stream); });
         if (rc) return rc;
@@ -1621,7 +1639,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         g.part = M.part;
         g.part_ld = M.nparts_cap;
         g.zt = M.zt;
-        g.dbg = (s->debug_logits || s->top_p > 0.f) ? M.dbg : nullptr;  // the draw of the sampling variant reads the logits
+        g.dbg = (s->debug_logits || s->top_p > 0.f || ruled) ? M.dbg : nullptr;  // the draw of the sampling variant reads the logits
         g.row_off = 0;
         if (xb_parts > 0) {
             g.xb_hi = M.xb + (size_t)(T - lm_rows) * d;
@@ -1636,6 +1654,39 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
             if (rc) return rc;
         }
         f.nparts = (int)gemm_num_blocks(g);
+    }
+    if (quant || ruled) {  // (without rules: the statistics of the logits as they are)
+        RulesArgs r;
+        std::memset((void*)&r, 0, sizeof(r));
+        r.logits = M.dbg;
+        r.out = ruled ? M.dbg : nullptr;
+        r.ld = r.ldo = c.vocab;
+        r.rows = lm_rows;
+        r.vocab = c.vocab;
+        r.dtype = BILD_DT_F32;
+        r.y = s->y;
+        r.len_ptr = len_ptr;
+        r.len_add = T - lm_rows;
+        r.ylen_ptr = &s->ctl->y_len;
+        if (s->has_penalties) {
+            r.tokens = s->y;
+            r.max_tokens = s->max_len;
+            r.penalties = s->penalties;
+            r.start_ptr = s->pair->decoder_only ? &s->ctl->n_src : nullptr;
+        }
+        if (s->n_bias > 0) {
+            r.bias_ids = s->bias_ids;
+            r.bias = s->bias;
+            r.max_bias = s->n_bias;
+        }
+        r.mask = s->masks;
+        r.mask_stride = (c.vocab + 31) / 32;
+        r.part = M.part;
+        r.part_ld = M.nparts_cap;
+        r.zt = M.zt;
+        s->stage_count += 1;
+        HIPC(launch_rules(r, s->stream, &f.nparts));
+        if (f.nparts > M.nparts_cap) return BILD_ECAP;  // (a range has 2048 ids at least, a part of the head 16)
     }
     if (lm_rows > 0) {
         f.part = M.part;
@@ -2303,6 +2354,72 @@ extern "C" int bild_set_acceptance(bild_state* s, int rule, const float* u_accep
     HIPC(hipMemcpy(s->u_acc, u_accept, sizeof(float) * (size_t)s->max_len, hipMemcpyHostToDevice));
     if (s->accept_mode != 1) drop_graphs(s);
     s->accept_mode = 1;
+    return BILD_OK;
+}
+
+extern "C" int bild_set_quant_head(bild_state* s, int which, const bild_quant* head) {
+    if (!s || which < 1 || which > 2) return BILD_EINVAL;
+    const bild_model_config& c = s->ms[which - 1].m->cfg;
+    if (head && (head->n != c.vocab || head->k != c.d_model || head->device != s->device)) return BILD_EINVAL;
+    if (head)
+        if (const int rc = alloc_logit_buffers(s)) return rc;
+    drop_graphs(s);
+    s->quant_head[which - 1] = head;
+    return BILD_OK;
+}
+
+extern "C" int bild_set_rules(bild_state* s, const bild_penalties* penalties, const int32_t* bias_ids, const float* bias, int n_bias) {
+    if (!s || n_bias < 0 || n_bias > kMaxBiases || (n_bias > 0 && (!bias_ids || !bias))) return BILD_EINVAL;
+    if (penalties && (!(penalties->repetition > 0.f) || !std::isfinite(penalties->repetition) || !std::isfinite(penalties->frequency) || !std::isfinite(penalties->presence)))
+        return BILD_EINVAL;
+    for (int i = 0; i < n_bias; ++i)
+        if (bias_ids[i] < 0 || bias_ids[i] >= s->ms[1].m->cfg.vocab || !std::isfinite(bias[i])) return BILD_EINVAL;
+    if (penalties && s->max_len > kMaxRuleTokens) return BILD_ECAP;
+    if (penalties || n_bias > 0) {
+        int rc = alloc_logit_buffers(s);
+        if (rc == BILD_OK && !s->penalties) rc = dev_alloc(s->allocs, (void**)&s->penalties, sizeof(bild_penalties));
+        if (rc == BILD_OK && !s->bias_ids) rc = dev_alloc(s->allocs, (void**)&s->bias_ids, sizeof(int) * kMaxBiases);
+        if (rc == BILD_OK && !s->bias) rc = dev_alloc(s->allocs, (void**)&s->bias, sizeof(float) * kMaxBiases);
+        if (rc) return rc;
+    }
+    drop_graphs(s);
+    if (penalties) HIPC(hipMemcpy(s->penalties, penalties, sizeof(*penalties), hipMemcpyHostToDevice));
+    if (n_bias > 0) {
+        HIPC(hipMemcpy(s->bias_ids, bias_ids, sizeof(int) * (size_t)n_bias, hipMemcpyHostToDevice));
+        HIPC(hipMemcpy(s->bias, bias, sizeof(float) * (size_t)n_bias, hipMemcpyHostToDevice));
+    }
+    s->has_penalties = penalties != nullptr;
+    s->n_bias = n_bias;
+    return BILD_OK;
+}
+
+extern "C" int bild_set_masks(bild_state* s, int first, int n, const uint32_t* masks) {
+    if (!s || first < 0 || n < 1 || n > s->max_len - first) return BILD_EINVAL;
+    const int vocab = s->ms[1].m->cfg.vocab;
+    const size_t words = (size_t)(vocab + 31) / 32;
+    if (masks)
+        for (int r = 0; r < n; ++r) {
+            const uint32_t* row = masks + (size_t)r * words;
+            uint32_t any = 0;
+            for (size_t i = 0; i < words; ++i) any |= i + 1 < words || vocab % 32 == 0 ? row[i] : row[i] & ((1u << vocab % 32) - 1u);
+            if (!any) return BILD_EINVAL;
+        }
+    if (!masks && !s->masks) return BILD_OK;
+    if (!s->masks) {
+        uint32_t* at = nullptr;
+        int rc = alloc_logit_buffers(s);
+        if (rc == BILD_OK) rc = dev_alloc(s->allocs, (void**)&at, sizeof(uint32_t) * words * (size_t)(s->max_len + 1));
+        if (rc) return rc;
+        HIPC(hipMemset(at, 0xFF, sizeof(uint32_t) * words * (size_t)(s->max_len + 1)));
+        drop_graphs(s);
+        s->masks = at;
+    }
+    HIPC(hipStreamSynchronize(s->stream));
+    if (masks) HIPC(hipMemcpy(s->masks + (size_t)first * words, masks, sizeof(uint32_t) * words * (size_t)n, hipMemcpyHostToDevice));
+    else {
+        HIPC(hipMemset(s->masks + (size_t)first * words, 0xFF, sizeof(uint32_t) * words * (size_t)n));
+        HIPC(hipStreamSynchronize(nullptr));
+    }
     return BILD_OK;
 }
 

@@ -286,6 +286,15 @@ struct bild_state {
     float* u_acc = nullptr;    // uniform number per sequence position for that rule
     float* s_ring = nullptr;   // [kMaxRows][vocab] the small model's logits of the pending drafts
     float4* s_draw = nullptr;  // [max_len + 1] (max, threshold key, nucleus mass) of the small model's row per position
+    const bild_quant* quant_head[2] = {nullptr, nullptr};  // 4-bit matrices in place of the models' LM heads
+    // rules on the logits of the state's passes (device memory; allocated where first asked for)
+    bild_penalties* penalties = nullptr;
+    int* bias_ids = nullptr;       // [kMaxBiases]
+    float* bias = nullptr;
+    uint32_t* masks = nullptr;     // [max_len + 1][words of a vocabulary]
+    bool has_penalties = false;
+    int n_bias = 0;
+    bool ruled() const { return has_penalties || n_bias > 0 || masks != nullptr; }
     float* trunk_x = nullptr;  // early-exit pair: [cap_len][d] hidden state after the trunk's last layer, by position
     int* y = nullptr;     // device [max_len + 1]
     int* src = nullptr;   // device [max_src]

@@ -22,6 +22,8 @@ struct bild_rotary {
 
 namespace bild {
 
+constexpr int kMaxRuleTokens = (1 << 20) - 1, kMaxBiases = 1023;  // of a row (see rules.hip)
+
 // Runs what follows on `device` and puts the caller's current device back.
 class OnDevice {
     int was = -1;
@@ -72,8 +74,16 @@ struct RulesArgs {
     int rows, vocab, dtype, max_tokens, max_bias;
     int parts, range;   // workgroups of a row, ids of each
     StatPart* part;     // [row][parts]
+    // Rows of a decoder pass: row r stands at position *len_ptr + len_add + r of the sequence `tokens` (penalties: what stands up to there; those of
+    // generated tokens from *start_ptr on, null: from 1), its logits are for the next position: the mask of that position, as target the token there if
+    // there is one.  The ranges' statistics and the target's logit are left for the policy kernel.
+    const int *len_ptr, *start_ptr, *ylen_ptr;
+    int len_add, part_ld;
+    const int* y;
+    float* zt;
     unsigned* arrived;  // a line per row, zero between launches
 };
-hipError_t launch_rules(RulesArgs a, hipStream_t st);
+// *parts (nullable): partial statistics a row.
+hipError_t launch_rules(RulesArgs a, hipStream_t st, int* parts = nullptr);
 
 }  // namespace bild

@@ -22,7 +22,7 @@ namespace {
 // A word of the table: how often the id occurs from `starts` on, whether it occurs at all, which of the biases is its last.
 constexpr unsigned kCountBits = 20, kSeen = 1u << kCountBits, kBiasAt = kCountBits + 1;
 constexpr unsigned kCountMask = kSeen - 1;
-constexpr int kMaxTokens = (1 << kCountBits) - 1, kMaxBias = (1 << (32 - kBiasAt)) / 2 - 1;  // (1023)
+static_assert(kMaxRuleTokens <= (int)kCountMask && kMaxBiases < 1 << (32 - kBiasAt), "a word holds them");
 constexpr int kThreads = 256;
 constexpr int kMaxRange = kThreads * 16;  // ids of a workgroup, 16 a thread: 16 KiB of table
 constexpr int kCountStride = 32;          // words between two rows' counts of arrivals: a line each (side by side, a thousand arrivals took 20 us)
@@ -131,12 +131,15 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RulesArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nthr = kThreads;
     const int row = blockIdx.y, v0 = (int)blockIdx.x * a.range, v1 = min(v0 + a.range, a.vocab), n = v1 - v0;
     const bool tabled = a.tokens || a.bias_ids;
-    const int n_tokens = a.tokens ? min(max(a.lengths[row], 0), a.max_tokens) : 0, from = a.tokens && a.starts ? a.starts[row] : 0;
+    const bool pass = a.len_ptr != nullptr;
+    const int next = pass ? *a.len_ptr + a.len_add + row + 1 : 0;  // position of a pass's logits
+    const int n_tokens = !a.tokens ? 0 : pass ? min(next, a.max_tokens) : min(max(a.lengths[row], 0), a.max_tokens);
+    const int from = !a.tokens ? 0 : pass ? (a.start_ptr ? *a.start_ptr : 1) : a.starts ? a.starts[row] : 0;
     const int n_bias = !a.bias_ids ? 0 : a.bias_counts ? min(max(a.bias_counts[row], 0), a.max_bias) : a.max_bias;
-    const int target = a.targets ? a.targets[row] : -1, ti = target - v0;
+    const int target = pass ? (next < *a.ylen_ptr ? a.y[next] : -1) : a.targets ? a.targets[row] : -1, ti = target - v0;
     const V* in = (const V*)a.logits + (int64_t)row * a.ld + v0;
     V* out = a.out ? (V*)a.out + (int64_t)row * a.ldo + v0 : nullptr;
-    const uint32_t* mask = a.mask ? a.mask + (int64_t)row * a.mask_stride + (v0 >> 5) : nullptr;
+    const uint32_t* mask = a.mask ? a.mask + (int64_t)(pass ? next : row) * a.mask_stride + (v0 >> 5) : nullptr;
     float* bias = (float*)(table + a.range);
 
     struct Slot {
@@ -240,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RulesArgs a) {
     // (the wave that tells of the workgroup's arrival waits for its stores first: its own logits come behind that)
     const bool tells = wave == 0 && a.parts > 1 && a.stats;
     if (out && !tells) put();
-    if (!a.stats) return;
+    if (!a.stats && !pass) return;
     const float mine = top;
     top = wave_max(top);
     if (lane == 0) tops[wave] = top;
@@ -290,6 +293,11 @@ __global__ __launch_bounds__(kThreads) void rules_kernel(const RulesArgs a) {
     if (wave != 0) return;
     r.s = to_base(sums[0] + sums[1] + sums[2] + sums[3], r.m);
     r.idx = min(min(ids_at[0], ids_at[1]), min(ids_at[2], ids_at[3]));
+    if (pass) {  // (a row of which nothing is left: its lowest id, as a token has to be one)
+        if (lane == 0) a.part[(size_t)row * a.part_ld + blockIdx.x] = StatPart{r.m, r.s, r.idx == 0x7FFFFFFF ? v0 : r.idx, 0};
+        if (lane == 0 && ti >= 0 && ti < n) a.zt[row] = at_target;
+        return;
+    }
     const bool has = target >= 0 && target < a.vocab;
     float zt = has ? at_target : NAN;  // (where the target is not this range's: not read)
     if (a.parts > 1) {
@@ -338,10 +346,11 @@ struct bild_rules {
 
 namespace bild {
 
-hipError_t launch_rules(RulesArgs a, hipStream_t st) {
+hipError_t launch_rules(RulesArgs a, hipStream_t st, int* parts) {
     a.parts = parts_of(a.rows, a.vocab);
     a.range = ((a.vocab + a.parts - 1) / a.parts + 31) / 32 * 32;  // whole words of the mask
     a.parts = (a.vocab + a.range - 1) / a.range;
+    if (parts) *parts = a.parts;
     const size_t lds = a.tokens || a.bias_ids ? sizeof(unsigned) * ((size_t)a.range + (a.bias_ids ? a.max_bias : 0)) : 0;
     if (a.dtype == BILD_DT_F32) launch<RowF32>(a, lds, st);
     else if (a.dtype == BILD_DT_BF16) launch<RowBf16>(a, lds, st);
@@ -386,7 +395,7 @@ extern "C" int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void
     if (c.rows > r->max_rows) return BILD_ECAP;
     if (c.tokens && (!c.lengths || !c.penalties || c.penalties_stride < 0 || c.penalties_stride > 1)) return BILD_EINVAL;
     if (c.bias_ids && !c.bias) return BILD_EINVAL;
-    if ((c.tokens && (c.max_tokens < 0 || c.max_tokens > kMaxTokens)) || (c.bias_ids && (c.max_bias < 0 || c.max_bias > kMaxBias))) return BILD_EINVAL;
+    if ((c.tokens && (c.max_tokens < 0 || c.max_tokens > kMaxRuleTokens)) || (c.bias_ids && (c.max_bias < 0 || c.max_bias > kMaxBiases))) return BILD_EINVAL;
     if (c.out == c.logits && c.out_stride != c.logits_stride && c.rows > 1) return BILD_EINVAL;
     RulesArgs a;
     std::memset((void*)&a, 0, sizeof(a));
