@@ -30,6 +30,7 @@ using namespace bild;
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileK = 128;    // inputs of a tile
 constexpr int kMaxWaves = 16;
@@ -38,6 +39,7 @@ constexpr int most_waves(int tiles) { return tiles <= 2 ? kMaxWaves : 8; }
 constexpr int kPartRows = 32;  // most rows of a workgroup
 // Tiles that a wave has under way (with a group per step of 32 inputs the scales take two thirds of a tile's registers).
 constexpr int ahead(int group) { return group == 32 ? 3 : 4; }
+constexpr int kDirectWaves = 8, kDirectAhead = 3;  // (with four, six, eight tiles ahead 4096 x 4096 takes 5.7, 6.2, 6.2 us instead of 5.35)
 constexpr int kChipUnits = 256;  // compute units
 constexpr int kLdsLimit = 160 * 1024;
 
@@ -312,8 +314,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
                     acc[t][s % CH] = mac<AS>(za, b, acc[t][s % CH]);
                 }
             }
-            typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-            const f16x4 sv = __builtin_bit_cast(f16x4, u.scales[g]);
+                        const f16x4 sv = __builtin_bit_cast(f16x4, u.scales[g]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -408,6 +409,98 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
     }
 }
 
+// Up to 16 rows of 16 bits without a gain, one feature tile a workgroup: its wk waves take the rows as they lie in memory, beside the codes of the same inputs.
+// Nothing is staged, so nobody waits for anybody before the sums meet.
+template <int G>
+struct DirectUnit {
+    Unit<kTileK / G> w;
+    uint4 x[4];
+};
+template <int AS, int G>
+__global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const QuantArgs a) {
+    constexpr int GT = kTileK / G, SG = G / 32, CH = SG > 1 ? 2 : 1;
+    constexpr int D = kDirectAhead;
+    __shared__ f32x4 sums[kDirectWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), f = blockIdx.x;
+    const int pieces = a.k / 8;  // (k is a multiple of 8)
+    const uint16_t* xrow = (const uint16_t*)a.x + (int64_t)min(lane & 15, a.rows - 1) * a.ldx;
+    int kt = wave;
+    const auto request = [&](DirectUnit<G>& u) {  // (past the last tile: that one again)
+        const int t = min(kt, a.tk - 1);
+        const size_t tile = (size_t)f * a.tk + t;
+        u.w.codes = a.codes[tile * 64 + lane];
+        const uint2* s = (const uint2*)a.scales + (tile * 4 + (lane >> 4)) * GT;
+#pragma unroll
+        for (int i = 0; i < GT; ++i) u.w.scales[i] = s[i];
+        if constexpr (GT == 4) u.w.zeros = ((const uint16_t*)a.zeros)[tile * 16 + (lane & 15)];
+        else u.w.zeros = a.zeros[tile * 16 + (lane & 15)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            RowVec<RowBf16, 8> v;  // (16 bits are 16 bits)
+            v.load(xrow + (size_t)min(t * 16 + j * 4 + (lane >> 4), pieces - 1) * 8);
+            __builtin_memcpy(&u.x[j], v.v, 16);
+        }
+        kt += a.wk;
+    };
+    const CodeBits bits = code_bits<AS>();
+    f32x4 total = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto process = [&](DirectUnit<G>& u, int t) {
+        const uint32_t cw[4] = {u.w.codes.x, u.w.codes.y, u.w.codes.z, u.w.codes.w};
+        if (t * 16 + 16 > pieces) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (t * 16 + j * 4 + (lane >> 4) >= pieces) u.x[j] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+            const uint32_t zw = zero_up<AS>(GT == 1 ? u.w.zeros : u.w.zeros >> (4 * g) & 15u);
+            const uint4 za = make_uint4(zw, zw, zw, zw);
+            f32x4 acc[CH];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < SG; ++s) {
+                const int j = g * SG + s;
+                const uint4 ca = codes_up<AS>(cw[j], bits);
+                acc[s % CH] = mac<AS>(ca, u.x[j], acc[s % CH]);
+                acc[s % CH] = mac<AS>(za, u.x[j], acc[s % CH]);
+            }
+                        const f16x4 sv = __builtin_bit_cast(f16x4, u.w.scales[g]);
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf((float)sv[i], acc[c][i], total[i]);
+            asm volatile("" : "+v"(total));
+        }
+    };
+    DirectUnit<G> ring[D];
+#pragma unroll
+    for (int i = 0; i < D; ++i) request(ring[i]);
+    int t = wave, left = a.turns;
+    for (; left > D; left -= D) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            if (t < a.tk) process(ring[i], t);
+            t += a.wk;
+            request(ring[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        if (i < left && t < a.tk) process(ring[i], t);
+        t += a.wk;
+    }
+    sums[wave][lane] = total;
+    lds_barrier();
+    const int q = threadIdx.x & 3, r = threadIdx.x >> 2;  // (16 rows of four: a wave)
+    if (r >= a.rows) return;
+    f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int w = 0; w < a.wk; ++w) sum += sums[w][q * 16 + r];
+    store_y(a, r, f * 16 + q * 4, sum * a.scale);
+}
+
 // What bf16 scales ask of the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
 __global__ __launch_bounds__(256) void quant_range_kernel(const uint16_t* scales, size_t count, int* range) {
     int most = -1024, least = 1024;
@@ -494,6 +587,15 @@ hipError_t launch_group(const QuantArgs& a, int group, int tiles, dim3 grid, int
     return launch_rows<AS, 128>(a, tiles, grid, waves, lds, device, st);
 }
 
+template <int AS>
+hipError_t launch_direct(const QuantArgs& a, int group, hipStream_t st) {
+    const dim3 grid(a.tn), block(64 * a.wk);
+    if (group == 32) hipLaunchKernelGGL((quant_direct_kernel<AS, 32>), grid, block, 0, st, a);
+    else if (group == 64) hipLaunchKernelGGL((quant_direct_kernel<AS, 64>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((quant_direct_kernel<AS, 128>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+
 bool shape_ok(int n, int k, int group) { return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 20) && (group == 32 || group == 64 || group == 128); }
 
 uint16_t to_scale(float v, int dtype) {
@@ -551,6 +653,15 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
     a.eps = c.eps;
     a.scale = (float)(16.0 * c.scale * std::ldexp(1.0, w->scale_exponent));
     const bool parts = c.gain || c.x_dtype == BILD_DT_F32;
+    // Where a compute unit has one feature tile at most, nobody takes the rows from LDS again.  us, staged / straight from memory, bf16, 1 and 11 rows: 1024 x 1024
+    // 3.26 / 2.72, 4.00 / 3.02; 4096 x 4096 6.23 / 5.35, 7.97 / 6.34; 4096 x 11008 11.0 / 9.5, 16.4 / 12.9; but 11008 x 4096 (688 feature tiles) 9.7 / 10.2, 11.4 / 13.8,
+    // 32000 x 4096 19.0 / 21.8, 19.6 / 28.3 (8 rows).  Four waves, from 64 input tiles on eight: 4096 x 4096 with eight 5.76, 7.46, 4096 x 11008 with four 10.1, 13.0.
+    if (!parts && c.rows <= 16 && w->tn <= kChipUnits && w->k % 8 == 0) {
+        a.wk = std::min(w->tk, w->tk >= 64 ? kDirectWaves : 4);
+        a.turns = (w->tk + a.wk - 1) / a.wk;
+        const hipError_t err = c.x_dtype == BILD_DT_F16 ? launch_direct<AS_F16>(a, w->group, st) : launch_direct<AS_BF16>(a, w->group, st);
+        return err == hipSuccess ? BILD_OK : BILD_EHIP;
+    }
     a.rows_per = std::min(c.rows, kPartRows);
     const int v = a.rows_per * (parts ? 3 : 1);
     const int tiles = v <= 16 ? 1 : v <= 32 ? 2 : v <= 48 ? 3 : 6;

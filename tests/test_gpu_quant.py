@@ -188,3 +188,28 @@ def test_refusals_leave_y_alone():
     with pytest.raises(pkg.BildError) as e:
         pkg.Quant(4, 32, 32, codes, scales, F16, np.full((4, 1), 16, np.uint8))
     assert e.value.code == b.EINVAL
+
+
+@pytest.mark.parametrize("rows", [1, 5, 16])
+@pytest.mark.parametrize("k", [8, 120, 136, 1000, 1160, 8328])
+@pytest.mark.parametrize("x_dtype", [BF16, F16])
+def test_narrow_matrices_with_any_number_of_inputs(rows, k, x_dtype):
+    """Fewer feature tiles than compute units, few and many tiles of inputs, the last of them in part; rows that do not begin at 16 bytes."""
+    rng = np.random.default_rng(k + rows)
+    for n, group, zeros in ((16, 32, True), (49, 64, False), (130, 128, True)):
+        check(rng, n, k, group, rows, x_dtype, F32 if rows == 5 else x_dtype, zeros=zeros, x_stride=k + 5, first=3)
+
+
+@pytest.mark.parametrize("x_dtype", [BF16, F16])
+@pytest.mark.parametrize("k", [72, 1032])
+def test_nothing_behind_a_row_counts(x_dtype, k):
+    """NaN in the elements behind a row's last one."""
+    rng = np.random.default_rng(k)
+    *_, q, w, s = matrix(rng, 40, k, 32)
+    wide = np.full((3, k + 9), np.nan)
+    wide[:, :k] = rng.standard_normal((3, k))
+    x, y = DeviceArray(pack(wide, x_dtype)), Rows(np.zeros((3, 40), np.float32))
+    q.matmul(x.ptr.value, x_dtype, 3, y.ptr, F32, x_stride=k + 9)
+    xh = unpack(pack(wide[:, :k], x_dtype), x_dtype)
+    want = xh @ w.T
+    close(y.get().astype(np.float64), want, tolerance(xh, s, want, F32))
