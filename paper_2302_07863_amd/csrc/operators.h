@@ -9,8 +9,8 @@ struct bild_quant {
     int scale_exponent = 0;    // the scales are those stored times 2^this
     void* mem = nullptr;       // one allocation
     const uint4* codes = nullptr;     // [tn][tk][64 lanes]: see quant.hip
-    const uint16_t* scales = nullptr; // fp16, [tn][tk][4 feature quads][128 / group][4 features]
-    const uint8_t* zeros = nullptr;   // [tn][tk][16 features], four bits a group (a byte, two with groups of 32)
+    const uint32_t* sides = nullptr;  // [tn][tk][16 features]: fp16 scales and zeros
+    const void* nothing = nullptr;    // 256 bytes of zeros
     int device = 0;
 };
 

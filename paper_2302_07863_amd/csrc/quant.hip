@@ -10,8 +10,9 @@
 //
 // Layout: tiles of 16 features x 128 inputs, 1 KiB, in the order of the matrix cores' A operand: lane l has feature l % 16, its word j
 // the inputs 32 j + 8 (l / 16) + 0 .. 7.  Of these, pair p (2p, 2p + 1) lies 4 p bits above the places where bf16 takes it (bits 3 .. 6 and 19 .. 22), the
-// last pair round the end of the word.  Scales of a tile: for the four features of an accumulator's lane side by side, group by group, as fp16 (which goes into
-// the products as it is) times a power of two of the whole matrix; zeros: feature by feature, four bits a group.
+// last pair round the end of the word.  Beside it, feature by feature, what one lane needs of a tile besides its codes: the scales as fp16 (which goes into the
+// products as it is) times a power of two of the whole matrix and the zeros, four bits a group; a word with groups of 128, two, three with groups of
+// 64, 32: one load.  (Apart, as two or more, a wave's four feature tiles of 4096 inputs took 18 instead of 13 us to come in, small as they are.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -20,6 +21,7 @@
 #include <cstring>
 #include <new>
 #include <thread>
+#include <type_traits>
 #include <vector>
 
 #include "operators.h"
@@ -30,7 +32,6 @@ using namespace bild;
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileK = 128;    // inputs of a tile
 constexpr int kMaxWaves = 16;
@@ -49,8 +50,7 @@ enum RowsAs : int { AS_BF16 = 0, AS_F16 = 1, AS_PARTS = 2 };
 
 struct QuantArgs {
     const uint4* codes;
-    const uint16_t* scales;
-    const uint8_t* zeros;
+    const uint32_t* sides;
     const void* x;
     void* y;
     const float* gain;
@@ -64,13 +64,21 @@ struct QuantArgs {
     int chunk;     // input tiles staged at a time
     int chunks;
     int turns;     // of a wave over them (several chunks: a multiple of ahead())
+    const uint4* nothing;  // 16 bytes of zeros
     int sums_at;   // where in LDS the sums lie: behind the rows, or (per 1) in their place
 };
 
+// Products of 16 features and 16 rows: a lane gets four rows of one feature, so that it scales them by one number.
 template <int AS>
-__device__ __forceinline__ f32x4 mac(const uint4& a, const uint4& b, const f32x4& c) {
-    if constexpr (AS == AS_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mac(const uint4& codes, const uint4& x, const f32x4& c) {
+    if constexpr (AS == AS_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, codes), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, codes), c, 0, 0, 0);
+}
+// A wave's products to LDS, [row][feature].
+__device__ __forceinline__ void put_sums(f32x4* to, int lane, const f32x4& v) {
+    float* p = (float*)to + (lane >> 4) * 64 + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[16 * i] = v[i];
 }
 
 // What turns codes into numbers, in registers: an and-or has room for one constant that is none.
@@ -221,12 +229,25 @@ __device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (
     if (gain) squares[0][tid] += ss;
 }
 
+// What a lane has of its feature besides codes, of the tile's GT groups.
+constexpr int side_words(int gt) { return gt == 4 ? 3 : gt; }
+template <int GT>
+struct Side {
+    uint32_t w[side_words(GT)];
+    __device__ __forceinline__ void load(const uint32_t* sides, size_t tile, int feature) {
+        __builtin_memcpy(w, sides + (tile * 16 + feature) * side_words(GT), sizeof(w));
+    }
+    __device__ __forceinline__ float scale(int g) const {
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(GT == 1 ? w[0] : w[g >> 1] >> (16 * (g & 1))));
+    }
+    __device__ __forceinline__ uint32_t zero(int g) const { return GT == 1 ? w[0] >> 16 : w[side_words(GT) - 1] >> (4 * g) & 15u; }
+};
+
 // What a wave has requested of one tile.
 template <int GT>
 struct Unit {
     uint4 codes;
-    uint2 scales[GT];
-    uint32_t zeros;
+    Side<GT> side;
 };
 
 // A workgroup has up to rows_per rows (NT tiles of 16 rows of the operand) and stages them once, or (CHUNKED) chunk by chunk of the inputs where they do
@@ -247,7 +268,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
     const int r0 = blockIdx.y * a.rows_per, rows = min(a.rows_per, a.rows - r0), v = PARTS * rows;
     const int f0 = (int)blockIdx.x * wf * a.per + wfid;  // the wave's feature tiles: every wf-th from here (some of the last workgroup's are not there: they load the last one's)
     const int turns = a.turns, segments = CHUNKED ? a.chunks : a.per;
-    f32x4* sums = (f32x4*)(lds + a.sums_at);  // [feature tile of a wave][wave][row tile][lane]
+    f32x4* sums = (f32x4*)(lds + a.sums_at);  // [feature tile of a wave][wave][row tile][row][four features]
 
     // the tile of a segment's turn (past the end: the last one there is)
     int ps = 0, pj = 0;
@@ -255,11 +276,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
         const int f = min(f0 + (CHUNKED ? 0 : ps) * wf, a.tn - 1), kt = min((CHUNKED ? ps * a.chunk : 0) + wkid + pj * wk, a.tk - 1);
         const size_t tile = (size_t)f * a.tk + kt;
         u.codes = a.codes[tile * 64 + lane];
-        const uint2* s = (const uint2*)a.scales + (tile * 4 + (lane >> 4)) * GT;
-#pragma unroll
-        for (int i = 0; i < GT; ++i) u.scales[i] = s[i];
-        if constexpr (GT == 4) u.zeros = ((const uint16_t*)a.zeros)[tile * 16 + (lane & 15)];
-        else u.zeros = a.zeros[tile * 16 + (lane & 15)];
+        u.side.load(a.sides, tile, lane & 15);
         if (++pj == turns) {
             pj = 0;
             ps = min(ps + 1, segments - 1);
@@ -296,7 +313,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
         asm volatile("" : "+v"(xs));  // (else the compiler keeps an address for every operand of the tiles ahead in a register)
 #pragma unroll
         for (int g = 0; g < GT; ++g) {
-            const uint32_t zw = zero_up<AS>(GT == 1 ? u.zeros : u.zeros >> (4 * g) & 15u);
+            const uint32_t zw = zero_up<AS>(u.side.zero(g));
             const uint4 za = make_uint4(zw, zw, zw, zw);
             f32x4 acc[NT][CH];
 #pragma unroll
@@ -314,13 +331,13 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
                     acc[t][s % CH] = mac<AS>(za, b, acc[t][s % CH]);
                 }
             }
-                        const f16x4 sv = __builtin_bit_cast(f16x4, u.scales[g]);
+                        const float scale = u.side.scale(g);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf((float)sv[i], acc[t][c][i], total[t][i]);
+                    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf(scale, acc[t][c][i], total[t][i]);
                 asm volatile("" : "+v"(total[t]));  // (now: four registers less than a group that waits)
             }
         }
@@ -328,7 +345,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
     const auto keep = [&](int s) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            sums[((s * nw + wave) * NT + t) * 64 + lane] = total[t];
+            put_sums(sums + ((s * nw + wave) * NT + t) * 64, lane, total[t]);
             total[t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     };
@@ -394,7 +411,7 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part) {
             const int c = part * rows + r;
-            const f32x4* from = sums + ((p * nw + w0) * NT + (c >> 4)) * 64 + q * 16 + (c & 15);
+            const f32x4* from = sums + ((p * nw + w0) * NT + (c >> 4)) * 64 + (c & 15) * 4 + q;
 #pragma unroll 4
             for (int w = 0; w < wk; ++w) sum += from[w * NT * 64];
         }
@@ -429,11 +446,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
         const int t = min(kt, a.tk - 1);
         const size_t tile = (size_t)f * a.tk + t;
         u.w.codes = a.codes[tile * 64 + lane];
-        const uint2* s = (const uint2*)a.scales + (tile * 4 + (lane >> 4)) * GT;
-#pragma unroll
-        for (int i = 0; i < GT; ++i) u.w.scales[i] = s[i];
-        if constexpr (GT == 4) u.w.zeros = ((const uint16_t*)a.zeros)[tile * 16 + (lane & 15)];
-        else u.w.zeros = a.zeros[tile * 16 + (lane & 15)];
+        u.w.side.load(a.sides, tile, lane & 15);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             RowVec<RowBf16, 8> v;  // (16 bits are 16 bits)
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
         }
 #pragma unroll
         for (int g = 0; g < GT; ++g) {
-            const uint32_t zw = zero_up<AS>(GT == 1 ? u.w.zeros : u.w.zeros >> (4 * g) & 15u);
+            const uint32_t zw = zero_up<AS>(u.w.side.zero(g));
             const uint4 za = make_uint4(zw, zw, zw, zw);
             f32x4 acc[CH];
 #pragma unroll
@@ -465,11 +478,11 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
                 acc[s % CH] = mac<AS>(ca, u.x[j], acc[s % CH]);
                 acc[s % CH] = mac<AS>(za, u.x[j], acc[s % CH]);
             }
-                        const f16x4 sv = __builtin_bit_cast(f16x4, u.w.scales[g]);
+                        const float scale = u.w.side.scale(g);
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf((float)sv[i], acc[c][i], total[i]);
+                for (int i = 0; i < 4; ++i) total[i] = __builtin_fmaf(scale, acc[c][i], total[i]);
             asm volatile("" : "+v"(total));
         }
     };
@@ -491,17 +504,184 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
         if (i < left && t < a.tk) process(ring[i], t);
         t += a.wk;
     }
-    sums[wave][lane] = total;
+    put_sums(sums[wave], lane, total);
     lds_barrier();
     const int q = threadIdx.x & 3, r = threadIdx.x >> 2;  // (16 rows of four: a wave)
     if (r >= a.rows) return;
     f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int w = 0; w < a.wk; ++w) sum += sums[w][q * 16 + r];
+    for (int w = 0; w < a.wk; ++w) sum += sums[w][r * 4 + q];
     store_y(a, r, f * 16 + q * 4, sum * a.scale);
 }
 
-// What bf16 scales ask of the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
+// ---- blocks of rows
+// 64 rows of 16 bits by 128 features a workgroup.  Eight waves: two have the block's halves of the features, 64 x 64 products each, of every fourth input tile, so
+// that an operand read from LDS serves four feature tiles and a code taken apart four row tiles.  The rows of four half tiles of inputs at a time go from
+// memory to LDS without passing through registers, three halves ahead of their use; codes come two tiles ahead into registers.
+// Bound: both what a compute unit multiplies, takes apart and scales and what it can have under way at once: 509 rows of fp16 by 4096 x 4096, groups of 128,
+// take 27 us (630 TFLOP/s), 20 to 22 without the loads, 18 the loads alone; a tile ahead instead of three halves and two tiles 29.  The matrix cores alone would need
+// 7.  bf16 34 us: it has no subtraction of pairs, so that every product with codes has a second with the zeros.
+constexpr int kBlockRows = 64, kBlockFeatures = 128, kBlockSplit = 4;
+
+// fp16 only: 1024 + q, then less 1024 + z, which is q - z as it is.  (bf16 has no subtraction of pairs: a second product does it, as above.)
+template <int AS>
+__device__ __forceinline__ uint4 codes_less(uint32_t w, const CodeBits& b, uint32_t z) {
+    const uint4 q = codes_up<AS>(w, b);
+    if constexpr (AS != AS_F16) return q;
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    const f16x2 less = __builtin_bit_cast(f16x2, z);
+    const auto one = [&](uint32_t v) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) + less); };
+    return make_uint4(one(q.x), one(q.y), one(q.z), one(q.w));
+}
+
+// Four feature tiles' codes; what lies beside those of the f-th is in the lanes 16 f .. 16 f + 15.
+template <int GT>
+struct Four {
+    uint4 codes[4];
+    Side<GT> side;
+};
+
+template <int AS, int G>
+__global__ __launch_bounds__(512) void quant_block_kernel(const QuantArgs a) {
+    constexpr int GT = kTileK / G, SG = G / 32;
+    constexpr int SUM = AS == AS_F16 || SG < 2 ? SG : 2;  // steps between scalings (bf16 has no registers for sums that outlast half a tile)
+    constexpr int kStage = kBlockSplit * kBlockRows * 8;  // pieces of 16 bytes: [input tile][row][half a tile's 8]
+    __shared__ uint4 x0[kStage], x1[kStage], x2[kStage], x3[kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ks = wave >> 1;
+    const int per_die = a.per, fb = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3) % per_die, rb = (int)(blockIdx.x >> 3) / per_die;
+    if (fb * (kBlockFeatures / 16) >= a.tn) return;
+    const int r0 = rb * kBlockRows, pieces = a.k / 8;
+    const int f0 = fb * (kBlockFeatures / 16) + (wave & 1) * 4;
+
+    // Piece p of row r lies at place p ^ (r / 2 & 7): the lanes of an operand have 16 rows and meet all banks.  A wave brings rows 8 w .. 8 w + 7 of every tile.
+    const int own = wave * 8 + (lane >> 3), first = (lane & 7) ^ (own >> 1 & 7);
+    const uint4* const row = (const uint4*)((const uint16_t*)a.x + (int64_t)min(r0 + own, a.rows - 1) * a.ldx);
+    const auto bring = [&](uint4* to, int step, int t) {  // `step`: pieces before it
+        const int p = step + t * 16 + first;
+        const uint4* from = p < pieces ? row + p : a.nothing;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)(to + (t * kBlockRows + wave * 8) * 8), 16, 0, 0);
+    };
+    const auto tile_of = [&](int f, int t0) { return (size_t)min(f0 + f, a.tn - 1) * a.tk + min(t0 + ks, a.tk - 1); };
+    const auto request = [&](Four<GT>& u, int t0, int f) {
+        u.codes[f] = a.codes[tile_of(f, t0) * 64 + lane];
+        if (f == 3) u.side.load(a.sides, tile_of(lane >> 4, t0), lane & 15);
+    };
+    const CodeBits bits = code_bits<AS>();
+    f32x4 total[4][4], acc[4][4];  // [feature tile][row tile]
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) total[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Half a tile; `feed` runs in eight parts between the products.
+    const auto process = [&](auto half, const Four<GT>& u, const Side<GT> (&side)[4], const uint4* x, auto&& feed) {
+        constexpr int H = decltype(half)::value;
+        const uint4* at = x + (ks * kBlockRows + (lane & 15)) * 8;
+        uint4 b[2][4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) b[s][t] = at[t * 128 + ((s * 4 + (lane >> 4)) ^ (lane >> 1 & 7))];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int j = 2 * H + s, g = j / SG;
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const uint32_t cw[4] = {u.codes[f].x, u.codes[f].y, u.codes[f].z, u.codes[f].w};
+                const uint32_t zw = zero_up<AS>(side[f].zero(g));
+                const uint4 za = make_uint4(zw, zw, zw, zw), ca = codes_less<AS>(cw[j], bits, zw);
+                feed(s * 4 + f);
+                __builtin_amdgcn_sched_barrier(0x8F);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    acc[f][t] = mac<AS>(ca, b[s][t], j % SUM == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[f][t]);
+                    if constexpr (AS != AS_F16) acc[f][t] = mac<AS>(za, b[s][t], acc[f][t]);
+                }
+                if (j % SUM == SUM - 1) {
+                    const float scale = side[f].scale(g);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) total[f][t][i] = __builtin_fmaf(scale, acc[f][t][i], total[f][t][i]);
+                        asm volatile("" : "+v"(total[f][t]));
+                    }
+                }
+            }
+        }
+    };
+    // The rows of half h are there: they were requested three halves ago, since when the wave has had thirteen loads more (four a half and, two tiles ahead, five of
+    // codes in the lower one).  Behind the barrier those of all waves are, and nobody reads the half before any more.
+    const auto arrive = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x007D);  // (vmcnt 13, lgkmcnt 0: what it has read itself)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // Past the end the rows are zeros; so is what lies beside the codes (of the last tile again, it may be infinite).
+    Side<GT> side[4];
+    const auto spread = [&](const Side<GT>& all, int t0) {
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int i = 0; i < side_words(GT); ++i)
+                side[f].w[i] = t0 + ks < a.tk ? (uint32_t)__builtin_amdgcn_ds_bpermute((f * 16 + (lane & 15)) * 4, (int)all.w[i]) : 0u;
+    };
+    typedef std::integral_constant<int, 0> Low;
+    typedef std::integral_constant<int, 1> High;
+    // A tile: its rows in x_low and x_high; to `third` and (when it has been read) x_low come the rows three halves on, to `u2` the codes two tiles on.
+    const auto turn = [&](int t0, const Four<GT>& u, Four<GT>& u2, uint4* x_low, const uint4* x_high, uint4* third) {
+        arrive();
+        spread(u.side, t0);
+        process(Low(), u, side, x_low, [&](int part) {
+            if (part < 4) bring(third, t0 * 16 + 72, part);
+            else request(u2, t0 + 2 * kBlockSplit, part - 4);
+        });
+        arrive();
+        process(High(), u, side, x_high, [&](int part) { if (part < 4) bring(x_low, t0 * 16 + 128, part); });
+        return t0 + kBlockSplit < a.tk;
+    };
+    Four<GT> u0, u1, u2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bring(x0, 0, i);
+        request(u0, 0, i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bring(x1, 8, i);
+        request(u1, kBlockSplit, i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bring(x2, 64, i);
+    for (int t0 = 0;; t0 += 6 * kBlockSplit) {
+        if (!turn(t0, u0, u2, x0, x1, x3)) break;
+        if (!turn(t0 + kBlockSplit, u1, u0, x2, x3, x1)) break;
+        if (!turn(t0 + 2 * kBlockSplit, u2, u1, x0, x1, x3)) break;
+        if (!turn(t0 + 3 * kBlockSplit, u0, u2, x2, x3, x1)) break;
+        if (!turn(t0 + 4 * kBlockSplit, u1, u0, x0, x1, x3)) break;
+        if (!turn(t0 + 5 * kBlockSplit, u2, u1, x2, x3, x1)) break;
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // (vmcnt 0: what is still under way goes where the sums come)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // The four shares meet in LDS: [wave][feature tile][row][four features], a row tile at a time; a wave has a feature tile of the result.
+    f32x4* sums = (f32x4*)x0;
+    const int half = wave >> 2, tile = wave & 3;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (t) lds_barrier();
+#pragma unroll
+        for (int f = 0; f < 4; ++f) put_sums(sums + (wave * 4 + f) * 64, lane, total[f][t]);
+        lds_barrier();
+        f32x4 sum = sums[(half * 4 + tile) * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < kBlockSplit; ++k) sum += sums[((2 * k + half) * 4 + tile) * 64 + lane];
+        const int to = r0 + t * 16 + (lane >> 2);
+        if (to < a.rows) store_y(a, to, (fb * (kBlockFeatures / 16) + half * 4 + tile) * 16 + (lane & 3) * 4, sum * a.scale);
+    }
+}
+
+// What bf16 scales ask of''' the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
 __global__ __launch_bounds__(256) void quant_range_kernel(const uint16_t* scales, size_t count, int* range) {
     int most = -1024, least = 1024;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
@@ -518,7 +698,7 @@ __global__ __launch_bounds__(256) void quant_range_kernel(const uint16_t* scales
 
 // From rows of codes (two a byte), scales and zeros to tiles.  A thread per lane and tile; `bad`: a zero above 15.
 __global__ __launch_bounds__(256) void quant_layout_kernel(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, int k, int group, int tk, size_t lanes,
-                                                           int bf16_shift, int bf16, uint32_t* to_codes, uint16_t* to_scales, uint8_t* to_zeros, unsigned* bad) {
+                                                           int bf16_shift, int bf16, uint32_t* to_codes, uint32_t* to_sides, unsigned* bad) {
     const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (at >= lanes) return;
     const int lane = (int)(at & 63);
@@ -538,19 +718,19 @@ __global__ __launch_bounds__(256) void quant_layout_kernel(const uint8_t* codes,
     }
     const int gt = kTileK / group, groups = (k + group - 1) / group;
     if (lane >= 16) return;  // feature `lane` of the tile
-    unsigned nibbles = 0;
+    uint32_t side[4] = {0, 0, 0, 0};
     for (int g = 0; g < gt; ++g) {
         const int gg = kt * gt + g;
         const bool in = f < n && gg < groups;
         uint16_t s = in ? scales[(size_t)f * groups + gg] : (uint16_t)0;
         if (bf16) s = RowF16::down(ldexpf(bf2f(s), bf16_shift));  // (exact: the caller has seen to it)
-        to_scales[((tile * 4 + (lane >> 2)) * gt + g) * 4 + (lane & 3)] = s;
         const unsigned z = in && zeros ? zeros[(size_t)f * groups + gg] : 8u;
         if (z > 15u) *bad = 1u;
-        nibbles |= (z & 15u) << (4 * g);
+        side[g >> 1] |= (uint32_t)s << (16 * (g & 1));
+        if (gt == 1) side[0] |= (z & 15u) << 16;
+        else side[side_words(gt) - 1] |= (z & 15u) << (4 * g);
     }
-    if (gt == 4) ((uint16_t*)to_zeros)[tile * 16 + lane] = (uint16_t)nibbles;
-    else to_zeros[tile * 16 + lane] = (uint8_t)nibbles;
+    for (int i = 0; i < side_words(gt); ++i) to_sides[(tile * 16 + lane) * side_words(gt) + i] = side[i];
 }
 
 template <void (*KERNEL)(QuantArgs)>
@@ -596,6 +776,14 @@ hipError_t launch_direct(const QuantArgs& a, int group, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <int AS>
+hipError_t launch_block(const QuantArgs& a, int group, dim3 grid, hipStream_t st) {
+    if (group == 32) hipLaunchKernelGGL((quant_block_kernel<AS, 32>), grid, dim3(512), 0, st, a);
+    else if (group == 64) hipLaunchKernelGGL((quant_block_kernel<AS, 64>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((quant_block_kernel<AS, 128>), grid, dim3(512), 0, st, a);
+    return hipGetLastError();
+}
+
 bool shape_ok(int n, int k, int group) { return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 20) && (group == 32 || group == 64 || group == 128); }
 
 uint16_t to_scale(float v, int dtype) {
@@ -636,8 +824,7 @@ namespace bild {
 int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) {
     QuantArgs a;
     a.codes = w->codes;
-    a.scales = w->scales;
-    a.zeros = w->zeros;
+    a.sides = w->sides;
     a.x = c.x;
     a.y = c.y;
     a.gain = c.gain;
@@ -660,6 +847,17 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
         a.wk = std::min(w->tk, w->tk >= 64 ? kDirectWaves : 4);
         a.turns = (w->tk + a.wk - 1) / a.wk;
         const hipError_t err = c.x_dtype == BILD_DT_F16 ? launch_direct<AS_F16>(a, w->group, st) : launch_direct<AS_BF16>(a, w->group, st);
+        return err == hipSuccess ? BILD_OK : BILD_EHIP;
+    }
+    // From 96 blocks of 64 rows by 128 features on.  us, staged / in blocks, groups of 64 (4096 x 4096, 1024 wide) and 128, fp16: 4096 x 4096 of 128, 256, 1024 rows (64, 128,
+    // 512 blocks) 20.1 / 25.3, 30.0 / 26.2, 90.9 / 51.7; 4096 x 11008 of 128, 256, 1024 46.4 / 51.6, 73.9 / 53.6, 213 / 107; 11008 x 4096 of 96 rows (172) 38.0 / 24.8;
+    // 32000 x 1024 of 33 and 512 (250, 2000) 18.4 / 13.2, 111 / 92; 1024 x 1024 of 512 and 1024 (64, 128) 7.4 / 12.0, 10.7 / 11.4.
+    const int blocks = (w->tn + kBlockFeatures / 16 - 1) / (kBlockFeatures / 16), row_blocks64 = (c.rows + kBlockRows - 1) / kBlockRows;
+    if (!parts && (int64_t)blocks * row_blocks64 >= 96 && (int64_t)blocks * row_blocks64 <= 1 << 22 && w->k % 8 == 0 && ((uintptr_t)c.x & 15) == 0 && c.x_stride % 8 == 0) {
+        a.nothing = (const uint4*)w->nothing;
+        a.per = (blocks + 7) / 8;
+        const dim3 grid((unsigned)(8 * a.per * row_blocks64));
+        const hipError_t err = c.x_dtype == BILD_DT_F16 ? launch_block<AS_F16>(a, w->group, grid, st) : launch_block<AS_BF16>(a, w->group, grid, st);
         return err == hipSuccess ? BILD_OK : BILD_EHIP;
     }
     a.rows_per = std::min(c.rows, kPartRows);
@@ -752,23 +950,23 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
     q->group = group;
     q->tn = (n + 15) / 16;
     q->tk = (k + kTileK - 1) / kTileK;
-    const size_t tiles = (size_t)q->tn * q->tk, tile_scales = 16 * (size_t)(kTileK / group);
+    const size_t tiles = (size_t)q->tn * q->tk;
     const size_t groups = (size_t)(k + group - 1) / group;
     // what stays, and behind it what was given
-    const size_t code_bytes = tiles * 1024, scale_bytes = (tiles * tile_scales * 2 + 255) / 256 * 256, zero_bytes = (tiles * 16 * (group == 32 ? 2 : 1) + 255) / 256 * 256;
+    const size_t code_bytes = tiles * 1024, side_bytes = (tiles * 64 * side_words(kTileK / group) + 255) / 256 * 256;
     const size_t raw_codes = (size_t)n * ((k + 1) / 2), raw_scales = (size_t)n * groups * 2, raw_zeros = zeros ? (size_t)n * groups : 0;
     const size_t scales_at = (raw_codes + 255) / 256 * 256, zeros_at = scales_at + (raw_scales + 255) / 256 * 256, bad_at = zeros_at + (raw_zeros + 255) / 256 * 256;
     char* raw = nullptr;
     int rc = BILD_OK;
     if (hipGetDevice(&q->device) != hipSuccess) rc = BILD_EHIP;
-    else if (hipMalloc(&q->mem, code_bytes + scale_bytes + zero_bytes) != hipSuccess) q->mem = nullptr, rc = BILD_ENOMEM;
+    else if (hipMalloc(&q->mem, code_bytes + side_bytes + 256) != hipSuccess) q->mem = nullptr, rc = BILD_ENOMEM;
     else if (hipMalloc((void**)&raw, bad_at + 256) != hipSuccess) raw = nullptr, rc = BILD_ENOMEM;
     if (rc == BILD_OK) {
         q->codes = (const uint4*)q->mem;
-        q->scales = (const uint16_t*)((char*)q->mem + code_bytes);
-        q->zeros = (const uint8_t*)q->mem + code_bytes + scale_bytes;
+        q->sides = (const uint32_t*)((char*)q->mem + code_bytes);
+        q->nothing = (char*)q->mem + code_bytes + side_bytes;
         unsigned bad = 0;
-        bool ok = hipMemcpy(raw, codes, raw_codes, hipMemcpyDefault) == hipSuccess && hipMemcpy(raw + scales_at, scales, raw_scales, hipMemcpyDefault) == hipSuccess &&
+        bool ok = hipMemset((void*)q->nothing, 0, 256) == hipSuccess && hipMemcpy(raw, codes, raw_codes, hipMemcpyDefault) == hipSuccess && hipMemcpy(raw + scales_at, scales, raw_scales, hipMemcpyDefault) == hipSuccess &&
                   (!zeros || hipMemcpy(raw + zeros_at, zeros, raw_zeros, hipMemcpyDefault) == hipSuccess) && hipMemset(raw + bad_at, 0, sizeof(unsigned)) == hipSuccess;
         const size_t lanes = tiles * 64;
         const int bf16 = scale_dtype == BILD_DT_BF16;
@@ -788,8 +986,8 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
         }
         if (ok && !bad) {
             hipLaunchKernelGGL(quant_layout_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, nullptr, (const uint8_t*)raw, (const uint16_t*)(raw + scales_at),
-                               zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, -q->scale_exponent, bf16, (uint32_t*)q->codes, (uint16_t*)q->scales,
-                               (uint8_t*)q->zeros, (unsigned*)(raw + bad_at));
+                               zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, -q->scale_exponent, bf16, (uint32_t*)q->codes, (uint32_t*)q->sides,
+                               (unsigned*)(raw + bad_at));
             ok = hipGetLastError() == hipSuccess && hipMemcpy(&bad, raw + bad_at, sizeof(bad), hipMemcpyDeviceToHost) == hipSuccess;
         }
         rc = !ok ? BILD_EHIP : bad ? BILD_EINVAL : BILD_OK;

@@ -213,3 +213,33 @@ def test_nothing_behind_a_row_counts(x_dtype, k):
     xh = unpack(pack(wide[:, :k], x_dtype), x_dtype)
     want = xh @ w.T
     close(y.get().astype(np.float64), want, tolerance(xh, s, want, F32))
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [(BF16, BF16), (F16, F16), (BF16, F32), (F16, BF16)])
+@pytest.mark.parametrize("n,k,rows", [(1600, 8, 500), (1601, 264, 509), (2050, 136, 470), (12300, 72, 33), (900, 1160, 833), (1700, 2056, 449)])
+def test_many_rows_and_features(n, k, rows, x_dtype, y_dtype):
+    """Blocks of rows and features, the last of either in part; inputs that end inside a tile, in one of the four that are multiplied at a time."""
+    rng = np.random.default_rng(n + k + rows)
+    group = {8: 32, 264: 64, 136: 128, 72: 64, 1160: 32, 2056: 128}[k]
+    check(rng, n, k, group, rows, x_dtype, y_dtype, zeros=rows % 2 == 1, scale_dtype=F16, scale=0.5, x_stride=k + 8, y_stride=n + 3)
+
+
+@pytest.mark.parametrize("x_dtype", [BF16, F16])
+def test_blocks_keep_to_their_rows(x_dtype):
+    """NaN behind the rows' inputs, an infinite row and an infinite scale of the last group: everything else stays finite."""
+    rng = np.random.default_rng(5)
+    n, k, rows, group = 1610, 200, 520, 64
+    codes, scales, z, _, w, s = matrix(rng, n, k, group, True)
+    scales[7, -1] = np.float16(np.inf).view(np.uint16)
+    q = pkg.Quant(n, k, group, codes, scales, F16, z)
+    wide = np.full((rows, k + 8), np.nan)
+    wide[:, :k] = rng.standard_normal((rows, k))
+    wide[100, :k] = np.inf
+    x, y = DeviceArray(pack(wide, x_dtype)), Rows(np.zeros((rows, n), np.float32))
+    q.matmul(x.ptr.value, x_dtype, rows, y.ptr, F32, x_stride=k + 8)
+    got = y.get().astype(np.float64)
+    assert not np.isfinite(got[100]).any() and not np.isfinite(got[:, 7]).any()
+    keep_rows, keep = np.arange(rows) != 100, np.arange(n) != 7
+    xh = unpack(pack(wide[keep_rows, :k], x_dtype), x_dtype)
+    want = xh @ w[keep].T
+    close(got[keep_rows][:, keep], want, tolerance(xh, s[keep], want, F32))
