@@ -308,7 +308,8 @@ int bild_quant_destroy(bild_quant* w); /* nothing that uses it may still run */
 
 /* y[r][n] = scale * sum over k of xh[r][k] * w[n][k], xh = x, or with gain x[r][k] * gain[k] / sqrt(mean over k of x[r][k]^2 + eps): the RMSNorm in front of
  * a projection or an LM head.  Products are those of the values themselves (none is rounded on the way, but x * gain to 24 bits), sums are
- * fp32, y is rounded once.  rows >= 1; made for the rows of a decoder pass (up to BILD_MAX_ROWS), longer blocks are taken as they are. */
+ * fp32, y is rounded once.  rows >= 1: those of a decoder pass, of a
+ * prompt (16 bits without gain from 96 blocks of 64 rows x 128 features on, if k is a multiple of 8 and rows begin at multiples of 16 bytes, in a kernel made for it). */
 typedef struct bild_quant_call {
     const void* x;      /* [rows][k], row r at x + r * x_stride               */
     int64_t x_stride;
@@ -433,7 +434,8 @@ int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_strea
 /* ---- the operators inside a state's passes ----
  * The LM head of model `which` (1 small, 2 large) of this state's passes becomes `head` (n = vocab, k = d_model, else BILD_EINVAL), behind the model's final
  * norm and times its logit scale; NULL: the model's own again.  Everything that is read off the logits (policies, draws, acceptance) follows.  The matrix is
- * borrowed and has to outlive the state or the next call.  The passes then keep their logits in device memory (32 x vocabulary floats a model). */
+ * borrowed and has to outlive the state or the next call.  The passes then keep their logits in device memory (32 x vocabulary floats a model).
+ * (bild_bench.h's counts of bytes stay those of the model's own head.) */
 int bild_set_quant_head(bild_state* s, int which, const bild_quant* head /* nullable */);
 /* Penalties (NULL: none) and biases (n 0: none; id i gets bias[i], the last entry of an id counts; finite, at most 1023, ids in the vocabulary) for every token that
  * either model of the state proposes from now on, as bild_rules_apply has them: the row's tokens are the sequence up to the row, drafts

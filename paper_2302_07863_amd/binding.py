@@ -268,14 +268,16 @@ class Quant:
         h = C.c_void_p()
         codes, scales, zeros = [np.ascontiguousarray(a) if isinstance(a, np.ndarray) else a for a in (codes, scales, zeros)]
         _check(lib().bild_quant_create(n, k, group, _where(codes), _where(scales), scale_dtype, _where(zeros), C.byref(h)), "bild_quant_create")
-        self.h, self.n, self.k = h, n, k
+        self.h, self.n, self.k, self._matmul = h, n, k, lib().bild_quant_matmul   # (looked up once: a call is as long as a small kernel)
 
     def matmul(self, x: int, x_dtype: int, rows: int, y: int, y_dtype: int, x_stride: Optional[int] = None, y_stride: Optional[int] = None,
                gain: Optional[int] = None, eps: float = 0.0, scale: float = 1.0, stream: Optional[int] = None):
         """Device pointers; strides in elements (None: rows side by side)."""
         call = _QUANT_CALL.pack(x or 0, self.k if x_stride is None else x_stride, y or 0, self.n if y_stride is None else y_stride, gain or 0, rows,
                                 x_dtype, y_dtype, eps, scale)
-        _check(lib().bild_quant_matmul(self.h, call, stream), "bild_quant_matmul")
+        code = self._matmul(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_quant_matmul")
 
     def close(self):
         if self.h:
@@ -293,7 +295,7 @@ class Rotary:
         self.cfg = RotaryConfig(int(halves), rot_dim, scaling, original, base, factor, low, high, magnitude)
         h = C.c_void_p()
         _check(lib().bild_rotary_create(C.byref(self.cfg), C.byref(h)), "bild_rotary_create")
-        self.h = h
+        self.h, self._apply = h, lib().bild_rotary_apply
 
     def frequencies(self):
         f, m = np.zeros(self.cfg.rot_dim // 2, np.float64), C.c_double()
@@ -303,7 +305,9 @@ class Rotary:
     def apply(self, d_head: int, dtype: int, tokens: int, q: RotaryRows, k: Optional[RotaryRows] = None, positions: Optional[int] = None,
               first: int = 0, inverse: bool = False, stream: Optional[int] = None):
         call = _ROTARY_CALL.pack(*q.fields, *(k or _NO_ROWS).fields, positions or 0, first, tokens, d_head, dtype, int(inverse), 0)
-        _check(lib().bild_rotary_apply(self.h, call, stream), "bild_rotary_apply")
+        code = self._apply(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_rotary_apply")
 
     def close(self):
         if self.h:
@@ -319,7 +323,7 @@ class Rules:
     def __init__(self, vocab: int, max_rows: int):
         h = C.c_void_p()
         _check(lib().bild_rules_create(vocab, max_rows, C.byref(h)), "bild_rules_create")
-        self.h, self.vocab = h, vocab
+        self.h, self.vocab, self._apply = h, vocab, lib().bild_rules_apply
 
     def apply(self, logits: int, dtype: int, rows: int, out: Optional[int] = None, stats: Optional[int] = None, targets: Optional[int] = None,
               logits_stride: Optional[int] = None, out_stride: Optional[int] = None, tokens: Optional[int] = None, tokens_stride: int = 0,
@@ -330,7 +334,9 @@ class Rules:
         call = _RULES_CALL.pack(logits or 0, self.vocab if logits_stride is None else logits_stride, out or 0, self.vocab if out_stride is None else out_stride,
                                 targets or 0, stats or 0, tokens or 0, tokens_stride, lengths or 0, starts or 0, penalties or 0, penalties_stride,
                                 bias_ids or 0, bias or 0, bias_stride, bias_counts or 0, mask or 0, mask_stride, rows, dtype, max_tokens, max_bias)
-        _check(lib().bild_rules_apply(self.h, call, stream), "bild_rules_apply")
+        code = self._apply(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_rules_apply")
 
     def close(self):
         if self.h:

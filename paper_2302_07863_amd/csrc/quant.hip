@@ -8,7 +8,7 @@
 // off again.  Both products are exact and go into the same fp32 accumulator step by step, so what cancels is never
 // larger than 32 inputs' sum; scales are applied to the accumulators once a group.  No weight is ever rounded.
 //
-// Layout: tiles of 16 features x 128 inputs, 1 KiB, in the order of the matrix cores' A operand: lane l has feature l % 16, its word j
+// Layout: tiles of 16 features x 128 inputs, 1 KiB, in the order of the matrix cores' operand: lane l has feature l % 16, its word j
 // the inputs 32 j + 8 (l / 16) + 0 .. 7.  Of these, pair p (2p, 2p + 1) lies 4 p bits above the places where bf16 takes it (bits 3 .. 6 and 19 .. 22), the
 // last pair round the end of the word.  Beside it, feature by feature, what one lane needs of a tile besides its codes: the scales as fp16 (which goes into the
 // products as it is) times a power of two of the whole matrix and the zeros, four bits a group; a word with groups of 128, two, three with groups of
@@ -164,7 +164,7 @@ __device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&
     }
 }
 
-// The workgroup's rows, inputs of the tiles t0 .. t1 - 1, to LDS in the order of the matrix cores' B operand:
+// The workgroup's rows, inputs of the tiles t0 .. t1 - 1, to LDS in the order of the matrix cores' operand:
 // [step of 32 inputs][row of the operand][4 pieces of 8].  Row v of the operand is part v / rows of row v % rows.  Inputs from the k-th on are zero.
 // A wave's 64 pieces belong to one row; with a norm it adds up their squares.  `between` runs behind the requests of the first U pieces a thread
 // (loads come back in order: what it requests does not keep these waiting).
@@ -849,11 +849,11 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
         const hipError_t err = c.x_dtype == BILD_DT_F16 ? launch_direct<AS_F16>(a, w->group, st) : launch_direct<AS_BF16>(a, w->group, st);
         return err == hipSuccess ? BILD_OK : BILD_EHIP;
     }
-    // From 96 blocks of 64 rows by 128 features on.  us, staged / in blocks, groups of 64 (4096 x 4096, 1024 wide) and 128, fp16: 4096 x 4096 of 128, 256, 1024 rows (64, 128,
+    // More rows than a workgroup stages, from 96 blocks of 64 rows by 128 features on.  us, staged / in blocks, groups of 64 (4096 x 4096, 1024 wide) and 128, fp16: 4096 x 4096 of 128, 256, 1024 rows (64, 128,
     // 512 blocks) 20.1 / 25.3, 30.0 / 26.2, 90.9 / 51.7; 4096 x 11008 of 128, 256, 1024 46.4 / 51.6, 73.9 / 53.6, 213 / 107; 11008 x 4096 of 96 rows (172) 38.0 / 24.8;
     // 32000 x 1024 of 33 and 512 (250, 2000) 18.4 / 13.2, 111 / 92; 1024 x 1024 of 512 and 1024 (64, 128) 7.4 / 12.0, 10.7 / 11.4.
     const int blocks = (w->tn + kBlockFeatures / 16 - 1) / (kBlockFeatures / 16), row_blocks64 = (c.rows + kBlockRows - 1) / kBlockRows;
-    if (!parts && (int64_t)blocks * row_blocks64 >= 96 && (int64_t)blocks * row_blocks64 <= 1 << 22 && w->k % 8 == 0 && ((uintptr_t)c.x & 15) == 0 && c.x_stride % 8 == 0) {
+    if (!parts && c.rows > kPartRows && (int64_t)blocks * row_blocks64 >= 96 && (int64_t)blocks * row_blocks64 <= 1 << 22 && w->k % 8 == 0 && ((uintptr_t)c.x & 15) == 0 && c.x_stride % 8 == 0) {
         a.nothing = (const uint4*)w->nothing;
         a.per = (blocks + 7) / 8;
         const dim3 grid((unsigned)(8 * a.per * row_blocks64));
