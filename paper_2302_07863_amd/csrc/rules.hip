@@ -47,15 +47,16 @@ __device__ __forceinline__ float apply(float z, unsigned w, const Penalty& p, co
     return z;
 }
 
-// Sums of exponentials are kept as sums of 2^(z log2 e - M), M the whole number above the largest z log2 e: two products and the
-// hardware's exponential a term, and what M takes off is exact.  The low part of log2 e keeps the argument to half a step.
-constexpr float kLog2e = 1.44269502162933349609375f, kLog2eLow = 1.92596299e-8f;
+// Sums of exponentials are kept as sums of 2^(z L - M), L = log2 e as fp32 has it, M the whole number above the largest z L: a product and the hardware's exponential a
+// term, and what M takes off is exact.  In the end the sum is multiplied by 2^(M - m L): a term is e^(z - m) to a factor of 2^((z - m) (L - log2 e)), which for a term of e^-20
+// is off by 2.7e-7 of it.
+constexpr float kLog2e = 1.44269502162933349609375f;
 constexpr float kFar = 1e30f;  // (the type's lowest value as a mask: there a difference of logits is what is left)
 __device__ __forceinline__ float whole_above(float m) { return m == -INFINITY || m == INFINITY ? 0.f : ceilf(m * kLog2e); }
-__device__ __forceinline__ float term(float z, float whole) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2eLow, __builtin_fmaf(z, kLog2e, -whole))); }
+__device__ __forceinline__ float term(float z, float whole) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -whole)); }
 // such a sum as one of e^(z - m)
 __device__ __forceinline__ float to_base(float s, float m) {
-    return !(fabsf(m) < kFar) ? s : s * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, kLog2eLow, __builtin_fmaf(-m, kLog2e, whole_above(m))));
+    return !(fabsf(m) < kFar) ? s : s * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, kLog2e, whole_above(m)));
 }
 
 // Statistics of two sets of ids.  (A sum that is NaN stays NaN beside any other; what lies infinitely far below counts nothing.)

@@ -243,3 +243,33 @@ def test_blocks_keep_to_their_rows(x_dtype):
     xh = unpack(pack(wide[keep_rows, :k], x_dtype), x_dtype)
     want = xh @ w[keep].T
     close(got[keep_rows][:, keep], want, tolerance(xh, s[keep], want, F32))
+
+
+@pytest.mark.parametrize("rows,n,k", [(3, 200, 1000), (500, 1600, 264)])
+def test_one_matrix_on_two_streams_and_in_two_graphs(rows, n, k):
+    """Calls in flight at once on one handle, replayed with other rows: the bits of calls by themselves."""
+    rng = np.random.default_rng(rows)
+    *_, q, w, s = matrix(rng, n, k, 64, True)
+    xs = [[pack(rng.standard_normal((rows, k)), BF16) for _ in range(2)] for _ in range(3)]
+    x, streams = [Rows(v) for v in xs[0]], [Stream(), Stream()]
+    y, alone = [Rows(np.zeros((rows, n), np.float32)) for _ in range(2)], Rows(np.zeros((rows, n), np.float32))
+    graphs = [Graph(st, lambda h, i=i: q.matmul(x[i].ptr, BF16, rows, y[i].ptr, F32, stream=h)) for i, st in enumerate(streams)]
+    for words in xs:
+        for i in range(2):
+            assert hip().hipMemcpy(x[i].dev.ptr, np.ascontiguousarray(words[i]).ctypes.data, words[i].nbytes, 1) == 0
+        for _ in range(3):
+            for g in graphs:
+                g.replay()
+        for st in streams:
+            st.sync()
+        for i in range(2):
+            q.matmul(x[i].ptr, BF16, rows, alone.ptr, F32)
+            assert np.array_equal(y[i].get(), alone.get())
+            want = unpack(words[i], BF16) @ w.T
+            close(alone.get().astype(np.float64), want, tolerance(unpack(words[i], BF16), s, want, F32))
+
+
+@pytest.mark.parametrize("first,more", [(1, 0), (0, 1), (8, 8)])
+def test_blocks_of_rows_at_any_address(first, more):
+    rng = np.random.default_rng(first + more)
+    check(rng, 1600, 520, 128, 510, F16, F16, x_stride=520 + more, first=first)
