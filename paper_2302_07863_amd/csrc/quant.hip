@@ -34,9 +34,7 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTileK = 128;    // inputs of a tile
-constexpr int kMaxWaves = 16;
-// Waves that may share a feature tile: what their registers leave room for.
-constexpr int most_waves(int tiles) { return tiles <= 2 ? kMaxWaves : 8; }
+constexpr int kMaxWaves = 16;  // of a workgroup (with 8 above two row tiles: 22 rows of fp32 by 250112 x 1024 138 us, with 16 108)
 constexpr int kPartRows = 32;  // most rows of a workgroup
 // Tiles that a wave has under way (with a group per step of 32 inputs the scales take two thirds of a tile's registers).
 constexpr int ahead(int group) { return group == 32 ? 3 : 4; }
@@ -63,6 +61,7 @@ struct QuantArgs {
     int per;       // feature tiles of a wave, one after the other (1 where there are several chunks)
     int chunk;     // input tiles staged at a time
     int chunks;
+    unsigned span_m;  // 2^32 / (waves that a row of a chunk's pieces takes), rounded up; 0: one
     int turns;     // of a wave over them (several chunks: a multiple of ahead())
     const uint4* nothing;  // 16 bytes of zeros
     int sums_at;   // where in LDS the sums lie: behind the rows, or (per 1) in their place
@@ -136,8 +135,8 @@ __device__ __forceinline__ void store_y(const QuantArgs& a, int row, int n0, con
 }
 
 // Eight inputs of row r, as they are or times the gain in three parts, to their place in the operand; their squares (with a gain).
-template <class R, bool PARTS>
-__device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&g)[8], bool gain, char* to, int rows, bool real) {
+template <class R, bool PARTS, bool GAIN>
+__device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&g)[8], char* to, int rows, bool real) {
     if constexpr (!PARTS) {
         uint4 q;
         __builtin_memcpy(&q, x.v, 16);
@@ -149,7 +148,7 @@ __device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a = R::up(x.v[2 * j]), b = R::up(x.v[2 * j + 1]);
-            if (gain) {
+            if constexpr (GAIN) {
                 ss = __builtin_fmaf(a, a, __builtin_fmaf(b, b, ss));
                 a *= g[2 * j];
                 b *= g[2 * j + 1];
@@ -168,26 +167,27 @@ __device__ __forceinline__ float put_piece(const RowVec<R, 8>& x, const float (&
 // [step of 32 inputs][row of the operand][4 pieces of 8].  Row v of the operand is part v / rows of row v % rows.  Inputs from the k-th on are zero.
 // A wave's 64 pieces belong to one row; with a norm it adds up their squares.  `between` runs behind the requests of the first U pieces a thread
 // (loads come back in order: what it requests does not keep these waiting).
-template <class R, bool PARTS, int U, class Between>
+template <class R, bool PARTS, bool GAIN, int U, class Between>
 __device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (*squares)[kPartRows], int r0, int rows, int t0, int t1, Between&& between) {
     const int nthr = blockDim.x, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int k0 = t0 * kTileK, pieces = (t1 - t0) * (kTileK / 8), span = (pieces + 63) & ~63;
+    const int k0 = t0 * kTileK, pieces = (t1 - t0) * (kTileK / 8), span = (a.chunk * (kTileK / 8) + 63) & ~63;  // (a row has whole waves)
     const int full = min(max((a.k - k0) / 8, 0), pieces);  // pieces that are there as a whole
     const bool tail = (a.k & 7) != 0 && full < pieces;     // one more is there in part
     const int v = PARTS ? 3 * rows : rows;                 // rows of the operand
-    const bool gain = PARTS && a.gain;
+    // (exact below 2^16 waves; what LDS holds is far less)
+    const auto row_of = [&](int i) { return a.span_m ? (int)__umulhi((unsigned)__builtin_amdgcn_readfirstlane(i >> 6), a.span_m) : __builtin_amdgcn_readfirstlane(i >> 6); };
     const auto place = [&](int p, int r) { return xs + ((size_t)((p >> 2) * v + r) * 4 + (p & 3)) * 16; };
     RowVec<R, 8> x[U];
     float g[U][8];
     const auto load = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * nthr + tid, r = min(__builtin_amdgcn_readfirstlane((i & ~63) / span), rows - 1), p = i - r * span;
+            const int i = i0 + u * nthr + tid, r = min(row_of(i), rows - 1), p = i - r * span;
             __builtin_memset(x[u].v, 0, sizeof(x[u].v));
             if (full > 0) {  // (past the end: a valid address, replaced below)
                 const int k = k0 + min(p, full - 1) * 8;
                 x[u].load((const typename R::type*)a.x + (int64_t)(r0 + r) * a.ldx + k);
-                if (gain) {
+                if constexpr (GAIN) {
                     RowVec<RowF32, 8> t;
                     t.load(a.gain + k);
 #pragma unroll
@@ -199,11 +199,11 @@ __device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (
     const auto put = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * nthr + tid, r = __builtin_amdgcn_readfirstlane((i & ~63) / span), p = i - r * span;
+            const int i = i0 + u * nthr + tid, r = row_of(i), p = i - r * span;
             if (r >= rows) break;
-            if (p >= full) __builtin_memset(x[u].v, 0, sizeof(x[u].v));
-            const float ss = put_piece<R, PARTS>(x[u], g[u], gain, place(p, r), rows, p < pieces && !(tail && p == full));
-            if (gain) {
+            if ((GAIN || full < pieces) && p >= full) __builtin_memset(x[u].v, 0, sizeof(x[u].v));
+            const float ss = put_piece<R, PARTS, GAIN>(x[u], g[u], place(p, r), rows, p < pieces && !(tail && p == full));
+            if constexpr (GAIN) {
                 const float all = wave_sum(ss);
                 if ((tid & 63) == 0) squares[wave][r] += all;
             }
@@ -224,9 +224,9 @@ __device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (
     RowVec<RowF32, 8> h;
     const int n = a.k & 7, k = a.k - n;
     y.load_some((const typename R::type*)a.x + (int64_t)(r0 + tid) * a.ldx + k, n);
-    h.load_some(a.gain ? a.gain + k : nullptr, gain ? n : 0);
-    const float ss = put_piece<R, PARTS>(y, h.v, gain, place(full, tid), rows, true);
-    if (gain) squares[0][tid] += ss;
+    if constexpr (GAIN) h.load_some(a.gain + k, n);
+    const float ss = put_piece<R, PARTS, GAIN>(y, h.v, place(full, tid), rows, true);
+    if constexpr (GAIN) squares[0][tid] += ss;
 }
 
 // What a lane has of its feature besides codes, of the tile's GT groups.
@@ -255,7 +255,7 @@ struct Unit {
 // tiles of codes one behind the other, ahead() of them under way.  Nothing is stored before the last one: stores would be counted among the loads that the waves
 // wait for.  The sums meet in LDS.
 template <int AS, int G, int NT, bool CHUNKED>
-__global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantArgs a) {
+__global__ __launch_bounds__(64 * kMaxWaves) void quant_kernel(const QuantArgs a) {
     constexpr int GT = kTileK / G;  // groups of a tile
     constexpr int SG = G / 32;      // steps of a group
     constexpr int kAhead = ahead(G);
@@ -291,12 +291,13 @@ __global__ __launch_bounds__(64 * most_waves(NT)) void quant_kernel(const QuantA
     const auto stage = [&](int t0, auto&& between) {
         const int t1 = min(t0 + a.chunk, a.tk);
         if constexpr (AS == AS_PARTS) {
-            if (a.x_dtype == BILD_DT_F32) stage_rows<RowF32, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
-            else if (a.x_dtype == BILD_DT_BF16) stage_rows<RowBf16, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
-            else stage_rows<RowF16, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            if (a.x_dtype == BILD_DT_F32 && a.gain) stage_rows<RowF32, true, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            else if (a.x_dtype == BILD_DT_F32) stage_rows<RowF32, true, false, 2>(a, lds, squares, r0, rows, t0, t1, between);
+            else if (a.x_dtype == BILD_DT_BF16) stage_rows<RowBf16, true, true, 1>(a, lds, squares, r0, rows, t0, t1, between);  // (without a gain they are as they are)
+            else stage_rows<RowF16, true, true, 1>(a, lds, squares, r0, rows, t0, t1, between);
         } else {  // (16 bits are 16 bits)
-            if (rows * ((t1 - t0) * (kTileK / 8)) <= (int)blockDim.x) stage_rows<RowBf16, false, 1>(a, lds, squares, r0, rows, t0, t1, between);
-            else stage_rows<RowBf16, false, 4>(a, lds, squares, r0, rows, t0, t1, between);
+            if (rows * ((a.chunk * (kTileK / 8) + 63) & ~63) <= (int)blockDim.x) stage_rows<RowBf16, false, false, 1>(a, lds, squares, r0, rows, t0, t1, between);
+            else stage_rows<RowBf16, false, false, 4>(a, lds, squares, r0, rows, t0, t1, between);
         }
     };
     const CodeBits bits = code_bits<AS>();
@@ -864,7 +865,7 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
     const int v = a.rows_per * (parts ? 3 : 1);
     const int tiles = v <= 16 ? 1 : v <= 32 ? 2 : v <= 48 ? 3 : 6;
     const int row_blocks = (c.rows + a.rows_per - 1) / a.rows_per, tile_bytes = v * kTileK * 2;
-    const int turn = ahead(w->group), most = most_waves(tiles), wave_sums = tiles * 1024;
+    const int turn = ahead(w->group), most = kMaxWaves, wave_sums = tiles * 1024;
     const int room = kLdsLimit - 4096;  // (beside the squares)
     const int units = std::max(1, kChipUnits / row_blocks);
     // How many waves share a feature tile, and how many tiles a workgroup has beside each other (no more than gives one to every compute unit) and one after the other.
@@ -872,18 +873,21 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
     int wf = 1, best = 0;
     for (int wk = 1, l = 0; wk <= most && wk <= w->tk; wk *= 2, ++l) {
         if (!fits && wk * tile_bytes > room) break;  // (of so few input tiles at a time every wave is to have one)
-        const int side = std::min(most / wk, (w->tn + units - 1) / units), waves = side * wk;
-        const int sums_room = fits ? std::max(1, (room - w->tk * tile_bytes) / (waves * wave_sums)) : 1;
-        const int per = std::max(1, std::min((w->tn + units * side - 1) / (units * side), sums_room));
-        const int rounds = (w->tn + units * side * per - 1) / (units * side * per);
-        // clocks of a compute unit: rows at 64 bytes each, a tile as fast as memory brings it or the matrix cores take it, the sums
-        const int cost = rounds * (v * w->k / 32 + per * (10 * ((w->tk + wk - 1) / wk) + 6) * std::max(waves, 12) * std::max(10, 6 * tiles));
-        if (best && cost >= best) continue;
-        best = cost;
-        a.wk = wk;
-        a.lwk = l;
-        a.per = per;
-        wf = side;
+        for (int side = std::min(most / wk, (w->tn + units - 1) / units); side * wk <= most; side *= 2) {
+            const int waves = side * wk, sums_room = fits ? std::max(1, (room - w->tk * tile_bytes) / (waves * wave_sums)) : 1;
+            const int per = std::max(1, std::min((w->tn + units * side - 1) / (units * side), sums_room));
+            const int rounds = (w->tn + units * side * per - 1) / (units * side * per);
+            // clocks of a compute unit: rows at 64 bytes each, or as fast as its waves take them apart, a tile as fast as memory brings it or the matrix cores take it, the sums
+            // (346 x 32 features, one wave each: 32 rows of fp32 16.8 us; several tiles' waves in a workgroup 7.5)
+            const int stage = std::max(v * w->k / 32, a.rows_per * ((w->tk + 3) / 4) * (parts ? 400 : 100) / std::min(waves, 4));
+            const int cost = rounds * (stage + per * (10 * ((w->tk + wk - 1) / wk) + 6) * std::max(waves, 12) * std::max(10, 6 * tiles));
+            if (best && cost >= best) continue;
+            best = cost;
+            a.wk = wk;
+            a.lwk = l;
+            a.per = per;
+            wf = side;
+        }
     }
     const int waves = wf * a.wk;
     // The rows in LDS, all of them or as many input tiles as there is room for, in chunks of equal turns.
@@ -894,6 +898,8 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
         a.chunk = ((w->tk + n - 1) / n + a.wk - 1) / a.wk * a.wk;
     }
     a.chunks = (w->tk + a.chunk - 1) / a.chunk;
+    const unsigned row_waves = (unsigned)(a.chunk * (kTileK / 8) + 63) / 64;
+    a.span_m = row_waves == 1 ? 0u : (unsigned)((0xFFFFFFFFull + row_waves) / row_waves);
     a.turns = (a.chunk + a.wk - 1) / a.wk;
     if (a.chunks > 1) a.turns = (a.turns + turn - 1) / turn * turn;
     a.sums_at = a.per > 1 ? a.chunk * tile_bytes : 0;

@@ -273,3 +273,12 @@ def test_one_matrix_on_two_streams_and_in_two_graphs(rows, n, k):
 def test_blocks_of_rows_at_any_address(first, more):
     rng = np.random.default_rng(first + more)
     check(rng, 1600, 520, 128, 510, F16, F16, x_stride=520 + more, first=first)
+
+
+@pytest.mark.parametrize("x_dtype,norm", [(F32, False), (F32, True), (BF16, True), (F16, False)])
+@pytest.mark.parametrize("rows", [17, 22, 32, 45])
+def test_few_inputs_and_long_ones_for_many_rows(rows, x_dtype, norm):
+    """More waves than tiles of inputs ask for; rows that LDS holds exactly, nearly, in chunks of unequal length."""
+    rng = np.random.default_rng(rows)
+    for n, k, group in ((346, 32, 32), (16, 130, 64), (40, 1536, 128), (33, 6752, 32), (33, 2500, 64)):
+        check(rng, n, k, group, rows, x_dtype, F32, zeros=rows % 2 == 0, norm=norm, mean=0.1)
