@@ -1685,8 +1685,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
         r.part_ld = M.nparts_cap;
         r.zt = M.zt;
         s->stage_count += 1;
-        HIPC(launch_rules(r, s->stream, &f.nparts));
-        if (f.nparts > M.nparts_cap) return BILD_ECAP;  // (a range has 2048 ids at least, a part of the head 16)
+        HIPC(launch_rules(r, s->stream, &f.nparts));  // (at most a part for every 2048 ids: there is room for one for every 16)
     }
     if (lm_rows > 0) {
         f.part = M.part;

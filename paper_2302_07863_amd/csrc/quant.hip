@@ -870,7 +870,8 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
     const int units = std::max(1, kChipUnits / row_blocks);
     // How many waves share a feature tile, and how many tiles a workgroup has beside each other (no more than gives one to every compute unit) and one after the other.
     const bool fits = w->tk * tile_bytes + wave_sums <= room;
-    int wf = 1, best = 0;
+    int wf = 1;
+    int64_t best = 0;
     for (int wk = 1, l = 0; wk <= most && wk <= w->tk; wk *= 2, ++l) {
         if (!fits && wk * tile_bytes > room) break;  // (of so few input tiles at a time every wave is to have one)
         for (int side = std::min(most / wk, (w->tn + units - 1) / units); side * wk <= most; side *= 2) {
@@ -880,7 +881,7 @@ int launch_quant(const bild_quant* w, const bild_quant_call& c, hipStream_t st) 
             // clocks of a compute unit: rows at 64 bytes each, or as fast as its waves take them apart, a tile as fast as memory brings it or the matrix cores take it, the sums
             // (346 x 32 features, one wave each: 32 rows of fp32 16.8 us; several tiles' waves in a workgroup 7.5)
             const int stage = std::max(v * w->k / 32, a.rows_per * ((w->tk + 3) / 4) * (parts ? 400 : 100) / std::min(waves, 4));
-            const int cost = rounds * (stage + per * (10 * ((w->tk + wk - 1) / wk) + 6) * std::max(waves, 12) * std::max(10, 6 * tiles));
+            const int64_t cost = (int64_t)rounds * (stage + per * (10 * ((w->tk + wk - 1) / wk) + 6) * std::max(waves, 12) * std::max(10, 6 * tiles));
             if (best && cost >= best) continue;
             best = cost;
             a.wk = wk;

@@ -6,7 +6,7 @@
 // give every thread one piece of 32 bytes.  A thread requests its piece and, while that is on its way, helps to form the tokens' cosines and sines, in 64 bits (an
 // angle of 100 000 radians has no correct digit after the sixth in fp32), into LDS.
 // us: 4096 tokens of 32 + 32 heads of 128 bf16 (134 MB) pairs 27.4, halves 26.1 (4.9, 5.1 TB/s; a copy of 512 MB reaches 5.4), 94 of 128 turned 34 and 38; 1531
-// tokens of packed fp32 heads of 80, 32 turned, 6.0; one token 2.75.
+// tokens of packed fp32 heads of 80, 32 turned, 6.0; one token 2.75 to 3.1.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -282,3 +282,27 @@ def test_few_inputs_and_long_ones_for_many_rows(rows, x_dtype, norm):
     rng = np.random.default_rng(rows)
     for n, k, group in ((346, 32, 32), (16, 130, 64), (40, 1536, 128), (33, 6752, 32), (33, 2500, 64)):
         check(rng, n, k, group, rows, x_dtype, F32, zeros=rows % 2 == 0, norm=norm, mean=0.1)
+
+
+def test_scales_of_bf16_far_apart():
+    """A factor of 2^32 between the scales fits, with any bits set; what no power of two brings into fp16 is refused."""
+    rng = np.random.default_rng(21)
+    n, k, group = 48, 256, 64
+    codes = rng.integers(0, 256, (n, k // 2)).astype(np.uint8)
+    for top in (2.0 ** 60, 1.0, 2.0 ** -80):
+        values = top * 2.0 ** -rng.integers(0, 33, (n, k // group)).astype(np.float64) * (1 + rng.integers(0, 128, (n, k // group)) / 128.0)
+        values[0, 0], values[1, 1], values[2] = top * 1.9921875, top * 2.0 ** -32 * 1.9921875, 0.0
+        scales = scale_words(values, BF16)
+        q, s = pkg.Quant(n, k, group, codes, scales, BF16), scales_of(scales, BF16)
+        xv = pack(rng.standard_normal((5, k)) / top, F32)
+        x, y = Rows(xv), Rows(np.zeros((5, n), np.float32))
+        q.matmul(x.ptr, F32, 5, y.ptr, F32)
+        xh = unpack(xv, F32)
+        want = xh @ weights(codes, s, None, k, group).T
+        close(y.get().astype(np.float64), want, tolerance(xh, np.abs(s)[:, np.arange(k) // group], want, F32))
+    for least in (2.0 ** -60, 2.0 ** -120):
+        values = np.ones((n, k // group))
+        values[3, 1] = least
+        with pytest.raises(pkg.BildError) as e:
+            pkg.Quant(n, k, group, codes, scale_words(values, BF16), BF16)
+        assert e.value.code == b.EINVAL

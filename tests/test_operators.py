@@ -122,3 +122,10 @@ def test_models_with_rotary_positions_that_are_refused():
     cfg.pos = 0
     assert lib.bild_model_create_rotary(C.byref(cfg), C.byref(good), ptrs, n, C.byref(h)) == b.EINVAL
     assert not h.value
+
+
+def test_a_state_that_is_not_there_takes_no_rules():
+    l = b.lib()
+    assert l.bild_set_quant_head(None, 1, None) == b.EINVAL
+    assert l.bild_set_rules(None, None, None, None, 0) == b.EINVAL
+    assert l.bild_set_masks(None, 0, 1, None) == b.EINVAL
