@@ -48,11 +48,12 @@ __device__ __forceinline__ float apply(float z, unsigned w, const Penalty& p, co
 }
 
 // Sums of exponentials are kept as sums of 2^(z L - M), L = log2 e as fp32 has it, M the whole number above the largest z L: a product and the hardware's exponential a
-// term, and what M takes off is exact.  In the end the sum is multiplied by 2^(M - m L): a term is e^(z - m) to a factor of 2^((z - m) (L - log2 e)), which for a term of e^-20
-// is off by 2.7e-7 of it.
+// term, rounded once, as the product is exact before M is taken off.  In the end the sum is multiplied by 2^(M - m L): a term is e^(z - m) to a factor of 2^((z - m) (L - log2 e)),
+// which for a term of e^-20 is off by 2.7e-7 of it.  M comes from a product that is rounded: of maxima below kFar by a quarter at most, so that no term is above 2^(1/4).
+// (From 4e9 on by more than the exponential's range.)  Beyond kFar, where logits are half an integer apart and more, terms are the exponentials of their differences.
 constexpr float kLog2e = 1.44269502162933349609375f;
-constexpr float kFar = 1e30f;  // (the type's lowest value as a mask: there a difference of logits is what is left)
-__device__ __forceinline__ float whole_above(float m) { return m == -INFINITY || m == INFINITY ? 0.f : ceilf(m * kLog2e); }
+constexpr float kFar = 4194304.f;  // 2^22
+__device__ __forceinline__ float whole_above(float m) { return m == -INFINITY ? 0.f : ceilf(m * kLog2e); }
 __device__ __forceinline__ float term(float z, float whole) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -whole)); }
 // such a sum as one of e^(z - m)
 __device__ __forceinline__ float to_base(float s, float m) {

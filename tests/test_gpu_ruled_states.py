@@ -305,3 +305,20 @@ def test_refusals():
     assert b.lib().bild_set_rules(st.h, None, None, None, 1) == b.EINVAL and b.lib().bild_set_rules(st.h, None, None, None, -1) == b.EINVAL
     assert b.lib().bild_set_rules(st.h, None, np.zeros(1024, np.int32).ctypes.data, np.zeros(1024, np.float32).ctypes.data, 1024) == b.EINVAL
     assert st.generate(R.src, 0.5, 2.0, R.cfg.max_new) == want        # nothing of it counted
+
+
+@pytest.mark.parametrize("fill", [-1e10, -1e20, 1e12])
+def test_biases_of_any_size(fill):
+    """All ids but five moved to one far value, then all of them: a step's probability is that of the ids at the top."""
+    R = Rig(bi.toy_pair(**TOY_VARIANTS["f32-relu-tied"]))
+    vocab = R.cfg.large.vocab
+    st = R.state(R.cfg.max_new, 3)
+    st.set_rules(None, {t: fill for t in range(5, vocab)})
+    st.encode(R.src)
+    st.debug_enable_logits(True)
+    tok, _, prob = st.small_step(0.0)
+    z = st.debug_logits(pkg.SMALL, 0).astype(np.float64)
+    assert tok == int(np.argmax(z)) and abs(prob - 1 / np.sum(np.exp(z - z.max()))) <= 1e-5
+    st.set_rules(None, {t: fill for t in range(vocab)})               # (every logit is the same now)
+    tok, _, prob = st.small_step(0.0)
+    assert np.all(st.debug_logits(pkg.SMALL, 0) == np.float32(fill)) and tok == 0 and abs(prob * vocab - 1) <= 1e-5

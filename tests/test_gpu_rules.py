@@ -303,3 +303,29 @@ def test_refusals():
         with pytest.raises(pkg.BildError) as e:
             pkg.Rules(vocab, rows)
         assert e.value.code == b.EINVAL
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_statistics_of_logits_of_any_size(dtype):
+    """Whole rows, whole ranges of workgroups and every other id at one value of any size, beside ordinary logits."""
+    rng = np.random.default_rng(9)
+    vocab = 9001
+    fills = [s * v for v in (65504.0, 1e6, 3e6, 4.3e6, 1e7, 1e9, 3.1e9, 4.4e9, 1e10, 1e12, 1e15, 1e20, 9e29, 1.1e30, 1e38) for s in (-1.0, 1.0)]
+    z = rng.standard_normal((4 * len(fills), vocab))
+    for i, v in enumerate(fills):
+        z[4 * i], z[4 * i + 1, 2000:8000], z[4 * i + 2, ::2] = v, v, v
+        z[4 * i + 3] = v * (1 + rng.random(vocab) / 16)
+    rules = pkg.Rules(vocab, len(z))
+    for rows in (len(z), 4):                                # (ranges of other lengths)
+        for first in range(0, len(z), rows):
+            call = Call(z[first:first + rows], dtype)
+            call.run(rules)
+            assert call.out.get().tobytes() == call.words.tobytes()
+            st, w = call.stats.to_host(b.ROW_STATS_DTYPE, rows), unpack(call.words, dtype)
+            for i in range(rows):
+                m = np.max(w[i])
+                lse = m + np.log(np.sum(np.exp(w[i] - m)))
+                # as in Call.check, with nothing off before the exponentials but a half step of each argument: below 10 on average, as the sum is of 9001
+                tol = 2.0 ** -22 + (vocab / 256 + 40 + 20) * U32 + 2 * U32 * abs(lse)
+                assert st["zmax"][i] == m and st["argmax"][i] == np.argmax(w[i])
+                assert abs(st["lse"][i] - lse) <= tol, (rows, fills[(first + i) // 4], i % 4, st["lse"][i], lse)
