@@ -445,7 +445,7 @@ int bild_set_quant_head(bild_state* s, int which, const bild_quant* head /* null
 int bild_set_rules(bild_state* s, const bild_penalties* penalties /* nullable */, const int32_t* bias_ids, const float* bias, int n_bias);
 /* Masks for the tokens at positions first .. first + n - 1 of the sequence (0 <= first, first + n <= max_len): bit id % 32 of word id / 32 of a row of ceil(vocab / 32) words
  * says whether the id may stand there.  masks [n][words]: HOST memory, copied; NULL: all ids may.  They hold until changed, also for later requests.  BILD_EINVAL for
- * a row that allows no id.  The first call allocates (max_len + 1) rows of device memory. */
+ * a row that allows no id.  The first call allocates (max_len + 1) rows of device memory.  While no position keeps an id out, passes are those of a state without masks. */
 int bild_set_masks(bild_state* s, int first, int n, const uint32_t* masks);
 
 /* Introspection (host copies of the control block). */

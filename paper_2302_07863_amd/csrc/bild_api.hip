@@ -1679,7 +1679,7 @@ int decoder_pass(bild_state* s, int w, int T, int lm_rows, int mode, int key_hin
             r.bias = s->bias;
             r.max_bias = s->n_bias;
         }
-        r.mask = s->masks;
+        r.mask = s->n_masked > 0 ? s->masks : nullptr;
         r.mask_stride = (c.vocab + 31) / 32;
         r.part = M.part;
         r.part_ld = M.nparts_cap;
@@ -1785,7 +1785,7 @@ int run_pass(bild_state* s, int w, int T, int lm_rows, int mode) {
         return rc;
     }
     const int source = one || s->pair->decoder_only ? 0 : key_bucket(s->n_src);
-    const std::array<int, 7> key = {w, T, lm_rows, mode, bucket, source, (s->debug_logits ? 1 : 0) | (s->gemm_only ? 2 : 0) | (s->top_p > 0.f ? 4 : 0) | (s->accept_mode ? 8 : 0) | (one ? 16 : 0) | (one && two_tiles(s, w, T) ? 32 : 0)};
+    const std::array<int, 7> key = {w, T, lm_rows, mode, bucket, source, (s->debug_logits ? 1 : 0) | (s->gemm_only ? 2 : 0) | (s->top_p > 0.f ? 4 : 0) | (s->accept_mode ? 8 : 0) | (one ? 16 : 0) | (one && two_tiles(s, w, T) ? 32 : 0) | (s->n_masked > 0 ? 64 : 0)};
     auto it = s->graphs.find(key);
     if (it == s->graphs.end()) {
         hipGraph_t g = nullptr;
@@ -2396,21 +2396,32 @@ extern "C" int bild_set_masks(bild_state* s, int first, int n, const uint32_t* m
     if (!s || first < 0 || n < 1 || n > s->max_len - first) return BILD_EINVAL;
     const int vocab = s->ms[1].m->cfg.vocab;
     const size_t words = (size_t)(vocab + 31) / 32;
-    if (masks)
-        for (int r = 0; r < n; ++r) {
-            const uint32_t* row = masks + (size_t)r * words;
-            uint32_t any = 0;
-            for (size_t i = 0; i < words; ++i) any |= i + 1 < words || vocab % 32 == 0 ? row[i] : row[i] & ((1u << vocab % 32) - 1u);
-            if (!any) return BILD_EINVAL;
+    // whether row r keeps an id out, or (negative) all of them
+    const auto keeps_out = [&](int r) {
+        const uint32_t* row = masks + (size_t)r * words;
+        const uint32_t last = vocab % 32 == 0 ? ~0u : (1u << vocab % 32) - 1u;
+        uint32_t any = row[words - 1] & last, missing = ~row[words - 1] & last;
+        for (size_t i = 0; i + 1 < words; ++i) {
+            any |= row[i];
+            missing |= ~row[i];
         }
+        return !any ? -1 : missing ? 1 : 0;
+    };
+    if (masks)
+        for (int r = 0; r < n; ++r)
+            if (keeps_out(r) < 0) return BILD_EINVAL;
     if (!masks && !s->masks) return BILD_OK;
     if (!s->masks) {
         uint32_t* at = nullptr;
         int rc = alloc_logit_buffers(s);
         if (rc == BILD_OK) rc = dev_alloc(s->allocs, (void**)&at, sizeof(uint32_t) * words * (size_t)(s->max_len + 1));
         if (rc) return rc;
+        try {
+            s->masked.assign((size_t)s->max_len + 1, 0);
+        } catch (const std::bad_alloc&) {
+            return BILD_ENOMEM;
+        }
         HIPC(hipMemset(at, 0xFF, sizeof(uint32_t) * words * (size_t)(s->max_len + 1)));
-        drop_graphs(s);
         s->masks = at;
     }
     HIPC(hipStreamSynchronize(s->stream));
@@ -2418,6 +2429,12 @@ extern "C" int bild_set_masks(bild_state* s, int first, int n, const uint32_t* m
     else {
         HIPC(hipMemset(s->masks + (size_t)first * words, 0xFF, sizeof(uint32_t) * words * (size_t)n));
         HIPC(hipStreamSynchronize(nullptr));
+    }
+    // (captured passes with and without masks stand beside each other: see run_pass)
+    for (int r = 0; r < n; ++r) {
+        const char now = masks && keeps_out(r) > 0;
+        s->n_masked += now - s->masked[(size_t)first + r];
+        s->masked[(size_t)first + r] = now;
     }
     return BILD_OK;
 }

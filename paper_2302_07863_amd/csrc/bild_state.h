@@ -292,9 +292,11 @@ struct bild_state {
     int* bias_ids = nullptr;       // [kMaxBiases]
     float* bias = nullptr;
     uint32_t* masks = nullptr;     // [max_len + 1][words of a vocabulary]
+    std::vector<char> masked;      // [max_len + 1] a position whose mask keeps an id out
+    int n_masked = 0;              // how many of them (none: passes take no masks)
     bool has_penalties = false;
     int n_bias = 0;
-    bool ruled() const { return has_penalties || n_bias > 0 || masks != nullptr; }
+    bool ruled() const { return has_penalties || n_bias > 0 || n_masked > 0; }
     float* trunk_x = nullptr;  // early-exit pair: [cap_len][d] hidden state after the trunk's last layer, by position
     int* y = nullptr;     // device [max_len + 1]
     int* src = nullptr;   // device [max_src]

@@ -322,3 +322,42 @@ def test_biases_of_any_size(fill):
     st.set_rules(None, {t: fill for t in range(vocab)})               # (every logit is the same now)
     tok, _, prob = st.small_step(0.0)
     assert np.all(st.debug_logits(pkg.SMALL, 0) == np.float32(fill)) and tok == 0 and abs(prob * vocab - 1) <= 1e-5
+
+
+def test_masks_taken_back_give_the_route_back():
+    """Where no position is restricted any more, passes take the kernels that they took before; where one is, its mask counts."""
+    R = Rig(bi.toy_pair(dtype=bi.DT_BF16, d=256, heads=4, d_head=64, d_ff=512, truncate=True, n_src=20, max_new=40))
+    vocab = R.cfg.large.vocab
+    st = R.state(R.cfg.max_new, 10)
+    st.encode(R.src)
+
+    def step():
+        before, at = st.pass_routes(), len(st.sequence())
+        tok = st.small_step(0.0)[0]
+        now = st.pass_routes()
+        return tok, st.pass_stages(), {k for k in now if now[k] > before[k]}, at
+
+    step()
+    _, stages, route, at = step()
+    want = st.generate(R.src, 0.5, 2.0, R.cfg.max_new)
+    only = np.zeros((1, vocab), bool)
+    for allowed in (17, vocab - 1, 3):
+        st.encode(R.src)
+        first = len(st.sequence())
+        only[:] = False
+        only[0, allowed] = True
+        st.set_masks(first, mask_words(np.repeat(only, 2, axis=0)))
+        tok, masked, *_ = step()
+        assert tok == allowed and masked > stages
+        st.set_masks(first, None, 1)                                  # (the other position is restricted still)
+        tok, masked, *_ = step()
+        assert tok == allowed and masked > stages
+        st.set_masks(first + 1, mask_words(np.ones((1, vocab), bool)))  # (a mask that allows all ids)
+        _, again, taken, _ = step()
+        assert again == stages and taken == route
+        st.set_masks(first, mask_words(only))
+        st.set_masks(0, None, st.max_len)
+        assert st.generate(R.src, 0.5, 2.0, R.cfg.max_new) == want
+        st.encode(R.src)
+        _, again, taken, _ = step()
+        assert again == stages and taken == route
