@@ -184,6 +184,7 @@ __device__ __forceinline__ void stage_rows(const QuantArgs& a, char* xs, float (
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * nthr + tid, r = min(row_of(i), rows - 1), p = i - r * span;
             __builtin_memset(x[u].v, 0, sizeof(x[u].v));
+            if constexpr (GAIN) __builtin_memset(g[u], 0, sizeof(g[u]));  // (times x: zero, also where no piece is there as a whole)
             if (full > 0) {  // (past the end: a valid address, replaced below)
                 const int k = k0 + min(p, full - 1) * 8;
                 x[u].load((const typename R::type*)a.x + (int64_t)(r0 + r) * a.ldx + k);

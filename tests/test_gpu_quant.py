@@ -306,3 +306,12 @@ def test_scales_of_bf16_far_apart():
         with pytest.raises(pkg.BildError) as e:
             pkg.Quant(n, k, group, codes, scale_words(values, BF16), BF16)
         assert e.value.code == b.EINVAL
+
+
+@pytest.mark.parametrize("x_dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,n,ks", [(1, 40, (1, 3, 7)), (5, 300, (1, 7, 9)), (11, 2048, (4097, 4103)), (32, 2048, (1, 7, 1025, 1031, 1537, 1543)), (45, 64, (5, 1025))])
+def test_norm_of_fewer_inputs_than_a_piece(rows, n, ks, x_dtype):
+    """Rows, or their last part in LDS, of one to seven inputs: what is behind them counts nothing."""
+    rng = np.random.default_rng(rows)
+    for k in ks:
+        check(rng, n, k, 64, rows, x_dtype, F32, norm=True, mean=0.1)
