@@ -307,8 +307,8 @@ int bild_quant_create(int n, int k, int group, const uint8_t* codes, const void*
 int bild_quant_destroy(bild_quant* w); /* nothing that uses it may still run */
 
 /* y[r][n] = scale * sum over k of xh[r][k] * w[n][k], xh = x, or with gain x[r][k] * gain[k] / sqrt(mean over k of x[r][k]^2 + eps): the RMSNorm in front of
- * a projection or an LM head.  Products are those of the values themselves (none is rounded on the way, but x * gain to 24 bits), sums are
- * fp32, y is rounded once.  rows >= 1: those of a decoder pass, of a
+ * a projection or an LM head.  Products are those of the values themselves (none is rounded on the way, but x * gain to 24 bits, and what fp32 inputs and x * gain
+ * have below 2^-133), sums are fp32, that of the squares too, y is rounded once.  rows >= 1: those of a decoder pass, of a
  * prompt (16 bits without gain from 96 blocks of 64 rows x 128 features on, if k is a multiple of 8 and rows begin at multiples of 16 bytes, in a kernel made for it). */
 typedef struct bild_quant_call {
     const void* x;      /* [rows][k], row r at x + r * x_stride               */
