@@ -987,9 +987,11 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
                 hipLaunchKernelGGL(quant_range_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 1024)), dim3(256), 0, nullptr, (const uint16_t*)(raw + scales_at), count, at);
                 ok = hipGetLastError() == hipSuccess && hipMemcpy(range, at, sizeof(range), hipMemcpyDeviceToHost) == hipSuccess;
             }
+            // (of the powers of two that do, the one nearest to none: sums of products then stay near the results' size, which fp32 holds)
             if (ok && range[0] >= range[1]) {
-                q->scale_exponent = range[0] - 15;
-                bad = range[1] - q->scale_exponent < -24;
+                const int least = range[0] - 15, most = range[1] + 24;
+                q->scale_exponent = std::max(least, std::min(most, 0));
+                bad = least > most;
             }
         }
         if (ok && !bad) {

@@ -111,3 +111,18 @@ def test_subnormal_inputs(rows, n, k):
             want = 2.0 ** 60 * (xv @ w.T)
             tol = U32 * np.abs(want) + (2.0 ** 60 * 2.0 ** -134 * np.abs(w.T[at[1]]) if x_dtype == F32 else 0.0)
             assert np.all(np.abs(multiply(q, words, x_dtype, n, scale=2.0 ** 60) - want) <= tol), (e, x_dtype)
+
+
+@pytest.mark.parametrize("top", [2.0 ** -125, 2.0 ** -110, 1.0, 2.0 ** 100, 2.0 ** 120])
+@pytest.mark.parametrize("rows,n,k", [(2, 48, 256), (7, 48, 250), (509, 1601, 264)])
+def test_scales_at_the_ends_of_bf16(rows, n, k, top):
+    """One power of two a row, a factor beside the matrix: codes, scales and their sums are exact, the factor's product is rounded once."""
+    rng = np.random.default_rng(rows)
+    q, w = matrix(rng, n, k, 64, True, top * np.array([1.0, -1.59375, 0.0078125 * 1.0078125]), BF16)
+    for x_dtype in (F32, BF16):
+        x = np.zeros((rows, k))
+        x[np.arange(rows), rng.integers(0, k, rows)] = 2.0 ** rng.integers(-6, 0, rows) / top
+        words = pack(x, x_dtype)
+        assert np.array_equal(unpack(words, x_dtype), x)
+        want = float(np.float32(0.7)) * (x @ w.T)
+        assert np.all(np.abs(multiply(q, words, x_dtype, n, scale=0.7) - want) <= 1.001 * U32 * np.abs(want))
