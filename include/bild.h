@@ -296,7 +296,8 @@ typedef struct bild_quant bild_quant; /* the matrix on the device, immutable */
  * input 2j in the low and 2j + 1 in the high half of byte j (an odd k leaves the last half zero); scales [n][groups], groups = ceil(k / group), of type
  * scale_dtype (BILD_DT_F16 or BILD_DT_BF16); zeros [n][groups], one of 0..15 a byte, or NULL.  Without zeros the scale is the group's largest magnitude / 7,
  * with zeros the group's range (widened to hold 0) / 15; codes and zeros are the nearest.  No value moves by more than half a scale, but for what the scale's own rounding adds
- * at the ends of the range.  BILD_EINVAL for a value that is not finite or a scale beyond the type. */
+ * at the ends of the range.  (A scale below what fp16 has becomes its smallest, 2^-24; in bf16 a group whose scale is 2^-134 or less becomes zeros.)  BILD_EINVAL for a value
+ * that is not finite or a scale beyond the type. */
 int bild_quant_round(const float* host_w, int n, int k, int inputs_first, int group, int scale_dtype, uint8_t* host_codes, void* host_scales,
                      uint8_t* host_zeros /* nullable */);
 /* Uploads a matrix given as above.  The arrays may be in host or in device memory (whatever wrote them there has to be done) and are copied.  group is 32, 64 or 128.

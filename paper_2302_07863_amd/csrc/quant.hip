@@ -809,6 +809,7 @@ bool round_feature(const float* w, int64_t step, int k, int group, int dtype, ui
         }
         const float want = zeros ? hi / 15.f - lo / 15.f : std::max(hi, -lo) / 7.f;
         scales[g] = to_scale(want, dtype);
+        if (scales[g] == 0 && want > 0.f && dtype == BILD_DT_F16) scales[g] = 1;  // (a scale of none would lose the group; in bf16 only what fp32 itself has as subnormal numbers)
         const float s = from_scale(scales[g], dtype);
         if (!std::isfinite(s)) return false;
         const auto nearest = [&](float v) { return s > 0.f ? (int)std::max(-32.f, std::min(32.f, std::nearbyint(v / s))) : 0; };

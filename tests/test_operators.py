@@ -6,7 +6,7 @@ import pytest
 
 import paper_2302_07863_amd as pkg
 from paper_2302_07863_amd import binding as b
-from tests.rows import BF16, F16, scales_of, weights
+from tests.rows import BF16, F16, HALF_STEP, TINY, scales_of, weights
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
@@ -129,3 +129,24 @@ def test_a_state_that_is_not_there_takes_no_rules():
     assert l.bild_set_quant_head(None, 1, None) == b.EINVAL
     assert l.bild_set_rules(None, None, None, None, 0) == b.EINVAL
     assert l.bild_set_masks(None, 0, 1, None) == b.EINVAL
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("size", [1e-9, 3e-7, 1e-6, 1e-4, 0.02, 1.0])
+def test_no_value_moves_by_more_than_half_a_scale(size, zeros, dtype):
+    """With zeros and without, down to groups whose scale is the type's smallest or would be none: half a scale, and of 7 (15) steps what the scale was off by."""
+    rng = np.random.default_rng(5)
+    n, k, group = 40, 200, 64
+    w = (size * (rng.standard_normal((n, k)) + (rng.uniform(-3, 3, (n, 1)) if zeros else 0.0))).astype(np.float32)
+    w[:, 64:128] *= 1e-3
+    codes, scales, z = pkg.quant_round(w, group, dtype, zeros)
+    s, g = scales_of(scales, dtype), np.arange(k) // group
+    lo = np.stack([np.minimum(w[:, g == j].min(axis=1), 0) for j in range(g[-1] + 1)], axis=1).astype(np.float64)
+    hi = np.stack([np.maximum(w[:, g == j].max(axis=1), 0) for j in range(g[-1] + 1)], axis=1).astype(np.float64)
+    best, steps = ((hi - lo) / 15, 15) if zeros else (np.maximum(hi, -lo) / 7, 7)
+    short = steps * np.maximum(best - s, 0)                           # (a scale that came out smaller leaves the ends of the range outside)
+    off = np.abs(weights(codes, s, z, k, group) - w)
+    assert np.all(off <= (0.5 * s * (1 + 1e-5) + short)[:, g]), np.max(off / s[:, g])
+    # (rounded to the nearest, near zero to half of the smallest, and never to none)
+    assert np.all(s > 0) and np.all(s <= np.maximum(best * (1 + HALF_STEP[dtype] * 1.001) + TINY[dtype] / 2, TINY[dtype]))
