@@ -248,6 +248,15 @@ def _where(a) -> Optional[int]:
     return a.ctypes.data if isinstance(a, np.ndarray) else a
 
 
+def _sized(a, count: int, itemsize: int, what: str):
+    """A host array in one piece, which has to have what the library reads of it; a device pointer as it is."""
+    if not isinstance(a, np.ndarray):
+        return a
+    if a.size != count or a.itemsize != itemsize:
+        raise BildError(EINVAL, f"{what}, an array of {a.size} x {a.itemsize} bytes for {count} x {itemsize}")
+    return np.ascontiguousarray(a)
+
+
 def quant_round(w: np.ndarray, group: int, scale_dtype: int = DT_F16, zeros: bool = False, inputs_first: bool = False):
     """Rounds an fp32 matrix ([n][k]; inputs_first: [k][n]) to 4 bits; (codes, scales as 16-bit words, zeros or None), see bild.h."""
     a = np.ascontiguousarray(w, dtype=np.float32)
@@ -266,7 +275,8 @@ class Quant:
 
     def __init__(self, n: int, k: int, group: int, codes, scales, scale_dtype: int, zeros=None):
         h = C.c_void_p()
-        codes, scales, zeros = [np.ascontiguousarray(a) if isinstance(a, np.ndarray) else a for a in (codes, scales, zeros)]
+        groups = -(-k // group) if group > 0 else 0
+        codes, scales, zeros = [_sized(a, n * each, size, "bild_quant_create") for a, each, size in ((codes, (k + 1) // 2, 1), (scales, groups, 2), (zeros, groups, 1))]
         _check(lib().bild_quant_create(n, k, group, _where(codes), _where(scales), scale_dtype, _where(zeros), C.byref(h)), "bild_quant_create")
         self.h, self.n, self.k, self._matmul = h, n, k, lib().bild_quant_matmul   # (looked up once: a call is as long as a small kernel)
 
@@ -435,12 +445,14 @@ class State:
 
     def set_quant_head(self, which: int, head: Optional["Quant"]):
         """A 4-bit matrix in place of the LM head of model `which` (None: the model's own)."""
+        if head is not None and not head.h:                          # (closed: not the model's own)
+            raise BildError(EINVAL, "bild_set_quant_head")
         _check(lib().bild_set_quant_head(self.h, which, head.h if head is not None else None), "bild_set_quant_head")
         self._heads = {**getattr(self, "_heads", {}), which: head}   # (borrowed by the state)
 
     def set_rules(self, penalties=None, bias=None):
         """penalties: (repetition, frequency, presence) or None; bias: {id: value} or None."""
-        p = np.asarray(penalties, dtype=np.float32) if penalties is not None else None
+        p = _sized(np.asarray(penalties, dtype=np.float32), 3, 4, "bild_set_rules") if penalties is not None else None
         bias = bias or {}
         ids, values = _i32(list(bias.keys())), np.asarray(list(bias.values()), dtype=np.float32)
         _check(lib().bild_set_rules(self.h, p.ctypes.data if p is not None else None, ids.ctypes.data if len(ids) else None,
@@ -448,8 +460,11 @@ class State:
 
     def set_masks(self, first: int, masks=None, n: int = 0):
         """masks [n][ceil(vocab / 32)] uint32 for the tokens at positions first .. first + n - 1; None: all ids at n positions."""
-        a = np.ascontiguousarray(masks, dtype=np.uint32) if masks is not None else None
-        _check(lib().bild_set_masks(self.h, first, len(a) if a is not None else n, a.ctypes.data if a is not None else None), "bild_set_masks")
+        if masks is not None:
+            masks = np.asarray(masks, dtype=np.uint32)
+            n = masks.shape[0] if masks.ndim == 2 else 1
+            masks = _sized(masks, n * ((self.pair.large.cfg.vocab + 31) // 32), 4, "bild_set_masks")
+        _check(lib().bild_set_masks(self.h, first, n, masks.ctypes.data if masks is not None else None), "bild_set_masks")
 
     def force_tokens(self, first: int, tokens, draft_start: int):
         a = _i32(tokens)

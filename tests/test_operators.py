@@ -150,3 +150,42 @@ def test_no_value_moves_by_more_than_half_a_scale(size, zeros, dtype):
     assert np.all(off <= (0.5 * s * (1 + 1e-5) + short)[:, g]), np.max(off / s[:, g])
     # (rounded to the nearest, near zero to half of the smallest, and never to none)
     assert np.all(s > 0) and np.all(s <= np.maximum(best * (1 + HALF_STEP[dtype] * 1.001) + TINY[dtype] / 2, TINY[dtype]))
+
+
+def test_host_arrays_of_other_sizes_are_refused(monkeypatch):
+    """The library reads as much as the sizes say: an array that has less, or values of another width, does not get there."""
+    good = dict(codes=np.zeros((5, 33), np.uint8), scales=np.zeros((5, 3), np.float16), zeros=np.zeros((5, 3), np.uint8))
+    for kw in (dict(codes=np.zeros((5, 32), np.uint8)), dict(codes=np.zeros((5, 33), np.int32)), dict(scales=np.zeros((5, 2), np.float16)),
+               dict(scales=np.zeros((5, 3), np.float32)), dict(zeros=np.zeros((4, 3), np.uint8)), dict(zeros=np.zeros((5, 3), np.int64)), dict(scales=np.zeros(0, np.uint16))):
+        with pytest.raises(pkg.BildError) as e:
+            pkg.Quant(5, 65, 32, scale_dtype=F16, **{**good, **kw})
+        assert e.value.code == b.EINVAL
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                calls.append((name, args, (C.c_float * 3).from_address(args[1])[:] if name == "bild_set_rules" else None))
+                return b.OK
+            return call if name != "bild_strerror" else lambda code: b""
+
+    class Large:
+        cfg = b.ModelConfig(vocab=100)
+
+    class Closed:
+        h = None
+
+    monkeypatch.setattr(b, "lib", Library)
+    st = pkg.State.__new__(pkg.State)
+    st.pair = type("Pair", (), dict(large=Large))
+    for call in (lambda: st.set_rules((1.0, 0.0)), lambda: st.set_rules((1.0, 0.0, 0.0, 0.0)), lambda: st.set_rules(1.0), lambda: st.set_masks(0, np.ones((2, 3), np.uint32)),
+                 lambda: st.set_masks(0, np.ones((2, 5), np.uint32)), lambda: st.set_masks(0, np.ones(8, np.uint32)), lambda: st.set_quant_head(1, Closed())):
+        with pytest.raises(pkg.BildError) as e:
+            call()
+        assert e.value.code == b.EINVAL and not calls
+    st.set_rules(np.arange(1, 7)[::2])                                # (every other value of an array: in one piece by then)
+    st.set_masks(3, np.ones(4, np.uint32))
+    st.set_masks(3, [[1, 2, 3, 4]] * 2)
+    st.set_masks(3, None, 7)
+    assert calls[0][0] == "bild_set_rules" and calls[0][2] == [1.0, 3.0, 5.0]
+    assert [(name, args[1], args[2]) for name, args, _ in calls[1:]] == [("bild_set_masks", 3, n) for n in (1, 2, 7)]
