@@ -162,30 +162,15 @@ const float* turned_columns(const bild_model* m, const float* w, std::vector<flo
     return to.data();
 }
 
-int model_create(const bild_model_config* cfg, const bild_rotary_config* rotary, const float* const* t, int n_tensors, bild_model** out) {
-    for (int i = 0; i < n_tensors; ++i)
-        if (!t[i]) return BILD_EINVAL;
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return BILD_EHIP;
-    bild_model* m = new (std::nothrow) bild_model();
-    if (!m) return BILD_ENOMEM;
-    if (rotary)
-        if (const int rc = bild_rotary_create(rotary, &m->rotary)) {
-            bild_model_destroy(m);
-            return rc;
-        }
-    m->cfg = *cfg;
-    m->cfg.tie_shift %= cfg->vocab;  // (kernels take the row below vocab with one subtraction)
+// The model's tensors to the device (host memory for the staging may not be had: std::bad_alloc).
+int upload_model(bild_model* m, const float* const* t) {
+    const bild_model_config* cfg = &m->cfg;
     const int d = cfg->d_model, I = m->inner(), F = cfg->d_ff, V = cfg->vocab;
-    int i = 0, rc = BILD_OK;
+    int i = 0;
     std::vector<float> tq, tk;
-#define UP(call)                         \
-    do {                                 \
-        rc = (call);                     \
-        if (rc) {                        \
-            bild_model_destroy(m);       \
-            return rc;                   \
-        }                                \
+#define UP(call)                            \
+    do {                                    \
+        if (const int rc = (call)) return rc; \
     } while (0)
     UP(upload_matrix(m, t[i++], false, V, d, &m->emb));
     if (cfg->tied_head)
@@ -240,6 +225,28 @@ int model_create(const bild_model_config* cfg, const bild_rotary_config* rotary,
         UP(upload_matrix(m, t[i++], true, d, F, &L.wout));
     }
 #undef UP
+    return BILD_OK;
+}
+
+int model_create(const bild_model_config* cfg, const bild_rotary_config* rotary, const float* const* t, int n_tensors, bild_model** out) {
+    for (int i = 0; i < n_tensors; ++i)
+        if (!t[i]) return BILD_EINVAL;
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return BILD_EHIP;
+    bild_model* m = new (std::nothrow) bild_model();
+    if (!m) return BILD_ENOMEM;
+    m->cfg = *cfg;
+    m->cfg.tie_shift %= cfg->vocab;  // (kernels take the row below vocab with one subtraction)
+    int rc = rotary ? bild_rotary_create(rotary, &m->rotary) : BILD_OK;
+    try {
+        if (rc == BILD_OK) rc = upload_model(m, t);
+    } catch (const std::exception&) {  // (nothing may leave a C entry)
+        rc = BILD_ENOMEM;
+    }
+    if (rc != BILD_OK) {
+        bild_model_destroy(m);
+        return rc;
+    }
     *out = m;
     return BILD_OK;
 }

@@ -234,3 +234,26 @@ def test_a_model_made_with_plain_pairs_is_the_ordinary_one():
         state = pkg.State(pkg.Pair(*models), max_src=16, max_len=60)
         out.append(state.generate(list(range(3, 15)), 0.5, 2.0, 30)[0])
     assert out[0] == out[1]
+
+
+def test_a_model_that_host_memory_does_not_hold():
+    """No memory for the staging of a tensor is an error of the call, and the process goes on."""
+    import resource
+    vocab, d = 1 << 17, 1024                                          # (half a gigabyte of embedding, never touched)
+    cfg = b.ModelConfig(n_enc_layers=0, n_dec_layers=1, d_model=d, n_heads=16, d_head=64, d_ff=1024, act=bi.ACT_SWIGLU, pos=bi.POS_ROPE, vocab=vocab, tied_head=1, dtype=0,
+                        cross_attn=0, logit_scale=1.0, embed_scale=1.0, norm_eps=1e-6, rope_base=10000.0)
+    small = np.zeros((d, d), np.float32)
+    tensors = [np.zeros((vocab, d), np.float32)] + [small] * (b.lib().bild_model_num_tensors(cfg) - 1)
+    DeviceArray(np.zeros(1, np.float32))                              # (the runtime is there)
+    now = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+    was = resource.getrlimit(resource.RLIMIT_AS)
+    resource.setrlimit(resource.RLIMIT_AS, (now + (128 << 20), was[1]))
+    try:
+        codes = []
+        for rotary in (None, b.RotaryConfig(1, 64, 0, 0, 10000.0, 1.0, 0, 0, 0)):
+            with pytest.raises(pkg.BildError) as e:
+                pkg.Model(cfg, tensors, rotary)
+            codes.append(e.value.code)
+    finally:
+        resource.setrlimit(resource.RLIMIT_AS, was)
+    assert codes == [b.ENOMEM] * 2
