@@ -335,6 +335,7 @@ int bild_quant_matmul(const bild_quant* w, const bild_quant_call* call, void* hi
  *             in between the mean weighted by (t_i - low) / (high - low)
  *     YARN    f_i below the pair that makes `high` turns in the original context, f_i / factor above the one that makes `low`, a ramp over the
  *             pairs' index in between; cos and sin are multiplied by `magnitude`, 0: 0.1 ln(factor) + 1
+ * A configuration with a frequency above 131072 radians a position (bases far below one) is refused.
  * original, low, high and magnitude are read by the last two alone (magnitude by YARN); low = high = 0 stands for 1 and 4 (BANDS), 1 and 32 (YARN). */
 #define BILD_ROTARY_PAIRS  0
 #define BILD_ROTARY_HALVES 1

@@ -45,7 +45,7 @@ struct RotaryArgs {
 // u / d by a product with m = 2^32 / d rounded up (0: d is 1); exact for u and d below 2^16, since u * (m * d - 2^32) < 2^32.
 __device__ __forceinline__ int divide(int u, unsigned m) { return m ? (int)__umulhi((unsigned)u, m) : u; }
 
-// Cosine and sine in 64 bits, good to some 2^-36 (the results are rounded to fp32): the quarter turn nearest to the angle is taken off in two
+// Cosine and sine in 64 bits, good to some 2^-36 (the results are rounded to fp32), of angles up to 2^48: the quarter turn nearest to the angle is taken off in two
 // steps, each with one rounding, and what is left, at most pi / 4, goes into the Taylor series.  A third of the library's
 // instructions, in a chain that every workgroup waits for.
 __device__ __forceinline__ void turn_of(double angle, double& cs, double& sn) {
@@ -186,7 +186,7 @@ hipError_t launch(const RotaryArgs& a, bool halves, hipStream_t st) {
     return hipGetLastError();
 }
 
-bool config_ok(const bild_rotary_config& c) {
+bool fields_ok(const bild_rotary_config& c) {
     if (c.layout != BILD_ROTARY_PAIRS && c.layout != BILD_ROTARY_HALVES) return false;
     if (c.rot_dim < 2 || c.rot_dim > 2 * kMaxHalf || c.rot_dim % 2) return false;
     if (c.scaling < BILD_ROTARY_NONE || c.scaling > BILD_ROTARY_YARN) return false;
@@ -224,6 +224,15 @@ void frequencies(const bild_rotary_config& c, double* f, double* magnitude) {
         f[i] = c.scaling == BILD_ROTARY_NONE || c.scaling == BILD_ROTARY_BASE ? g : g * keep + g / factor * (1.0 - keep);
     }
     *magnitude = c.scaling != BILD_ROTARY_YARN ? 1.0 : c.magnitude > 0.f ? c.magnitude : 0.1 * std::log(factor) + 1.0;
+}
+
+// (turn_of's reduction: angles up to 2^48, of positions up to 2^31.  Only bases below one have such frequencies.)
+constexpr double kMaxFrequency = 131072.0;
+bool config_ok(const bild_rotary_config& c) {
+    if (!fields_ok(c)) return false;
+    double f[kMaxHalf], magnitude;
+    frequencies(c, f, &magnitude);
+    return std::all_of(f, f + c.rot_dim / 2, [](double v) { return v <= kMaxFrequency; });
 }
 
 bool rows_ok(const bild_rotary_rows& r) { return r.heads >= 0 && r.reserved == 0 && (r.heads == 0 || (r.src && r.dst)); }

@@ -257,3 +257,10 @@ def test_a_model_that_host_memory_does_not_hold():
     finally:
         resource.setrlimit(resource.RLIMIT_AS, was)
     assert codes == [b.ENOMEM] * 2
+
+
+def test_the_largest_angles():
+    """Up to 2^48 radians, where a step of the angle is 2^-5: the same 64-bit product here and there, so that its cosine is the same."""
+    rng = np.random.default_rng(12)
+    for halves in (False, True):
+        run(rng, 4, (2, 1), 64, F32, pkg.Rotary(64, halves, base=6e-6), positions=[(1 << 31) - 1, -(1 << 31), 123456789, 3])

@@ -189,3 +189,15 @@ def test_host_arrays_of_other_sizes_are_refused(monkeypatch):
     st.set_masks(3, None, 7)
     assert calls[0][0] == "bild_set_rules" and calls[0][2] == [1.0, 3.0, 5.0]
     assert [(name, args[1], args[2]) for name, args, _ in calls[1:]] == [("bild_set_masks", 3, n) for n in (1, 2, 7)]
+
+
+@pytest.mark.parametrize("kw", [dict(base=1e-20), dict(base=4e-6), dict(rot_dim=4, base=5e-11), dict(base=1e-12, scaling=1, factor=2.0), dict(base=1e-38, scaling=2, factor=1.5)])
+def test_frequencies_that_no_angle_can_be_formed_of_are_refused(kw):
+    """Angles of 2^48 and more (positions go to 2^31) are beyond what the sines are formed from."""
+    kw = {**dict(rot_dim=64), **kw}
+    for call in (lambda: pkg.Rotary(**kw), lambda: pkg.Rotary(**{**kw, "halves": True})):
+        with pytest.raises(pkg.BildError) as e:
+            call()
+        assert e.value.code == b.EINVAL
+    f, _ = pkg.Rotary(**{**kw, "base": 6e-6}).frequencies() if kw["rot_dim"] == 64 and "scaling" not in kw else pkg.Rotary(4, base=6e-11).frequencies()
+    assert 1e5 < np.max(f) <= 131072
