@@ -309,7 +309,10 @@ int bild_quant_destroy(bild_quant* w); /* nothing that uses it may still run */
 
 /* y[r][n] = scale * sum over k of xh[r][k] * w[n][k], xh = x, or with gain x[r][k] * gain[k] / sqrt(mean over k of x[r][k]^2 + eps): the RMSNorm in front of
  * a projection or an LM head.  Products are those of the values themselves (none is rounded on the way, but x * gain to 24 bits, and what fp32 inputs and x * gain
- * have below 2^-133), sums are fp32, that of the squares too, y is rounded once.  rows >= 1: those of a decoder pass, of a
+ * have below 2^-133), sums are fp32, that of the squares too, y is rounded once.  A row with an infinite input or NaN has no finite result and
+ * leaves the others alone: all NaN, but for fp16 rows of a prompt in blocks, which have the formula's infinities.  Inputs whose sum at twice their size is beyond fp32 may be
+ * taken for infinite; a row whose squares' sum is becomes zeros behind a gain.
+ * rows 1 .. 2097120: those of a decoder pass, of a
  * prompt (16 bits without gain from 96 blocks of 64 rows x 128 features on, if k is a multiple of 8 and rows begin at multiples of 16 bytes, in a kernel made for it). */
 typedef struct bild_quant_call {
     const void* x;      /* [rows][k], row r at x + r * x_stride               */
@@ -395,8 +398,8 @@ int bild_model_create_rotary(const bild_model_config* cfg, const bild_rotary_con
  *   an id with a bias:                           z = z + bias (the entry that stands last, if there are several)
  *   an id whose mask bit is 0:                   z = -infinity, whatever stood there
  * and the statistics of what is left, as bild_head_stats gives them, of the values before they are rounded to the rows' type: zmax, lse, argmax (lowest id among equal maxima; -1 where no id is
- * above -infinity, zmax and lse are -infinity then) and z_target (NaN without targets or for an id outside the vocabulary).  A NaN that the rules leave makes lse NaN, zmax and
- * argmax are those of the numbers; +infinity makes lse +infinity. */
+ * above -infinity, zmax and lse are -infinity then) and z_target (NaN without targets or for an id outside the vocabulary).  +infinity makes lse +infinity; without one a NaN that the
+ * rules leave makes lse NaN, zmax and argmax are those of the numbers. */
 typedef struct bild_penalties {
     float repetition;  /* 1: none */
     float frequency;   /* 0: none */
@@ -429,7 +432,7 @@ typedef struct bild_rules_call {
 typedef struct bild_rules bild_rules; /* device memory for the statistics of rows that several workgroups share */
 /* A handle's calls have to follow each other (one stream, or ordered by the caller): two streams, or two captured graphs, that may
  * run at the same time take a handle each. */
-int bild_rules_create(int vocab, int max_rows, bild_rules** out);
+int bild_rules_create(int vocab /* up to 2^24 */, int max_rows /* up to 65535 */, bild_rules** out);
 int bild_rules_destroy(bild_rules* r);
 int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_stream);
 

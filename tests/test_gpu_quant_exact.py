@@ -126,3 +126,27 @@ def test_scales_at_the_ends_of_bf16(rows, n, k, top):
         assert np.array_equal(unpack(words, x_dtype), x)
         want = float(np.float32(0.7)) * (x @ w.T)
         assert np.all(np.abs(multiply(q, words, x_dtype, n, scale=0.7) - want) <= 1.001 * U32 * np.abs(want))
+
+
+@pytest.mark.parametrize("rows,n,k", SHAPES)
+@pytest.mark.parametrize("x_dtype", [F32, BF16, F16])
+def test_rows_with_an_infinite_input(x_dtype, rows, n, k):
+    """NaN throughout, but for fp16 rows in blocks: there infinity times a code, NaN where that is none."""
+    rng = np.random.default_rng(rows + k)
+    q, w = matrix(rng, n, k, 64, True, [0.5, -0.25])
+    x = rng.integers(-3, 4, (rows, k)).astype(np.float64)
+    bad = np.zeros(rows, bool)
+    bad[rng.integers(0, rows, (rows + 2) // 3)] = True
+    at = rng.integers(0, k, rows)
+    x[bad, at[bad]] = np.inf
+    words = pack(x, x_dtype)
+    blocks = x_dtype == F16 and rows > 32 and k % 8 == 0 and -(-n // 128) * -(-rows // 64) >= 96
+    with np.errstate(invalid="ignore"):
+        far = np.inf * w.T[at[bad]] if blocks else np.full((int(bad.sum()), n), np.nan)
+    got = multiply(q, words, x_dtype, n)
+    assert np.array_equal(got[bad], far, equal_nan=True)
+    assert np.array_equal(got[~bad], x[~bad] @ w.T)
+    if x_dtype == F32:
+        huge = DeviceArray(np.ones(k, np.float32))
+        got = multiply(q, pack(np.where(np.isinf(x), 2.0 ** 70, x), F32), F32, n, gain=huge.ptr.value, eps=1e-6)
+        assert np.all(got[bad] == 0) and np.all(np.isfinite(got))
