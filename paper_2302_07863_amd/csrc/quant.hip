@@ -55,7 +55,7 @@ struct QuantArgs {
     int64_t ldx, ldy;
     int n, k, tn, tk, rows;
     int x_dtype, y_dtype;
-    float eps, scale;  // (the scale with what codes and scales are short of)
+    float eps, scale;  // (the scale with what codes and scales are short of: 16 and the scales' power of two)
     int rows_per;  // rows of a workgroup
     int wk, lwk;   // waves that share a feature tile's inputs (a power of two)
     int per;       // feature tiles of a wave, one after the other (1 where there are several chunks)
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void quant_kernel(const QuantArgs a
                     acc[t][s % CH] = mac<AS>(za, b, acc[t][s % CH]);
                 }
             }
-                        const float scale = u.side.scale(g);
+            const float scale = u.side.scale(g);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
                 acc[s % CH] = mac<AS>(ca, u.x[j], acc[s % CH]);
                 acc[s % CH] = mac<AS>(za, u.x[j], acc[s % CH]);
             }
-                        const float scale = u.w.side.scale(g);
+            const float scale = u.w.side.scale(g);
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -525,7 +525,8 @@ __global__ __launch_bounds__(64 * kDirectWaves) void quant_direct_kernel(const Q
 // 7.  bf16 34 us: it has no subtraction of pairs, so that every product with codes has a second with the zeros.
 constexpr int kBlockRows = 64, kBlockFeatures = 128, kBlockSplit = 4;
 
-// fp16 only: 1024 + q, then less 1024 + z, which is q - z as it is.  (bf16 has no subtraction of pairs: a second product does it, as above.)
+// fp16 only: 1 + q / 16 less 1 + z / 16, which is (q - z) / 16 exactly (the 16 is in QuantArgs::scale, as for the other forms).  (bf16 has no subtraction of pairs: a second
+// product does it, as above.)
 template <int AS>
 __device__ __forceinline__ uint4 codes_less(uint32_t w, const CodeBits& b, uint32_t z) {
     const uint4 q = codes_up<AS>(w, b);
@@ -683,7 +684,7 @@ __global__ __launch_bounds__(512) void quant_block_kernel(const QuantArgs a) {
     }
 }
 
-// What bf16 scales ask of''' the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
+// What bf16 scales ask of the power of two that makes them fp16: the largest exponent, and the lowest bit that is set.
 __global__ __launch_bounds__(256) void quant_range_kernel(const uint16_t* scales, size_t count, int* range) {
     int most = -1024, least = 1024;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
