@@ -27,7 +27,10 @@ namespace bild {
 int dev_alloc(std::vector<void*>& keep, void** p, size_t bytes) {
     void* d = nullptr;
     if (bytes == 0) bytes = 16;
-    if (hipMalloc(&d, bytes) != hipSuccess) return BILD_ENOMEM;
+    if (hipMalloc(&d, bytes) != hipSuccess) {
+        (void)hipGetLastError();  // (told by what is returned: no later launch is to find it)
+        return BILD_ENOMEM;
+    }
     keep.push_back(d);
     *p = d;
     return BILD_OK;

@@ -44,6 +44,17 @@ public:
     OnDevice(const OnDevice&) = delete;
 };
 
+// Launches a kernel and returns that launch's own status (hipGetLastError would also give what an earlier call, the caller's perhaps, has left).
+template <class T>
+struct As {
+    typedef T type;
+};
+template <class... P>
+hipError_t launch_on(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t st, const typename As<P>::type&... a) {
+    void* args[] = {(void*)&a...};
+    return hipLaunchKernel((const void*)kernel, grid, block, args, lds, st);
+}
+
 inline int row_bytes(int dtype) { return dtype == BILD_DT_F32 ? 4 : 2; }
 inline bool row_type(int dtype) { return dtype == BILD_DT_F32 || dtype == BILD_DT_BF16 || dtype == BILD_DT_F16; }
 

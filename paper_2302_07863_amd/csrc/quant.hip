@@ -747,8 +747,7 @@ hipError_t launch_kernel(const QuantArgs& a, dim3 grid, int waves, size_t lds, i
             asked.fetch_or(bit, std::memory_order_relaxed);
         }
     }
-    hipLaunchKernelGGL(KERNEL, grid, dim3(64 * waves), lds, st, a);
-    return hipGetLastError();
+    return launch_on(KERNEL, grid, dim3(64 * waves), lds, st, a);
 }
 template <int AS, int G>
 hipError_t launch_rows(const QuantArgs& a, int tiles, dim3 grid, int waves, size_t lds, int device, hipStream_t st) {
@@ -773,18 +772,12 @@ hipError_t launch_group(const QuantArgs& a, int group, int tiles, dim3 grid, int
 template <int AS>
 hipError_t launch_direct(const QuantArgs& a, int group, hipStream_t st) {
     const dim3 grid(a.tn), block(64 * a.wk);
-    if (group == 32) hipLaunchKernelGGL((quant_direct_kernel<AS, 32>), grid, block, 0, st, a);
-    else if (group == 64) hipLaunchKernelGGL((quant_direct_kernel<AS, 64>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((quant_direct_kernel<AS, 128>), grid, block, 0, st, a);
-    return hipGetLastError();
+    return launch_on(group == 32 ? quant_direct_kernel<AS, 32> : group == 64 ? quant_direct_kernel<AS, 64> : quant_direct_kernel<AS, 128>, grid, block, 0, st, a);
 }
 
 template <int AS>
 hipError_t launch_block(const QuantArgs& a, int group, dim3 grid, hipStream_t st) {
-    if (group == 32) hipLaunchKernelGGL((quant_block_kernel<AS, 32>), grid, dim3(512), 0, st, a);
-    else if (group == 64) hipLaunchKernelGGL((quant_block_kernel<AS, 64>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((quant_block_kernel<AS, 128>), grid, dim3(512), 0, st, a);
-    return hipGetLastError();
+    return launch_on(group == 32 ? quant_block_kernel<AS, 32> : group == 64 ? quant_block_kernel<AS, 64> : quant_block_kernel<AS, 128>, grid, dim3(512), 0, st, a);
 }
 
 bool shape_ok(int n, int k, int group) { return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 20) && (group == 32 || group == 64 || group == 128); }
@@ -986,8 +979,8 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
             ok = hipMemcpy(at, range, sizeof(range), hipMemcpyHostToDevice) == hipSuccess;
             if (ok) {
                 const size_t count = (size_t)n * groups;
-                hipLaunchKernelGGL(quant_range_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 1024)), dim3(256), 0, nullptr, (const uint16_t*)(raw + scales_at), count, at);
-                ok = hipGetLastError() == hipSuccess && hipMemcpy(range, at, sizeof(range), hipMemcpyDeviceToHost) == hipSuccess;
+                ok = launch_on(quant_range_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 1024)), dim3(256), 0, nullptr, (const uint16_t*)(raw + scales_at), count, at) == hipSuccess &&
+                     hipMemcpy(range, at, sizeof(range), hipMemcpyDeviceToHost) == hipSuccess;
             }
             // (of the powers of two that do, the one nearest to none: sums of products then stay near the results' size, which fp32 holds)
             if (ok && range[0] >= range[1]) {
@@ -997,15 +990,15 @@ extern "C" int bild_quant_create(int n, int k, int group, const uint8_t* codes, 
             }
         }
         if (ok && !bad) {
-            hipLaunchKernelGGL(quant_layout_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, nullptr, (const uint8_t*)raw, (const uint16_t*)(raw + scales_at),
-                               zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, -q->scale_exponent, bf16, (uint32_t*)q->codes, (uint32_t*)q->sides,
-                               (unsigned*)(raw + bad_at));
-            ok = hipGetLastError() == hipSuccess && hipMemcpy(&bad, raw + bad_at, sizeof(bad), hipMemcpyDeviceToHost) == hipSuccess;
+            ok = launch_on(quant_layout_kernel, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, nullptr, (const uint8_t*)raw, (const uint16_t*)(raw + scales_at),
+                           zeros ? (const uint8_t*)(raw + zeros_at) : nullptr, n, k, group, q->tk, lanes, -q->scale_exponent, bf16, (uint32_t*)q->codes, (uint32_t*)q->sides,
+                           (unsigned*)(raw + bad_at)) == hipSuccess && hipMemcpy(&bad, raw + bad_at, sizeof(bad), hipMemcpyDeviceToHost) == hipSuccess;
         }
         rc = !ok ? BILD_EHIP : bad ? BILD_EINVAL : BILD_OK;
     }
     if (raw) (void)hipFree(raw);
     if (rc != BILD_OK) {
+        (void)hipGetLastError();  // (told by rc: not to be found by a later call as well)
         (void)bild_quant_destroy(q);
         return rc;
     }

@@ -181,9 +181,7 @@ __global__ __launch_bounds__(64) void rotary_table_kernel(double2* table, int pa
 template <class R>
 hipError_t launch(const RotaryArgs& a, bool halves, hipStream_t st) {
     const dim3 grid((a.tokens + a.tokens_per - 1) / a.tokens_per, (a.heads + a.heads_per - 1) / a.heads_per);
-    if (halves) hipLaunchKernelGGL((rotary_kernel<R, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((rotary_kernel<R, false>), grid, dim3(kThreads), 0, st, a);
-    return hipGetLastError();
+    return launch_on(halves ? rotary_kernel<R, true> : rotary_kernel<R, false>, grid, dim3(kThreads), 0, st, a);
 }
 
 bool fields_ok(const bild_rotary_config& c) {
@@ -243,8 +241,7 @@ namespace bild {
 
 hipError_t launch_rotary_table(double2* table, int positions, int d_head, const bild_rotary& r, hipStream_t st) {
     if (!table || positions < 1 || r.cfg.rot_dim > d_head) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(rotary_table_kernel, dim3(positions), dim3(64), 0, st, table, d_head / 2, r);
-    return hipGetLastError();
+    return launch_on(rotary_table_kernel, dim3(positions), dim3(64), 0, st, table, d_head / 2, r);
 }
 
 }  // namespace bild

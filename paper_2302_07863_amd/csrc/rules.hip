@@ -330,10 +330,8 @@ int parts_of(int rows, int vocab) {
     return std::max(least, std::min(most, (2048 + rows - 1) / rows));
 }
 template <class R>
-void launch(const RulesArgs& a, size_t lds, hipStream_t st) {
-    const dim3 grid(a.parts, a.rows), block(kThreads);
-    if (a.range <= kThreads * 8) hipLaunchKernelGGL((rules_kernel<R, 8>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((rules_kernel<R, 16>), grid, block, lds, st, a);
+hipError_t launch(const RulesArgs& a, size_t lds, hipStream_t st) {
+    return launch_on(a.range <= kThreads * 8 ? rules_kernel<R, 8> : rules_kernel<R, 16>, dim3(a.parts, a.rows), dim3(kThreads), lds, st, a);
 }
 size_t parts_cap(int max_rows, int vocab) { return (size_t)max_rows * ((vocab + kMaxRange - 1) / kMaxRange) + 2048 + max_rows; }
 
@@ -354,10 +352,7 @@ hipError_t launch_rules(RulesArgs a, hipStream_t st, int* parts) {
     a.parts = (a.vocab + a.range - 1) / a.range;
     if (parts) *parts = a.parts;
     const size_t lds = a.tokens || a.bias_ids ? sizeof(unsigned) * ((size_t)a.range + (a.bias_ids ? a.max_bias : 0)) : 0;
-    if (a.dtype == BILD_DT_F32) launch<RowF32>(a, lds, st);
-    else if (a.dtype == BILD_DT_BF16) launch<RowBf16>(a, lds, st);
-    else launch<RowF16>(a, lds, st);
-    return hipGetLastError();
+    return a.dtype == BILD_DT_F32 ? launch<RowF32>(a, lds, st) : a.dtype == BILD_DT_BF16 ? launch<RowBf16>(a, lds, st) : launch<RowF16>(a, lds, st);
 }
 
 }  // namespace bild
@@ -374,6 +369,7 @@ extern "C" int bild_rules_create(int vocab, int max_rows, bild_rules** out) {
     else if (hipMalloc(&r->mem, counts + sizeof(StatPart) * parts_cap(max_rows, vocab)) != hipSuccess) r->mem = nullptr, rc = BILD_ENOMEM;
     else if (hipMemset(r->mem, 0, counts) != hipSuccess || hipStreamSynchronize(nullptr) != hipSuccess) rc = BILD_EHIP;
     if (rc != BILD_OK) {
+        (void)hipGetLastError();  // (told by rc: not to be found by a later call as well)
         (void)bild_rules_destroy(r);
         return rc;
     }

@@ -238,7 +238,9 @@ def test_a_model_made_with_plain_pairs_is_the_ordinary_one():
 
 def test_a_model_that_host_memory_does_not_hold():
     """No memory for the staging of a tensor is an error of the call, and the process goes on."""
+    import gc
     import resource
+    gc.collect()                                                      # (what is freed later would make room)
     vocab, d = 1 << 17, 1024                                          # (half a gigabyte of embedding, never touched)
     cfg = b.ModelConfig(n_enc_layers=0, n_dec_layers=1, d_model=d, n_heads=16, d_head=64, d_ff=1024, act=bi.ACT_SWIGLU, pos=bi.POS_ROPE, vocab=vocab, tied_head=1, dtype=0,
                         cross_attn=0, logit_scale=1.0, embed_scale=1.0, norm_eps=1e-6, rope_base=10000.0)

@@ -104,3 +104,42 @@ def test_a_step(rows, dtype):
             lse = np.log(np.sum(np.exp(got[r] - np.max(got[r])))) + np.max(got[r])
             assert abs(st["lse"][r] - lse) <= 1e-5 + 2 * U32 * abs(lse)
             assert st["z_target"][r] == got[r][tgt[r]]
+
+
+def test_errors_of_other_calls_are_not_theirs():
+    """A refused allocation, the caller's or one of the library's own that has told of it, is not reported again by the calls behind it."""
+    import ctypes as C
+    import bild_inputs as bi
+    from tests.test_gpu_parity import Rig, TOY_VARIANTS
+    rng = np.random.default_rng(3)
+    R = Rig(bi.toy_pair(**TOY_VARIANTS["f32-relu-tied"]))
+    st = R.state(R.cfg.max_new, 3)
+    st.encode(R.src)
+    x, y, z = (Rows(pack(rng.standard_normal((120, n)), BF16)) for n in (264, 12300, 264))
+    rules, rotary, stats = pkg.Rules(264, 120), pkg.Rotary(24), DeviceArray(nbytes=120 * 16)
+
+    def callers():
+        p = C.c_void_p()
+        assert hip().hipMalloc(C.byref(p), C.c_size_t(1 << 50)) != 0
+
+    def librarys():
+        with pytest.raises(pkg.BildError) as e:
+            pkg.Quant(1 << 24, 1 << 20, 32, x.ptr, x.ptr, F16)        # (8 TB: nothing is read before there is room for it)
+        assert e.value.code == b.ENOMEM
+
+    def steps():
+        st.small_step(0.0)
+        st.set_rules((1.2, 0.0, 0.0))
+        st.small_step(0.0)
+        st.set_rules()
+
+    for fail in (callers, librarys):
+        calls = [lambda: matrix(rng, 40, 264, 32, True), lambda: pkg.Quant(4, 32, 32, np.zeros((4, 16), np.uint8), np.full((4, 1), 0x3F80, np.uint16), BF16),
+                 lambda: rules.apply(z.ptr, BF16, 120, out=z.ptr, stats=stats.ptr.value),
+                 lambda: rotary.apply(24, BF16, 120, pkg.RotaryRows(z.ptr, z.ptr, 11, 264, 24, 264, 24))]
+        for n, rows in ((40, 3), (12300, 3), (12300, 120), (40, 120)):
+            q = matrix(rng, n, 264, 32, True)[0]
+            calls.append(lambda q=q, rows=rows: q.matmul(x.ptr, BF16, rows, y.ptr, BF16))
+        for call in calls + ([steps] if fail is librarys else []):
+            fail()
+            call()
