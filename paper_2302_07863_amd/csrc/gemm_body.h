@@ -590,7 +590,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& a, const int vblock, c
                 hook(false);
                 row(0, noop);
             }
-            for (int j = 1; j < 8; ++j) {
+            for (int j = 1; j < 8; ++j) {  // (several rows are launched with four waves at least)
                 if ((few ? j : wave + NWV * j) >= T) break;  // wave-uniform
                 row(j, noop);
             }

@@ -190,7 +190,8 @@ void gemm_pick_shape(GemmArgs& a, int dtype) {
         while (wr > 1 && ((a.W.tn + wr * a.rw - 1) / (wr * a.rw)) * row_blocks < 256) wr /= 2;
         a.wk = 8 / wr;
         while (a.wk > 1 && a.wk > tiles_chunk) a.wk /= 2;  // (a power of two: the kernels cut the wave index by shifts)
-        a.nwv = a.wk * wr;
+        // (with rows of no whole number of wavefront-wide pieces a wave stages at most eight of the block's 32: four waves, also where there are fewer than four input tiles)
+        a.nwv = a.wk * std::max(wr, 4 / a.wk);
         return;
     }
     // feature groups: as many as keep >= 512 workgroups; at least 4 waves per workgroup, 8 once a thread of a 4-wave

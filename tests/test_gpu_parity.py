@@ -833,3 +833,16 @@ def test_verify_stress_7b_widths_cache_of_4096_rows():
         assert st.lengths()["len_large"] == cut
         cache.truncate(cut)
     print("verify stress: worst logit error", worst, "bar", tol, flush=True)
+
+
+@pytest.mark.parametrize("shape", [dict(), dict(d=32, heads=1, d_head=32, d_ff=32), dict(d=64, heads=1, d_head=32, d_ff=32), dict(d=96, heads=2, d_head=16, d_ff=64)])
+@pytest.mark.parametrize("kind", ["deconly", "encoder", "deconly-relative"])
+@pytest.mark.parametrize("n_src", [33, 34, 50, 65, 200])
+def test_narrow_f32_models_over_many_rows(kind, shape, n_src):
+    """Prompts and sources of more than 32 rows through projections of two or three input tiles."""
+    more = dict(cross=True) if kind == "encoder" else dict(cross=False, tied=False, act=bi.ACT_SWIGLU, pos=bi.POS_RELATIVE if kind != "deconly" else bi.POS_ROPE)
+    R = Rig(bi.toy_pair(**{**more, **shape, "n_src": n_src, "max_new": 12}))
+    ref = oracle.bild_generate(R.req, 0.5, 2.0, 5, R.cfg.max_new, keep_logits=True)
+    st = R.state(R.cfg.max_new, 5)
+    st.encode(R.src)
+    parity.teacher_forced(st, ref, R.n0, 0.5, 2.0, R.cfg)
