@@ -436,6 +436,134 @@ int bild_rules_create(int vocab /* up to 2^24 */, int max_rows /* up to 65535 */
 int bild_rules_destroy(bild_rules* r);
 int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_stream);
 
+/* ---- a cache of keys and values in 8 bits, in pages ----
+ * For callers with sequences of their own (batches, beams, drafts): keys and values of any number of sequences in one pool of pages that sequences may share.
+ * A page holds page_tokens consecutive positions of a sequence: for each layer, keys and values and each key head their codes in one piece, and a scale, the
+ * value that code 127 stands for: code c is c * scale / 127.  The arrays are DEVICE memory of the caller, who may read them, save them and bring them back, and has to keep them
+ * where they are while the handle lives.  An empty cache has lengths and refs of 0 and -1 throughout the table; of a page that no sequence holds, codes and scales are not read.
+ * Entries of the table that are no page's number count as none, also where a row would see them; lengths are limited to 0 .. max_pages * page_tokens.
+ * Sequences are grown, cut, forked and freed on the device, by numbers that a device array may hold (a beam's parents), so none of these calls waits, and all may be
+ * captured.  Wherever a call has `sequences`, entries outside 0 .. sequences - 1 are passed over, and none may stand twice.  A handle's calls have to follow each other
+ * (one stream, or ordered by the caller). */
+typedef struct bild_cache_config {
+    int8_t* codes;       /* [pages][layers][2: keys, values][heads][page_tokens][d_head], 16-byte aligned */
+    float* scales;       /* [pages][layers][2][heads]                                            */
+    int32_t* table;      /* [sequences][max_pages]: the page of each page_tokens positions, -1: none */
+    int32_t* lengths;    /* [sequences]                                                          */
+    int32_t* refs;       /* [pages]: how many entries of the table name the page; 0: it is free  */
+    int32_t pages;       /* 1 .. 2^24                                                            */
+    int32_t page_tokens; /* 32, 64 or 128                                                        */
+    int32_t layers;      /* 1 .. 1024                                                            */
+    int32_t heads;       /* key heads, 1 .. 1024                                                 */
+    int32_t d_head;      /* a multiple of 8, 16 .. 256                                           */
+    int32_t sequences;   /* 1 .. 65535                                                           */
+    int32_t max_pages;   /* of a sequence; max_pages * page_tokens <= 2^30, sequences * max_pages <= 2^28 */
+    int32_t reserved;    /* 0                                                                    */
+} bild_cache_config;
+typedef struct bild_cache bild_cache; /* the geometry, and device memory for what the calls' kernels hand on */
+int bild_cache_create(const bild_cache_config* cfg, bild_cache** out);
+int bild_cache_destroy(bild_cache* c); /* nothing that uses it may still run */
+
+/* Cuts and grows sequences.  First each is cut to `cut` positions (where that is less than it has) and gives back the pages behind; with a window, so it does with the pages that no row from
+ * the cut on sees (bild_cache_attend; a later cut must not reach behind those).  Then each gets room for its new rows: free pages, lowest number first, in the order of the list; where new
+ * rows would go into a page that others hold too, a copy of its positions below the cut (the last in the list keeps the page, if nobody else is left on it).  Either all sequences
+ * grow or, if the pages are not enough, a sequence would become longer than max_pages, or one has no page where it was cut, none does; until the next call bild_cache_append then writes nothing. */
+typedef struct bild_cache_extend_call {
+    const int32_t* sequences; /* [n], nullable: 0 .. n - 1                                       */
+    const int32_t* cut;       /* [n], nullable: nothing is cut                                   */
+    const int32_t* starts;    /* [n + 1], nullable: sequence i gets starts[i + 1] - starts[i] rows; else `rows` each */
+    int32_t* granted;         /* nullable: 1 if the sequences have grown, else 0                 */
+    int32_t n;                /* 1 .. sequences                                                  */
+    int32_t rows;             /* >= 0                                                            */
+    int32_t window;           /* 0: none                                                         */
+    int32_t sinks;
+} bild_cache_extend_call;
+int bild_cache_extend(bild_cache* c, const bild_cache_extend_call* call, void* hip_stream);
+
+/* Entry i of the list becomes a copy of entry parents[i] of its group (of `group` consecutive entries, 0: all n), all at the same time and sharing pages; a parent that is not in 0 .. group - 1: empty. */
+int bild_cache_fork(bild_cache* c, const int32_t* sequences /* [n], nullable */, const int32_t* parents, int n, int group, void* hip_stream);
+
+/* Moves pages so that those in use are the lowest: the i-th free page among them takes what the i-th page behind them held (of all layers), and the tables follow.  used (device memory,
+ * nullable): how many there are. */
+int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream);
+
+/* Writes keys and values of one layer for the last rows of each sequence, which bild_cache_extend has made room for.  A page's scale becomes the largest magnitude among its positions, of which
+ * those that were there are rounded once more if it grows: codes are the nearest to 127 x / scale (fp32), with scale, the products and quotients in fp32.  Values beyond 2^120 are limited to it, NaN counts as 0.
+ * Pages that several sequences hold are not written. */
+typedef struct bild_cache_append_call {
+    const void* k;            /* head h of row t at k + t * k_token + h * k_head, its d_head values side by side */
+    const void* v;
+    int64_t k_token, k_head, v_token, v_head;
+    const int32_t* sequences; /* [n], nullable: 0 .. n - 1                                        */
+    const int32_t* starts;    /* [n + 1], nullable: sequence i has the rows starts[i] .. starts[i + 1] - 1; else i * rows .. (i + 1) * rows - 1 */
+    int32_t n;
+    int32_t rows;             /* of a sequence; with starts: the most that one is expected to have (a choice of kernels goes by it) */
+    int32_t tokens;           /* with starts: rows in all; rows behind are not touched            */
+    int32_t layer;
+    int32_t dtype;
+    int32_t reserved;         /* 0 */
+} bild_cache_append_call;
+int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* hip_stream);
+
+/* Attention of one layer: row t of sequence i stands at position length - (rows of i) + its place among them and sees the keys j up to its own position, with a window those with j > position - window
+ * and the first `sinks`; without `causal` all of the sequence (window 0 then).
+ *   out[t][h] = sum over j of p_j v_j,  p = softmax of scale * q[t][h] k_j,  lse = ln of the sum of e^(scale * q k_j)
+ * Query head h has the key head h / (heads / key heads).  A row that sees nothing: out 0, lse -infinity.  Products are those of q as fp16, times a power of two that puts the largest of its row below 2^15
+ * (fp32: two fp16 parts), with the codes themselves; weights of the values are fp16 (fp32 rows: two parts); sums are fp32; out is rounded once.  A row whose q has an infinity or NaN, or
+ * whose products go beyond fp32, has no finite result and leaves the others alone. */
+typedef struct bild_cache_attend_call {
+    const void* q;            /* head h of row t at q + t * q_token + h * q_head                  */
+    void* out;
+    float* lse;               /* [tokens][heads], nullable                                        */
+    int64_t q_token, q_head, out_token, out_head;
+    const int32_t* sequences; /* as above                                                         */
+    const int32_t* starts;
+    int32_t n;
+    int32_t rows;
+    int32_t tokens;           /* as above; n * rows or `tokens` times heads is below 2^31         */
+    int32_t layer;
+    int32_t heads;            /* of q: a multiple of the cache's, up to 64 times as many          */
+    int32_t dtype;            /* of q and out                                                     */
+    float scale;
+    int32_t window;           /* 0: none                                                          */
+    int32_t sinks;
+    int32_t causal;
+} bild_cache_attend_call;
+int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* call, void* hip_stream);
+
+/* ---- beams ----
+ * The best continuations of each of `batch` groups of `beams` rows.  A beam that has not ended goes on with any id v: its sum is scores + logit - lse of its row (lse in fp32, sums in 64 bits from there),
+ * its length one more.  One that has ended goes on with `pad` alone, sum and length unchanged.  The `choices` best by sum / max(length, 1)^penalty come out in that order, of equals the lower beam and id first.  Beams
+ * whose score is -infinity or NaN, rows without finite lse and ids of logit -infinity offer nothing; choices that nobody offers: parent and token -1, score -infinity, length 0, ended. */
+typedef struct bild_beams_call {
+    const void* logits;        /* [batch * beams][vocab]                                          */
+    int64_t logits_stride;
+    const float* scores;       /* [batch * beams]                                                 */
+    const int32_t* lengths;    /* [batch * beams], nullable: 0                                    */
+    const int32_t* finished;   /* [batch * beams], nullable: none has ended                       */
+    float* out_scores;         /* [batch * choices], rounded to fp32                              */
+    int32_t* out_parents;      /* beams of the group, 0 .. beams - 1                              */
+    int32_t* out_tokens;
+    int32_t* out_lengths;      /* nullable                                                        */
+    int32_t* out_finished;     /* nullable: 1 if the parent had ended or the token is eos         */
+    const int32_t* history;    /* nullable: the `steps` tokens of each beam so far                */
+    int64_t history_stride;
+    int32_t* out_history;      /* with history: those of the parents and the new token behind (-1 throughout where nobody offers) */
+    int64_t out_history_stride;
+    int32_t batch;
+    int32_t choices;           /* 1 .. 64                                                         */
+    int32_t dtype;
+    int32_t eos;               /* -1: none                                                        */
+    int32_t pad;
+    int32_t steps;
+    float penalty;             /* 0: by sums                                                      */
+    int32_t reserved;          /* 0 */
+} bild_beams_call;
+typedef struct bild_beams bild_beams; /* device memory for the statistics of rows that several workgroups share */
+int bild_beams_create(int vocab /* up to 2^24 */, int max_batch, int beams /* 1 .. 64; max_batch * beams up to 65535 */, bild_beams** out);
+int bild_beams_destroy(bild_beams* b);
+int bild_beams_select(bild_beams* b, const bild_beams_call* call, void* hip_stream);
+
 /* ---- the operators inside a state's passes ----
  * The LM head of model `which` (1 small, 2 large) of this state's passes becomes `head` (n = vocab, k = d_model, else BILD_EINVAL), behind the model's final
  * norm and times its logit scale; NULL: the model's own again.  Everything that is read off the logits (policies, draws, acceptance) follows.  The matrix is

@@ -83,10 +83,44 @@ class RulesCall(C.Structure):
                 ("rows", C.c_int32), ("dtype", C.c_int32), ("max_tokens", C.c_int32), ("max_bias", C.c_int32)]
 
 
+class CacheConfig(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales", "table", "lengths", "refs")] + [
+        (n, C.c_int32) for n in ("pages", "page_tokens", "layers", "heads", "d_head", "sequences", "max_pages", "reserved")]
+
+
+class CacheExtendCall(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("sequences", "cut", "starts", "granted")] + [(n, C.c_int32) for n in ("n", "rows", "window", "sinks")]
+
+
+class CacheAppendCall(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64),
+                ("sequences", C.c_void_p), ("starts", C.c_void_p)] + [(n, C.c_int32) for n in ("n", "rows", "tokens", "layer", "dtype", "reserved")]
+
+
+class CacheAttendCall(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_token", C.c_int64), ("q_head", C.c_int64), ("out_token", C.c_int64),
+                ("out_head", C.c_int64), ("sequences", C.c_void_p), ("starts", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("n", "rows", "tokens", "layer", "heads", "dtype")] + [("scale", C.c_float)] + [
+        (n, C.c_int32) for n in ("window", "sinks", "causal")]
+
+
+class BeamsCall(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_stride", C.c_int64)] + [(n, C.c_void_p) for n in (
+        "scores", "lengths", "finished", "out_scores", "out_parents", "out_tokens", "out_lengths", "out_finished", "history")] + [
+        ("history_stride", C.c_int64), ("out_history", C.c_void_p), ("out_history_stride", C.c_int64)] + [
+        (n, C.c_int32) for n in ("batch", "choices", "dtype", "eos", "pad", "steps")] + [("penalty", C.c_float), ("reserved", C.c_int32)]
+
+
 # The calls' structs as bytes: one packing costs less than setting a ctypes structure field by field.
 _QUANT_CALL = struct.Struct("@PqPqPiiiff4x")
 _ROTARY_CALL = struct.Struct("@PPqqqqiiPPqqqqiiPiiiiii")
 _RULES_CALL = struct.Struct("@PqPqPPPqPPPqPPqPPqiiii")
+_EXTEND_CALL = struct.Struct("@PPPPiiii")
+_APPEND_CALL = struct.Struct("@PPqqqqPPiiiiii")
+_ATTEND_CALL = struct.Struct("@PPPqqqqPPiiiiiifiii")
+_BEAMS_CALL = struct.Struct("@PqPPPPPPPPPqPqiiiiiifi")
+assert _EXTEND_CALL.size == C.sizeof(CacheExtendCall) and _APPEND_CALL.size == C.sizeof(CacheAppendCall) and _ATTEND_CALL.size == C.sizeof(CacheAttendCall)
+assert _BEAMS_CALL.size == C.sizeof(BeamsCall)
 assert _QUANT_CALL.size == C.sizeof(QuantCall) and _ROTARY_CALL.size == C.sizeof(RotaryCall) and _RULES_CALL.size == C.sizeof(RulesCall)
 
 
@@ -138,6 +172,16 @@ _SIGS = {
     "bild_rules_create": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_void_p)]),
     "bild_rules_destroy": (C.c_int, [C.c_void_p]),
     "bild_rules_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_cache_create": (C.c_int, [C.POINTER(CacheConfig), C.POINTER(C.c_void_p)]),
+    "bild_cache_destroy": (C.c_int, [C.c_void_p]),
+    "bild_cache_extend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_cache_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p]),
+    "bild_cache_compact": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_cache_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_cache_attend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bild_beams_create": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_void_p)]),
+    "bild_beams_destroy": (C.c_int, [C.c_void_p]),
+    "bild_beams_select": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "bild_get_lengths": (C.c_int, [C.c_void_p] + [C.POINTER(C.c_int32)] * 4),
     "bild_get_sequence": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.POINTER(C.c_int32)]),
     "bild_debug_enable_logits": (C.c_int, [C.c_void_p, C.c_int]),
@@ -351,6 +395,90 @@ class Rules:
     def close(self):
         if self.h:
             lib().bild_rules_destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+
+class Cache:
+    """Keys and values of many sequences in 8 bits, in pages; the arrays are the caller's device pointers, see bild.h."""
+    h = None
+
+    def __init__(self, pages: int, page_tokens: int, layers: int, heads: int, d_head: int, sequences: int, max_pages: int, codes: int, scales: int, table: int,
+                 lengths: int, refs: int):
+        h = C.c_void_p()
+        cfg = CacheConfig(codes, scales, table, lengths, refs, pages, page_tokens, layers, heads, d_head, sequences, max_pages, 0)
+        _check(lib().bild_cache_create(C.byref(cfg), C.byref(h)), "bild_cache_create")
+        self.h, self.heads, self.d_head = h, heads, d_head
+        self._extend, self._fork, self._append, self._attend = lib().bild_cache_extend, lib().bild_cache_fork, lib().bild_cache_append, lib().bild_cache_attend
+
+    def extend(self, n: int, rows: int = 0, sequences: Optional[int] = None, cut: Optional[int] = None, starts: Optional[int] = None, granted: Optional[int] = None,
+               window: int = 0, sinks: int = 0, stream: Optional[int] = None):
+        code = self._extend(self.h, _EXTEND_CALL.pack(sequences or 0, cut or 0, starts or 0, granted or 0, n, rows, window, sinks), stream)
+        if code != OK:
+            raise BildError(code, "bild_cache_extend")
+
+    def fork(self, n: int, parents: int, sequences: Optional[int] = None, group: int = 0, stream: Optional[int] = None):
+        code = self._fork(self.h, sequences, parents, n, group, stream)
+        if code != OK:
+            raise BildError(code, "bild_cache_fork")
+
+    def compact(self, used: Optional[int] = None, stream: Optional[int] = None):
+        _check(lib().bild_cache_compact(self.h, used, stream), "bild_cache_compact")
+
+    def append(self, layer: int, dtype: int, n: int, rows: int, k: int, v: int, k_token: Optional[int] = None, k_head: Optional[int] = None,
+               v_token: Optional[int] = None, v_head: Optional[int] = None, sequences: Optional[int] = None, starts: Optional[int] = None, tokens: int = 0,
+               stream: Optional[int] = None):
+        """Device pointers; strides in elements (None: [tokens][heads][d_head])."""
+        d, row = self.d_head, self.heads * self.d_head
+        call = _APPEND_CALL.pack(k or 0, v or 0, row if k_token is None else k_token, d if k_head is None else k_head, row if v_token is None else v_token,
+                                 d if v_head is None else v_head, sequences or 0, starts or 0, n, rows, tokens, layer, dtype, 0)
+        code = self._append(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_cache_append")
+
+    def attend(self, layer: int, dtype: int, n: int, rows: int, heads: int, q: int, out: int, scale: float, lse: Optional[int] = None, q_token: Optional[int] = None,
+               q_head: Optional[int] = None, out_token: Optional[int] = None, out_head: Optional[int] = None, sequences: Optional[int] = None,
+               starts: Optional[int] = None, tokens: int = 0, window: int = 0, sinks: int = 0, causal: bool = True, stream: Optional[int] = None):
+        """Device pointers; strides in elements (None: [tokens][heads][d_head])."""
+        d, row = self.d_head, heads * self.d_head
+        call = _ATTEND_CALL.pack(q or 0, out or 0, lse or 0, row if q_token is None else q_token, d if q_head is None else q_head, row if out_token is None else out_token,
+                                 d if out_head is None else out_head, sequences or 0, starts or 0, n, rows, tokens, layer, heads, dtype, scale, window, sinks, int(causal))
+        code = self._attend(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_cache_attend")
+
+    def close(self):
+        if self.h:
+            lib().bild_cache_destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+
+class Beams:
+    h = None
+
+    def __init__(self, vocab: int, max_batch: int, beams: int):
+        h = C.c_void_p()
+        _check(lib().bild_beams_create(vocab, max_batch, beams, C.byref(h)), "bild_beams_create")
+        self.h, self.vocab, self._select = h, vocab, lib().bild_beams_select
+
+    def select(self, logits: int, dtype: int, batch: int, choices: int, scores: int, out_scores: int, out_parents: int, out_tokens: int,
+               logits_stride: Optional[int] = None, lengths: Optional[int] = None, finished: Optional[int] = None, out_lengths: Optional[int] = None,
+               out_finished: Optional[int] = None, eos: int = -1, pad: int = 0, penalty: float = 0.0, history: Optional[int] = None, history_stride: int = 0,
+               out_history: Optional[int] = None, out_history_stride: int = 0, steps: int = 0, stream: Optional[int] = None):
+        """The fields of bild_beams_call by name: device pointers, strides in elements (None: rows side by side)."""
+        call = _BEAMS_CALL.pack(logits or 0, self.vocab if logits_stride is None else logits_stride, scores or 0, lengths or 0, finished or 0, out_scores or 0,
+                                out_parents or 0, out_tokens or 0, out_lengths or 0, out_finished or 0, history or 0, history_stride, out_history or 0,
+                                out_history_stride, batch, choices, dtype, eos, pad, steps, penalty, 0)
+        code = self._select(self.h, call, stream)
+        if code != OK:
+            raise BildError(code, "bild_beams_select")
+
+    def close(self):
+        if self.h:
+            lib().bild_beams_destroy(self.h)
             self.h = None
 
     __del__ = close

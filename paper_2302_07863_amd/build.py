@@ -34,6 +34,9 @@ UNITS = [
     ("quant.hip", "quant.o", []),
     ("rotary.hip", "rotary.o", []),
     ("rules.hip", "rules.o", []),
+    ("cache.hip", "cache.o", []),
+    ("cache_attend.hip", "cache_attend.o", []),
+    ("beams.hip", "beams.o", []),
     ("layout.cpp", "layout.o", []),
 ]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-pthread",

@@ -1,0 +1,615 @@
+// A cache of keys and values in 8 bits, in pages that sequences share: its pages (bild_cache_extend, _fork, _compact) and what is written into them
+// (bild_cache_append).  Attention over it: cache_attend.hip.
+//
+// Tables, lengths and counts of holders live in device memory and are changed there, so that a beam's parents never come to the host.  Who gets which page is a
+// matter of order (lowest free page first, in the order of the list); one workgroup settles it with prefix sums, so that it is the same every time.  Counts are whole
+// numbers: the order of the atomics shows nowhere.
+// Bound: pages that are copied, by memory, 16 bytes a lane; appending, by the reads of the rows; the rest by launches and a few dependent loads.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "cache.h"
+#include "rows_common.h"
+
+using namespace bild;
+
+namespace {
+
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr float kLimit = 1.329227995784916e36f;  // 2^120: 127 times it is below fp32's largest
+
+// Words of a handle that kernels hand on.
+enum : int { W_FITS = 0, W_COPIES, W_USED, W_MOVES, W_COUNT = 16 };
+
+struct ExtendArgs {
+    CacheView c;
+    CacheRows r;
+    const int* cut;
+    int* granted;
+    int window, sinks;
+    int *plan;             // [sequences][4]: length after the cut, new rows, pages needed before it in the list, page to be copied (-1: none)
+    int *fresh;            // [pages]: the free pages that are given away, lowest first
+    int *asked, *latest;   // [pages], zero between launches: how many of a shared page's holders want to write into it, the last of these + 1
+    int* copies;           // [sequences][3]: from, to, positions
+    int* words;
+};
+
+__device__ __forceinline__ int seen(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Exclusive prefix sum over a workgroup of kPlanThreads, and the sum of all; values up to kMany, and sums beyond that are only known to be beyond.
+constexpr int kMany = kMaxLimit + 1;
+__device__ __forceinline__ int scan(int v, int& total, int* sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o, 64);
+        if (lane >= o) x = min(x + y, kMany);
+    }
+    __syncthreads();  // (of the last call's sums)
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+        before += w < wave ? sums[w] : 0;
+        total += sums[w];
+    }
+    return before + x - v;
+}
+
+// Pages [from, to) of a sequence are given back, by the whole wave.  up_to_none: from the last on, and no further than 64 entries that have none.
+__device__ __forceinline__ void give_back(const CacheView& c, int64_t row, int from, int to, bool up_to_none) {
+    const int lane = threadIdx.x & 63;
+    for (int last = to; last > from; last -= 64) {
+        const int b = last - 1 - lane;
+        int p = -1;
+        if (b >= from) {
+            p = c.table[row + b];
+            if (p != -1) c.table[row + b] = -1;
+            if (c.has(p)) atomicSub(&c.refs[p], 1);
+        }
+        if (up_to_none && !__any(p != -1)) break;
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const ExtendArgs a) {
+    __shared__ int sums[kPlanWaves];
+    __shared__ int wrong;
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 63, n = a.r.n, shift = c.page_shift, mask = c.page_tokens - 1;
+    if (tid == 0) wrong = 0;
+    // the cut, and what a window has left behind
+    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+        const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
+        int length = 0, keep = 0, add = 0, slide0 = 0, slide1 = 0;
+        if (s >= 0) {
+            int first;
+            length = min(max(c.lengths[s], 0), c.cap());
+            keep = a.cut ? min(max(a.cut[i], 0), length) : length;
+            if (a.r.starts) {
+                first = a.r.starts[i];
+                add = (int)min(max((int64_t)a.r.starts[i + 1] - first, (int64_t)0), (int64_t)c.cap() + 1);
+            } else {
+                add = a.r.rows;
+            }
+            if (a.window > 0) {
+                slide0 = (int)(((int64_t)a.sinks + mask) >> shift);
+                slide1 = max(keep - a.window + 1, 0) >> shift;
+            }
+            if (keep != length) c.lengths[s] = keep;
+        }
+        if (i < n) {
+            a.plan[4 * i] = keep;
+            a.plan[4 * i + 1] = s >= 0 ? add : 0;
+        }
+        const int cut0 = (keep + mask) >> shift, cut1 = (length + mask) >> shift;
+        for (unsigned long long todo = __ballot(cut1 > cut0 || slide1 > slide0); todo; todo &= todo - 1) {
+            const int l = (int)__builtin_ctzll(todo);
+            const int64_t row = (int64_t)__shfl(s, l, 64) * c.max_pages;
+            give_back(c, row, __shfl(cut0, l, 64), __shfl(cut1, l, 64), false);
+            give_back(c, row, __shfl(slide0, l, 64), min(__shfl(slide1, l, 64), __shfl(cut0, l, 64)), true);
+        }
+    }
+    __syncthreads();
+    // pages that are shared and would be written
+    for (int i = tid; i < n; i += kPlanThreads) {
+        const int s = a.r.sequence(i, c.sequences), keep = a.plan[4 * i], add = a.plan[4 * i + 1];
+        int shared = -1;
+        if (s >= 0 && add > 0) {
+            if ((int64_t)keep + add > c.cap()) wrong = 1;
+            if (keep & mask) {
+                const int p = c.table[(int64_t)s * c.max_pages + (keep >> shift)];
+                if (!c.has(p)) {
+                    wrong = 1;
+                } else if (seen(&c.refs[p]) > 1) {
+                    shared = p;
+                    atomicAdd(&a.asked[p], 1);
+                    atomicMax(&a.latest[p], i + 1);
+                }
+            }
+        }
+        a.plan[4 * i + 3] = shared;
+    }
+    __threadfence_block();
+    __syncthreads();
+    int needed = 0;
+    const bool fits_so_far = !wrong;
+    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        int need = 0;
+        if (i < n) {
+            const int keep = a.plan[4 * i], add = a.plan[4 * i + 1], p = a.plan[4 * i + 3];
+            if (fits_so_far) need = min(((keep + add + mask) >> shift) - ((keep + mask) >> shift), kMany - 1);
+            if (p >= 0) {
+                if (seen(&a.asked[p]) == seen(&c.refs[p]) && seen(&a.latest[p]) == i + 1) a.plan[4 * i + 3] = -1;  // (the others get copies)
+                else ++need;
+            }
+        }
+        int all;
+        const int before = scan(need, all, sums);
+        if (i < n) a.plan[4 * i + 2] = needed + before;
+        needed = min(needed + all, kMany);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kPlanThreads) {  // (those that keep theirs as well: the count is of all)
+        const int s = a.r.sequence(i, c.sequences), keep = a.plan[4 * i];
+        if (s < 0 || a.plan[4 * i + 1] <= 0 || !(keep & mask)) continue;
+        const int p = c.table[(int64_t)s * c.max_pages + (keep >> shift)];
+        if (c.has(p)) a.asked[p] = a.latest[p] = 0;
+    }
+    // the free pages, lowest first
+    bool fits = fits_so_far && needed <= c.pages;
+    if (fits && needed > 0) {
+        int found = 0;
+        for (int p0 = 0; p0 < c.pages && found < needed; p0 += 8 * kPlanThreads) {
+            int r[8], mine = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int p = p0 + 8 * tid + e;
+                r[e] = p < c.pages ? seen(&c.refs[p]) : 1;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mine += r[e] == 0;
+            int all, at = scan(mine, all, sums);
+            at += found;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (r[e] == 0) {
+                    if (at < needed) a.fresh[at] = p0 + 8 * tid + e;
+                    ++at;
+                }
+            found += all;
+        }
+        fits = found >= needed;
+    }
+    __threadfence_block();
+    __syncthreads();
+    // they are handed out
+    int copies = 0;
+    for (int i0 = 0; fits && i0 < n; i0 += kPlanThreads) {
+        const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
+        int keep = 0, add = 0, at = 0, old = -1;
+        if (s >= 0) {
+            keep = a.plan[4 * i];
+            add = a.plan[4 * i + 1];
+            at = a.plan[4 * i + 2];
+            old = a.plan[4 * i + 3];
+        }
+        int all;
+        const int place = scan(old >= 0, all, sums);
+        if (old >= 0) {
+            const int p = a.fresh[at++];
+            c.table[(int64_t)s * c.max_pages + (keep >> shift)] = p;
+            atomicSub(&c.refs[old], 1);
+            c.refs[p] = 1;
+            int* copy = a.copies + 3 * (copies + place);
+            copy[0] = old;
+            copy[1] = p;
+            copy[2] = keep & mask;
+        }
+        copies += all;
+        if (s >= 0 && add > 0) c.lengths[s] = keep + add;
+        const int b0 = (keep + mask) >> shift, b1 = add > 0 ? (keep + add + mask) >> shift : b0;
+        for (unsigned long long todo = __ballot(b1 > b0); todo; todo &= todo - 1) {
+            const int l = (int)__builtin_ctzll(todo);
+            const int64_t row = (int64_t)__shfl(s, l, 64) * c.max_pages;
+            const int f0 = __shfl(b0, l, 64), f1 = __shfl(b1, l, 64), from = __shfl(at, l, 64);
+            for (int b = f0 + lane; b < f1; b += 64) {
+                const int p = a.fresh[from + b - f0];
+                c.table[row + b] = p;
+                c.refs[p] = 1;
+            }
+        }
+    }
+    if (tid == 0) {
+        a.words[W_FITS] = fits;
+        a.words[W_COPIES] = copies;
+        if (a.granted) *a.granted = fits;
+    }
+}
+
+// The first positions of pages, a wave a layer, half and head.
+__global__ __launch_bounds__(256) void cache_copy_kernel(const CacheView c, const int* copies, const int* words) {
+    const int lane = threadIdx.x & 63, planes = c.layers * 2 * c.heads, per = c.plane_bytes();
+    const int64_t items = (int64_t)words[W_COPIES] * planes;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < items; u += (int64_t)gridDim.x * 4) {
+        const int k = (int)(u / planes), plane = (int)(u - (int64_t)k * planes);
+        const int64_t from = (int64_t)copies[3 * k] * planes + plane, to = (int64_t)copies[3 * k + 1] * planes + plane;
+        const int bytes = copies[3 * k + 2] * c.d_head;  // (a multiple of 8)
+        const int8_t* src = c.codes + from * per;
+        int8_t* dst = c.codes + to * per;
+        for (int b = lane * 16; b + 16 <= bytes; b += 64 * 16) *(uint4*)(dst + b) = *(const uint4*)(src + b);
+        if (lane == 0) {
+            if (bytes & 8) *(uint2*)(dst + (bytes & ~15)) = *(const uint2*)(src + (bytes & ~15));
+            c.scales[to] = c.scales[from];
+        }
+    }
+}
+
+struct ForkArgs {
+    CacheView c;
+    const int *sequences, *parents;
+    int n, group;
+    int* rows;  // [sequences][max_pages]: tables on their way
+    int* plan;  // [sequences][4]: new length, -1: stays
+};
+
+__global__ __launch_bounds__(256) void cache_fork_read_kernel(const ForkArgs a) {
+    const CacheView& c = a.c;
+    const int i = blockIdx.x;
+    const CacheRows r = {a.sequences, nullptr, a.n, 0, 0};
+    const int s = r.sequence(i, c.sequences), parent = a.parents[i], first = i / a.group * a.group;
+    const int from = (unsigned)parent < (unsigned)a.group && first + parent < a.n ? r.sequence(first + parent, c.sequences) : -1;
+    const bool stays = s < 0 || from == s;
+    const int length = from < 0 ? 0 : min(max(c.lengths[from], 0), c.cap());
+    if (threadIdx.x == 0) a.plan[4 * i] = stays ? -1 : length;
+    if (stays) return;
+    const int count = (length + c.page_tokens - 1) >> c.page_shift;
+    for (int b = threadIdx.x; b < count; b += 256) {
+        int p = c.table[(int64_t)from * c.max_pages + b];
+        if (!c.has(p)) p = -1;
+        else atomicAdd(&c.refs[p], 1);
+        a.rows[(int64_t)i * c.max_pages + b] = p;
+    }
+}
+
+__global__ __launch_bounds__(256) void cache_fork_write_kernel(const ForkArgs a) {
+    const CacheView& c = a.c;
+    const int i = blockIdx.x, length = a.plan[4 * i];
+    if (length < 0) return;
+    const CacheRows r = {a.sequences, nullptr, a.n, 0, 0};
+    const int s = r.sequence(i, c.sequences);
+    if (s < 0) return;
+    const int was = min(max(c.lengths[s], 0), c.cap());
+    const int before = (was + c.page_tokens - 1) >> c.page_shift, count = (length + c.page_tokens - 1) >> c.page_shift;
+    for (int b = threadIdx.x; b < max(before, count); b += 256) {
+        int* entry = c.table + (int64_t)s * c.max_pages + b;
+        const int old = b < before ? *entry : -1;
+        *entry = b < count ? a.rows[(int64_t)i * c.max_pages + b] : -1;
+        if (c.has(old)) atomicSub(&c.refs[old], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) c.lengths[s] = length;
+}
+
+struct CompactArgs {
+    CacheView c;
+    int* moves;  // [pages][2]: from, to
+    int* to;     // [pages]
+    int* used;
+    int* words;
+};
+
+__global__ __launch_bounds__(kPlanThreads) void cache_compact_kernel(const CompactArgs a) {
+    __shared__ int sums[kPlanWaves];
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x;
+    int used = 0, all;
+    for (int p0 = 0; p0 < c.pages; p0 += 8 * kPlanThreads)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int p = p0 + e * kPlanThreads + tid;
+            used += p < c.pages && c.refs[p] > 0;
+        }
+    scan(used, all, sums);
+    used = all;
+    int holes = 0, movers = 0;
+    for (int p0 = 0; p0 < c.pages; p0 += 8 * kPlanThreads) {
+        int r[8], h = 0, m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int p = p0 + 8 * tid + e;
+            r[e] = p < c.pages ? c.refs[p] : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int p = p0 + 8 * tid + e;
+            h += p < used && r[e] <= 0;
+            m += p >= used && p < c.pages && r[e] > 0;
+        }
+        int all_h, all_m;
+        int at_h = holes + scan(h, all_h, sums), at_m = movers + scan(m, all_m, sums);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int p = p0 + 8 * tid + e;
+            if (p < used && r[e] <= 0) a.moves[2 * (at_h++) + 1] = p;
+            if (p >= used && p < c.pages && r[e] > 0) a.moves[2 * (at_m++)] = p;
+        }
+        holes += all_h;
+        movers += all_m;
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int k = tid; k < movers; k += kPlanThreads) {
+        const int from = a.moves[2 * k], to = a.moves[2 * k + 1];
+        a.to[from] = to;
+        c.refs[to] = c.refs[from];
+        c.refs[from] = 0;
+    }
+    if (tid == 0) {
+        a.words[W_USED] = used;
+        a.words[W_MOVES] = movers;
+        if (a.used) *a.used = used;
+    }
+}
+
+// Whole pages; the first workgroups' threads turn the tables.
+__global__ __launch_bounds__(256) void cache_move_kernel(const CompactArgs a) {
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, used = a.words[W_USED], moves = a.words[W_MOVES];
+    if (moves == 0) return;
+    for (int s = blockIdx.x; s < c.sequences; s += gridDim.x) {
+        const int length = min(max(c.lengths[s], 0), c.cap()), count = (length + c.page_tokens - 1) >> c.page_shift;
+        for (int b = tid; b < count; b += 256) {
+            int* entry = c.table + (int64_t)s * c.max_pages + b;
+            const int p = *entry;
+            if (p >= used && c.has(p)) *entry = a.to[p];
+        }
+    }
+    const int64_t page_bytes = (int64_t)c.layers * 2 * c.heads * c.plane_bytes(), pieces = (page_bytes + 4095) / 4096;
+    const int planes = c.layers * 2 * c.heads;
+    for (int64_t u = blockIdx.x; u < moves * pieces; u += gridDim.x) {
+        const int k = (int)(u / pieces);
+        const int64_t from = a.moves[2 * k], to = a.moves[2 * k + 1], b = (u - k * pieces) * 4096 + tid * 16;
+        if (b < page_bytes) *(uint4*)(c.codes + to * page_bytes + b) = *(const uint4*)(c.codes + from * page_bytes + b);  // (page_bytes: a multiple of 256)
+        if (u == k * pieces)
+            for (int p = tid; p < planes; p += 256) c.scales[to * planes + p] = c.scales[from * planes + p];
+    }
+}
+
+struct AppendArgs {
+    CacheView c;
+    CacheRows r;
+    const void *x[2];
+    int64_t token[2], head[2];
+    int layer;
+    const int* words;
+};
+
+__device__ __forceinline__ float bounded(float x) { return __builtin_amdgcn_fmed3f(x != x ? 0.f : x, -kLimit, kLimit); }
+
+// A workgroup has the new positions of one page, of keys or values of a head: their largest magnitude, then their codes.
+template <class R, int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs a) {
+    constexpr int E = 8, KEPT = 4;  // values of a piece; pieces a thread keeps from the first pass for the second
+    typedef typename R::type V;
+    __shared__ float tops[THREADS / 64];
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y, which = blockIdx.z, T = c.page_tokens;
+    if (!a.words[W_FITS]) return;
+    // entry i of the list has the slots floor(first row / T) + 2 i and those behind, as many as it can have pages
+    int i, first, count, nth;
+    if (a.r.starts) {
+        int lo = 0, hi = a.r.n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            a.r.span(mid, first, count);
+            if ((first >> c.page_shift) + 2 * mid <= slot) lo = mid; else hi = mid;
+        }
+        i = lo;
+        a.r.span(i, first, count);
+        nth = slot - (first >> c.page_shift) - 2 * i;
+    } else {
+        const int per = ((a.r.rows - 1) >> c.page_shift) + 2;
+        i = slot / per;
+        nth = slot - i * per;
+        a.r.span(i, first, count);
+    }
+    if (nth < 0 || nth > ((count - 1) >> c.page_shift) + 1) return;
+    const int s = a.r.sequence(i, c.sequences);
+    if (s < 0 || count == 0) return;
+    const int length = min(max(c.lengths[s], 0), c.cap()), begin = length - count;  // (rows from before the beginning are not written)
+    const int b = (max(begin, 0) >> c.page_shift) + nth;
+    if ((b << c.page_shift) >= length) return;
+    const int p0 = max(begin, b << c.page_shift), p1 = min(length, (b + 1) << c.page_shift);
+    const int page = c.table[(int64_t)s * c.max_pages + b];
+    if (!c.has(page) || c.refs[page] != 1) return;
+    const int64_t plane = c.plane(page, a.layer, which, head);
+    const int before = p0 - (b << c.page_shift), m = p1 - p0, d = c.d_head, per_row = d / E, pieces = m * per_row;
+    int8_t* codes = c.codes + plane * c.plane_bytes();
+    const V* x = (const V*)a.x[which] + (int64_t)(first + p0 - begin) * a.token[which] + (int64_t)head * a.head[which];
+    const float was = before > 0 ? fabsf(bounded(c.scales[plane])) : 0.f;
+    RowVec<R, E> kept[KEPT];
+    const auto at = [&](int u) {
+        const int row = u / per_row;
+        return x + (int64_t)row * a.token[which] + (u - row * per_row) * E;
+    };
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+        if (k * THREADS + tid < pieces) {
+            kept[k].load(at(k * THREADS + tid));
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) kept[k].v[e] = 0;
+        }
+    const auto largest = [&](const RowVec<R, E>& q) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(bounded(R::up(q.v[e]))));
+    };
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) largest(kept[k]);
+    for (int u = KEPT * THREADS + tid; u < pieces; u += THREADS) {
+        RowVec<R, E> q;
+        q.load(at(u));
+        largest(q);
+    }
+    top = wave_max(top);
+    if (THREADS > 64) {
+        if ((tid & 63) == 0) tops[tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, tops[w]);
+    }
+    const float scale = fmaxf(was, top);
+    // (contraction would change nothing: each is a product, a division, a rounding)
+    if (scale > was) {
+        for (int u = tid; u < before * per_row; u += THREADS) {
+            uint2 q = *(const uint2*)(codes + 8 * u);
+            int8_t v[8];
+            __builtin_memcpy(v, &q, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (int8_t)rintf((float)v[e] * was / scale);
+            __builtin_memcpy(&q, v, 8);
+            *(uint2*)(codes + 8 * u) = q;
+        }
+    }
+    const auto put = [&](const RowVec<R, E>& q, int u) {
+        int8_t v[8];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = scale > 0.f ? (int8_t)rintf(bounded(R::up(q.v[e])) * 127.f / scale) : (int8_t)0;
+        uint2 w;
+        __builtin_memcpy(&w, v, 8);
+        *(uint2*)(codes + (int64_t)before * d + 8 * u) = w;
+    };
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+        if (k * THREADS + tid < pieces) put(kept[k], k * THREADS + tid);
+    for (int u = KEPT * THREADS + tid; u < pieces; u += THREADS) {
+        RowVec<R, E> q;
+        q.load(at(u));
+        put(q, u);
+    }
+    if (tid == 0) c.scales[plane] = scale;
+}
+
+template <class R>
+hipError_t launch_append(const AppendArgs& a, dim3 grid, bool few, hipStream_t st) {
+    return few ? launch_on(cache_append_kernel<R, 64>, grid, dim3(64), 0, st, a) : launch_on(cache_append_kernel<R, 256>, grid, dim3(256), 0, st, a);
+}
+
+bool config_ok(const bild_cache_config& g) {
+    if (!g.codes || !g.scales || !g.table || !g.lengths || !g.refs || g.reserved != 0) return false;
+    if ((uintptr_t)g.codes % 16 || ((uintptr_t)g.scales | (uintptr_t)g.table | (uintptr_t)g.lengths | (uintptr_t)g.refs) % 4) return false;
+    if (g.page_tokens != 32 && g.page_tokens != 64 && g.page_tokens != 128) return false;
+    if (g.pages < 1 || g.pages > kMaxLimit || g.layers < 1 || g.layers > 1024 || g.heads < 1 || g.heads > 1024) return false;
+    if (g.d_head < 16 || g.d_head > 256 || g.d_head % 8 || g.sequences < 1 || g.sequences > 65535 || g.max_pages < 1) return false;
+    return (int64_t)g.max_pages * g.page_tokens <= 1 << 30 && (int64_t)g.sequences * g.max_pages <= 1 << 28;
+}
+
+}  // namespace
+
+extern "C" int bild_cache_create(const bild_cache_config* cfg, bild_cache** out) {
+    if (!cfg || !out || !config_ok(*cfg)) return BILD_EINVAL;
+    const bild_cache_config& g = *cfg;
+    bild_cache* c = new (std::nothrow) bild_cache();
+    if (!c) return BILD_ENOMEM;
+    c->view = {g.codes, g.scales, g.table, g.lengths, g.refs, g.pages, g.page_tokens, g.page_tokens == 32 ? 5 : g.page_tokens == 64 ? 6 : 7, g.layers, g.heads,
+               g.d_head, g.sequences, g.max_pages};
+    const size_t seqs = (size_t)g.sequences, pages = (size_t)g.pages, counts = attend_counts(g.heads);
+    // (asked, latest, counts of arrivals and words begin as zeros)
+    const size_t zeros = 2 * pages + counts + W_COUNT, ints = zeros + 7 * seqs + 4 * pages + seqs * (size_t)g.max_pages;
+    const size_t bytes = (ints * 4 + 255) / 256 * 256, floats = attend_part_floats(g.heads, g.d_head);
+    int rc = BILD_OK;
+    const int one = 1;
+    if (hipGetDevice(&c->device) != hipSuccess || attend_init(g.d_head) != hipSuccess) rc = BILD_EHIP;
+    else if (hipMalloc(&c->mem, bytes + 4 * floats) != hipSuccess) c->mem = nullptr, rc = BILD_ENOMEM;
+    else {
+        c->words = (int*)c->mem;
+        c->asked = c->words + W_COUNT;
+        c->latest = c->asked + pages;
+        c->arrived = (unsigned*)(c->latest + pages);
+        c->plan = (int*)(c->arrived + counts);
+        c->fresh = c->plan + 7 * seqs;
+        c->moves = c->fresh + pages;
+        c->rows = c->moves + 3 * pages;
+        c->part = (float*)((char*)c->mem + bytes);
+        if (hipMemset(c->mem, 0, 4 * zeros) != hipSuccess || hipMemcpy(c->words + W_FITS, &one, 4, hipMemcpyHostToDevice) != hipSuccess ||
+            hipStreamSynchronize(nullptr) != hipSuccess)
+            rc = BILD_EHIP;
+    }
+    if (rc != BILD_OK) {
+        (void)hipGetLastError();  // (told by rc: not to be found by a later call as well)
+        (void)bild_cache_destroy(c);
+        return rc;
+    }
+    *out = c;
+    return BILD_OK;
+}
+
+extern "C" int bild_cache_destroy(bild_cache* c) {
+    if (!c) return BILD_EINVAL;
+    if (c->mem) (void)hipFree(c->mem);
+    delete c;
+    return BILD_OK;
+}
+
+extern "C" int bild_cache_extend(bild_cache* c, const bild_cache_extend_call* call, void* hip_stream) {
+    if (!c || !call) return BILD_EINVAL;
+    const bild_cache_extend_call& k = *call;
+    if (k.n < 1 || k.n > c->view.sequences || k.rows < 0 || k.window < 0 || k.sinks < 0) return BILD_EINVAL;
+    const ExtendArgs a = {c->view, {k.sequences, k.starts, k.n, std::min(k.rows, c->view.cap() + 1), 0}, k.cut, k.granted, k.window, k.sinks, c->plan, c->fresh, c->asked, c->latest,
+                          c->plan + 4 * (size_t)c->view.sequences, c->words};
+    const OnDevice on(c->device);
+    if (!on.ok) return BILD_EHIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (launch_on(cache_extend_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) != hipSuccess) return BILD_EHIP;
+    if (!k.starts && k.rows == 0) return BILD_OK;  // (nothing is copied)
+    const int64_t planes = (int64_t)c->view.layers * 2 * c->view.heads, groups = std::min<int64_t>((k.n * planes + 3) / 4, 2048);
+    const int* copies = a.copies;
+    return launch_on(cache_copy_kernel, dim3((unsigned)groups), dim3(256), 0, st, c->view, copies, c->words) == hipSuccess ? BILD_OK : BILD_EHIP;
+}
+
+extern "C" int bild_cache_fork(bild_cache* c, const int32_t* sequences, const int32_t* parents, int n, int group, void* hip_stream) {
+    if (!c || !parents || n < 1 || n > c->view.sequences || group < 0 || group > n) return BILD_EINVAL;
+    const ForkArgs a = {c->view, sequences, parents, n, group ? group : n, c->rows, c->plan};
+    const OnDevice on(c->device);
+    if (!on.ok) return BILD_EHIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (launch_on(cache_fork_read_kernel, dim3(n), dim3(256), 0, st, a) != hipSuccess) return BILD_EHIP;
+    return launch_on(cache_fork_write_kernel, dim3(n), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
+}
+
+extern "C" int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream) {
+    if (!c) return BILD_EINVAL;
+    const CompactArgs a = {c->view, c->moves, c->moves + 2 * (size_t)c->view.pages, used, c->words};
+    const OnDevice on(c->device);
+    if (!on.ok) return BILD_EHIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (launch_on(cache_compact_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) != hipSuccess) return BILD_EHIP;
+    return launch_on(cache_move_kernel, dim3(2048), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
+}
+
+extern "C" int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* hip_stream) {
+    if (!c || !call) return BILD_EINVAL;
+    const bild_cache_append_call& k = *call;
+    if (!k.k || !k.v || k.reserved != 0 || !row_type(k.dtype) || k.layer < 0 || k.layer >= c->view.layers) return BILD_EINVAL;
+    if (k.n < 1 || k.n > c->view.sequences || k.rows < 1 || (k.starts && k.tokens < 1)) return BILD_EINVAL;
+    const int64_t slots = k.starts ? (k.tokens >> c->view.page_shift) + 2 * (int64_t)k.n : k.n * (int64_t)(((k.rows - 1) >> c->view.page_shift) + 2);
+    if ((!k.starts && (int64_t)k.n * k.rows > 0x7FFFFFFF) || slots > 0x7FFFFFFF) return BILD_EINVAL;
+    const AppendArgs a = {c->view, {k.sequences, k.starts, k.n, k.rows, k.starts ? k.tokens : k.n * k.rows}, {k.k, k.v}, {k.k_token, k.v_token}, {k.k_head, k.v_head}, k.layer, c->words};
+    const OnDevice on(c->device);
+    if (!on.ok) return BILD_EHIP;
+    const dim3 grid((unsigned)slots, c->view.heads, 2);
+    const bool few = k.rows <= 4;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const hipError_t err = k.dtype == BILD_DT_F32 ? launch_append<RowF32>(a, grid, few, st) : k.dtype == BILD_DT_BF16 ? launch_append<RowBf16>(a, grid, few, st)
+                                                                                                                : launch_append<RowF16>(a, grid, few, st);
+    return err == hipSuccess ? BILD_OK : BILD_EHIP;
+}

@@ -1,0 +1,514 @@
+// Attention over the cache in 8 bits (bild_cache_attend), all keys or a sliding window with sinks.
+//
+//   out = sum_j p_j s_v[j] cv_j / 127,  p = softmax_j(scale s_k[j] q ck_j / 127)
+//
+// Bound, for a few rows a sequence: HBM, a byte a value, each key and value read once for all rows and query heads of its key head.  Sixteen such rows are one operand of the matrix
+// cores.  Scores come out transposed, S^T = K Q^T, so that a lane has eight consecutive keys of one row, which is what the second product, O^T = V^T P^T, takes from it: weights
+// go from one to the other in registers.  Codes become fp16 in one byte permutation for two (code ^ 0x80 as the bits of a subnormal) and one packed product and sum, for the values' transposition
+// into the bargain: the pairs that the permutation joins are two tokens' codes.  (c + 128) 2^-24 * 2^15 - 2^-2 = c 2^-9: every code is exact.  A page's scale is applied to
+// scores and to partial sums in fp32.
+//
+// Work is cut where it is: the 32-token blocks of all sequences and row tiles lie in one line, of which each workgroup of a key head takes an equal piece, wherever sequences begin or
+// end (the lengths are in device memory, and a batch's are far apart); a workgroup's four waves take turns over its blocks.  What several workgroups have of a tile the last of them joins, in order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "cache.h"
+#include "last_in.h"
+#include "rows_common.h"
+
+using namespace bild;
+
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kBlock = 32;     // keys of a step
+constexpr int kTile = 16;      // rows of a tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Weights are powers of two relative to a maximum that is moved only when a score is beyond it by this much: they stay below 2^8, far from fp16's end.
+constexpr float kSlack = 8.f;
+
+struct AttendArgs {
+    CacheView c;
+    CacheRows r;
+    const void* q;
+    void* out;
+    float* lse;
+    int64_t q_token, q_head, out_token, out_head;
+    int layer, heads, group;
+    int window, sinks, causal;
+    float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
+    int groups, least;  // workgroups of a key head; blocks that one takes at least
+    float* part;
+    unsigned* arrived;
+};
+
+// Floats of a row of partial results: the sums over the values, maximum, sum of weights.
+constexpr int part_row(int DP) { return DP + 4; }
+
+__device__ __forceinline__ f16x2 two(uint32_t x) {
+    const f16x2 by = {(_Float16)32768.f, (_Float16)32768.f}, off = {(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), by, off);
+}
+struct Halves {
+    f16x2 v[4];
+};
+__device__ __forceinline__ f16x8 eight(f16x2 a, f16x2 b, f16x2 c, f16x2 d) { return __builtin_bit_cast(f16x8, Halves{{a, b, c, d}}); }
+// eight codes (already ^ 0x80) side by side
+__device__ __forceinline__ f16x8 eight_of(uint32_t a, uint32_t b) {
+    return eight(two(__builtin_amdgcn_perm(0u, a, 0x0c010c00u)), two(__builtin_amdgcn_perm(0u, a, 0x0c030c02u)), two(__builtin_amdgcn_perm(0u, b, 0x0c010c00u)),
+                 two(__builtin_amdgcn_perm(0u, b, 0x0c030c02u)));
+}
+// byte k of two words
+__device__ __forceinline__ f16x2 pair_of(uint32_t a, uint32_t b, int k) { return two(__builtin_amdgcn_perm(b, a, 0x0c000c00u | (unsigned)(4 + k) << 16 | (unsigned)k)); }
+
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// A sequence's share of the work.
+struct Seq {
+    int s, first, count, length;  // which, its rows, its positions
+    int tiles, sink_blocks, low_block, blocks;
+};
+__device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
+    Seq q;
+    q.s = a.r.sequence(i, a.c.sequences);
+    a.r.span(i, q.first, q.count);
+    if (q.s < 0) q.count = 0;
+    q.length = q.s < 0 ? 0 : min(max(a.c.lengths[q.s], 0), a.c.cap());
+    q.tiles = (int)(((int64_t)q.count * a.group + kTile - 1) / kTile);
+    q.low_block = a.window ? max(q.length - q.count - a.window + 1, 0) / kBlock : 0;
+    q.sink_blocks = a.window ? min((int)(((int64_t)a.sinks + kBlock - 1) / kBlock), q.low_block) : 0;
+    q.blocks = max(q.sink_blocks + (q.length + kBlock - 1) / kBlock - q.low_block, 1);  // (one that has none is written all the same)
+    return q;
+}
+
+// Registers of a block's codes.
+template <int DP>
+struct Codes {
+    static constexpr int NK = DP / 64, NJ = DP / 16, WV = NJ / 4;
+    u32x4 k[2][NK];   // two keys of a lane, 16 codes of each 64
+    uint32_t v[8][WV];  // eight values, NJ codes of each
+};
+
+template <class R, int DP>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kernel(const AttendArgs a) {
+    constexpr bool TWO = R::kDtype == BILD_DT_F32;  // rows and weights in two fp16 parts
+    constexpr int NK = DP / 64, KS = DP / 32, NJ = DP / 16, WV = NJ / 4, TERMS = TWO ? 2 : 1, LD = DP + 4;
+    typedef typename R::type V;
+    extern __shared__ __attribute__((aligned(16))) float sums[];  // [4 waves or 16 slots][16 rows][LD], then maxima and sums of weights
+    __shared__ float tops[kWaves * kTile], weights[kWaves * kTile];
+    __shared__ long long scan_sums[kWaves];
+    __shared__ int found;
+    __shared__ long long found_at;
+    __shared__ unsigned share;
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
+    const int head = blockIdx.y, d = c.d_head;
+
+    // where this workgroup's piece of the line begins
+    long long w0, w1, line;
+    {
+        const int per = (a.r.n + kThreads - 1) / kThreads, i0 = min(tid * per, a.r.n), i1 = min(i0 + per, a.r.n);
+        long long mine = 0;
+        for (int i = i0; i < i1; ++i) {
+            const Seq q = sequence_at(a, i);
+            mine += (long long)q.tiles * q.blocks;
+        }
+        long long x = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const long long y = __shfl_up(x, o, 64);
+            if (lane >= o) x += y;
+        }
+        if (lane == 63) scan_sums[wave] = x;
+        __syncthreads();
+        long long before = x - mine;
+        line = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            before += w < wave ? scan_sums[w] : 0;
+            line += scan_sums[w];
+        }
+        const long long chunk = max((line + a.groups - 1) / a.groups, (long long)a.least);
+        w0 = blockIdx.x * chunk;
+        w1 = min(w0 + chunk, line);
+        if (w0 >= line) return;
+        if (before <= w0 && w0 < before + mine) {
+            int i = i0;
+            for (;; ++i) {
+                const Seq q = sequence_at(a, i);
+                const long long next = before + (long long)q.tiles * q.blocks;
+                if (w0 < next) break;
+                before = next;
+            }
+            found = i;
+            found_at = before;
+        }
+        __syncthreads();
+    }
+    const long long chunk = max((line + a.groups - 1) / a.groups, (long long)a.least);
+    int i = __builtin_amdgcn_readfirstlane(found);
+    long long at = found_at;
+    Seq sq = sequence_at(a, i);
+
+    for (long long w = w0; w < w1;) {
+        while (w >= at + (long long)sq.tiles * sq.blocks) {
+            at += (long long)sq.tiles * sq.blocks;
+            sq = sequence_at(a, ++i);
+        }
+        const int tile = (int)((w - at) / sq.blocks), b0 = (int)((w - at) - (long long)tile * sq.blocks), b1 = (int)min((long long)sq.blocks, b0 + (w1 - w));
+        const long long unit = at + (long long)tile * sq.blocks;  // where the tile begins
+        // ---- rows
+        const int rows = sq.count * a.group, idx = tile * kTile + n16, mine = min(idx, rows - 1), j = mine / a.group, e = mine - j * a.group;
+        const int pos = a.causal ? sq.length - sq.count + j : sq.length - 1, low = a.window ? pos - a.window : -1;
+        f16x8 q[TERMS][KS];
+        float row_scale;
+        {
+            const V* x = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
+            RowVec<R, 8> raw[KS];
+            float big = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
+                raw[s].load(x + off);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) big = fmaxf(big, off + t >= begin ? fabsf(R::up(raw[s].v[t])) : 0.f);
+            }
+            big = quad_rows_max(big);
+            int up = 0;
+            if (big > 0.f && big < INFINITY) {
+                frexpf(big, &up);
+                up = 15 - up;
+            }
+            row_scale = ldexpf(1.f, -up);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    // (a piece behind the head's end begins earlier, and what another lane has as well is 0 here)
+                    const float v = off + t >= begin ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
+                    q[0][s][t] = (_Float16)v;
+                    if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
+                }
+            }
+        }
+        // the positions that the tile's rows see
+        const int j0 = tile * kTile / a.group, j1 = min((tile * kTile + kTile - 1) / a.group, sq.count - 1);
+        const int first_pos = a.causal ? sq.length - sq.count + j0 : sq.length - 1, last_pos = a.causal ? sq.length - sq.count + j1 : sq.length - 1;
+        const auto block_at = [&](int b) { return b < sq.sink_blocks ? b : b - sq.sink_blocks + sq.low_block; };
+        // ---- a page and its scales for each of the next 64 blocks of this wave, a lane a block
+        int pages = -1;
+        float k_scale = 0.f, v_scale = 0.f;
+        const auto look_up = [&](int b) {
+            const int mine_at = b + kWaves * lane, blk = block_at(mine_at), p0 = blk * kBlock;
+            pages = -1;
+            if (mine_at < b1 && p0 < sq.length && p0 <= last_pos && (!a.window || p0 + kBlock - 1 > first_pos - a.window || p0 < a.sinks))
+                pages = c.table[(int64_t)sq.s * c.max_pages + (p0 >> c.page_shift)];
+            if (!c.has(pages)) pages = -1;
+            if (pages >= 0) {
+                k_scale = c.scales[c.plane(pages, a.layer, 0, head)];
+                v_scale = c.scales[c.plane(pages, a.layer, 1, head)] * (512.f / 127.f);
+            }
+        };
+        float top = -INFINITY, sum = 0.f;
+        f32x4 acc[NJ];
+#pragma unroll
+        for (int t = 0; t < NJ; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        const int key = (n16 >> 2) * 8 + (n16 & 3);  // the lane's row of the first operand, in two halves: tokens key and key + 4
+        const auto load = [&](Codes<DP>& x, int page, int blk) {
+            const int in_page = blk * kBlock & (c.page_tokens - 1);
+            const auto k = make_rsrc(c.codes + c.plane(page, a.layer, 0, head) * c.plane_bytes(), (size_t)c.plane_bytes());
+            const auto v = make_rsrc(c.codes + c.plane(page, a.layer, 1, head) * c.plane_bytes(), (size_t)c.plane_bytes());
+            const int base = in_page * d;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < NK; ++t) {
+                    // (rows begin at multiples of 8 bytes)
+                    x.k[h][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, (key + 4 * h) * d + min(64 * t + 16 * g, d - 16), base, 0));
+                }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const int off = (8 * g + t) * d + min(n16 * NJ, d - NJ);
+                if constexpr (WV == 1) {
+                    x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, base, 0);
+                } else if constexpr (WV == 2) {
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, base, 0);
+                    x.v[t][0] = (uint32_t)y[0];
+                    x.v[t][1] = (uint32_t)y[1];
+                } else {
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b128(v, off, base, 0);
+#pragma unroll
+                    for (int w4 = 0; w4 < 4; ++w4) x.v[t][w4] = (uint32_t)y[w4];
+                }
+            }
+        };
+        const auto use = [&](Codes<DP>& x, int blk, float ks, float vs) {
+            f32x4 z[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                z[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < NK; ++t) {
+                    const u32x4 y = x.k[h][t] ^ 0x80808080u;
+                    const f16x8 lo = eight_of(y[0], y[1]), hi = eight_of(y[2], y[3]);
+#pragma unroll
+                    for (int m = 0; m < TERMS; ++m) {
+                        z[h] = mma(lo, q[m][2 * t], z[h]);
+                        z[h] = mma(hi, q[m][2 * t + 1], z[h]);
+                    }
+                }
+            }
+            const float by = ks * a.scale * row_scale;
+            const int p0 = blk * kBlock + 8 * g;
+            float p[8], big = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const int at_pos = p0 + t;
+                const bool sees = at_pos <= pos && (at_pos > low || at_pos < a.sinks);
+                p[t] = sees ? z[t >> 2][t & 3] * by : -INFINITY;
+                big = fmaxf(big, p[t]);
+            }
+            big = quad_rows_max(big);
+            if (__any(big > top + kSlack)) {
+                const float now = big > top + kSlack ? big : top;
+                const float less = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                sum *= less;
+#pragma unroll
+                for (int t = 0; t < NJ; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[t][r] *= less;
+                top = now;
+            }
+            const float base = top == -INFINITY ? 0.f : top;
+            f16x8 w[TERMS];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const float v = __builtin_amdgcn_exp2f(p[t] - base);
+                sum += v;
+                w[0][t] = (_Float16)v;
+                if (TWO) w[TERMS - 1][t] = (_Float16)(v - (float)w[0][t]);
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int y = 0; y < WV; ++y) x.v[t][y] ^= 0x80808080u;
+#pragma unroll
+            for (int t = 0; t < NJ; ++t) {
+                const int y = t / 4, k = t % 4;
+                const f16x8 v = eight(pair_of(x.v[0][y], x.v[1][y], k), pair_of(x.v[2][y], x.v[3][y], k), pair_of(x.v[4][y], x.v[5][y], k), pair_of(x.v[6][y], x.v[7][y], k));
+                f32x4 part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int m = 0; m < TERMS; ++m) part = mma(v, w[m], part);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[t][r] = __builtin_fmaf(part[r], vs, acc[t][r]);
+            }
+        };
+        // ---- the wave's blocks, the next one's codes on their way
+        Codes<DP> one, other;
+        int nth = 64, b = b0 + wave - kWaves;  // of the looked up ones
+        struct Next {
+            int blk;  // -1: no more
+            float ks, vs;
+        };
+        const auto next = [&](Codes<DP>& x) {
+            Next r = {-1, 0.f, 0.f};
+            for (b += kWaves; b < b1; b += kWaves) {
+                if (nth == 64) {
+                    look_up(b);
+                    nth = 0;
+                }
+                const int page = __builtin_amdgcn_readlane(pages, nth);
+                r.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k_scale), nth));
+                r.vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v_scale), nth));
+                ++nth;
+                if (page >= 0) {
+                    r.blk = block_at(b);
+                    load(x, page, r.blk);
+                    break;
+                }
+            }
+            return r;
+        };
+        Next x = next(one);
+        while (x.blk >= 0) {
+            const Next y = next(other);
+            use(one, x.blk, x.ks, x.vs);
+            if (y.blk < 0) break;
+            x = next(one);
+            use(other, y.blk, y.ks, y.vs);
+        }
+
+        // ---- the waves' results joined: a slot of 16 threads a row
+        sum = quad_rows_sum(sum);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float* to = sums + (wave * kTile + n16) * LD + (4 * g + r) * NJ;
+#pragma unroll
+            for (int t = 0; t < NJ; t += 4) *(float4*)(to + t) = make_float4(acc[t][r], acc[t + 1][r], acc[t + 2][r], acc[t + 3][r]);
+        }
+        if (g == 0) {
+            tops[wave * kTile + n16] = top;
+            weights[wave * kTile + n16] = sum;
+        }
+        __syncthreads();
+        const int slot = tid >> 4, col = (tid & 15) * NJ, valid = min(kTile, rows - tile * kTile);
+        float m = -INFINITY, l = 0.f, o[NJ];
+#pragma unroll
+        for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+        const auto fold = [&](float pm, float pl, const float* po) {  // (parts that have seen nothing: of weight 0)
+            const float now = fmaxf(m, pm), base = now == -INFINITY ? 0.f : now;
+            const float was = __builtin_amdgcn_exp2f(m - base), is = __builtin_amdgcn_exp2f(pm - base);
+            l = l * was + pl * is;
+#pragma unroll
+            for (int t = 0; t < NJ; ++t) o[t] = o[t] * was + po[t] * is;
+            m = now;
+        };
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) fold(tops[k * kTile + slot], weights[k * kTile + slot], sums + (k * kTile + slot) * LD + col);
+        const auto put = [&](int row) {
+            const int jr = (tile * kTile + row) / a.group, er = tile * kTile + row - jr * a.group, h = head * a.group + er;
+            const int64_t t_at = sq.first + jr;
+            const float by = l == 0.f ? 0.f : 1.f / l;
+            RowVec<R, NJ> y;
+#pragma unroll
+            for (int t = 0; t < NJ; ++t) y.v[t] = R::down(o[t] * by);
+            V* out = (V*)a.out + t_at * a.out_token + (int64_t)h * a.out_head;
+            if (col < d) y.store(out + min(col, d - NJ));  // (a last piece that is cut begins earlier, as its loads did: the lane before writes the same there)
+            if (a.lse && col == 0) a.lse[t_at * a.heads + h] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+        };
+        const bool whole = b0 == 0 && b1 == sq.blocks;
+        if (whole) {
+            if (slot < valid) put(slot);
+            __syncthreads();
+        } else {
+            // the workgroups that share the tile: in the first of them it begins last, in the others first
+            const int from = (int)(unit / chunk), to = (int)((unit + sq.blocks - 1) / chunk);
+            constexpr int kRow = part_row(DP);
+            const int64_t place = ((int64_t)head * a.groups + blockIdx.x) * 2 + (blockIdx.x == from);
+            const auto mem = make_rsrc(a.part + place * kTile * kRow, sizeof(float) * kTile * kRow);
+            if (slot < valid) {
+#pragma unroll
+                for (int t = 0; t < NJ; t += 4)
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[t]), __float_as_uint(o[t + 1]), __float_as_uint(o[t + 2]), __float_as_uint(o[t + 3])}, mem,
+                                                           (slot * kRow + col + t) * 4, 0, kPartAux);
+                if (col == 0) __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(m), __float_as_uint(l), 0u, 0u}, mem, (slot * kRow + DP) * 4, 0, kPartAux);
+            }
+            if (last_in(a.arrived + (int64_t)head * a.groups + from, (unsigned)(to - from + 1), &share)) {
+                // each row's parts dealt to as many slots as there are
+                int lanes = 1;
+                while (lanes < valid) lanes <<= 1;
+                const int apart = kTile / lanes, row = slot & (lanes - 1), sub = slot / lanes;
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll
+                for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+                for (int p = from + sub; p <= to && row < valid; p += apart) {
+                    const int64_t where = ((int64_t)head * a.groups + p) * 2 + (p == from);
+                    const auto src = make_rsrc(a.part + where * kTile * kRow, sizeof(float) * kTile * kRow);
+                    float po[NJ];
+                    const u32x4 ml = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (row * kRow + DP) * 4, 0, kPartAux));
+#pragma unroll
+                    for (int t = 0; t < NJ; t += 4) {
+                        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (row * kRow + col + t) * 4, 0, kPartAux));
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) po[t + u] = __uint_as_float(y[u]);
+                    }
+                    fold(__uint_as_float(ml[0]), __uint_as_float(ml[1]), po);
+                }
+                if (apart > 1) {
+#pragma unroll
+                    for (int t = 0; t < NJ; t += 4) *(float4*)(sums + slot * LD + col + t) = make_float4(o[t], o[t + 1], o[t + 2], o[t + 3]);
+                    if (col == 0) {
+                        tops[slot] = m;
+                        weights[slot] = l;
+                    }
+                    __syncthreads();
+                    if (slot < valid) {
+                        m = -INFINITY;
+                        l = 0.f;
+#pragma unroll
+                        for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+                        for (int k = 0; k < apart; ++k) fold(tops[k * lanes + slot], weights[k * lanes + slot], sums + (k * lanes + slot) * LD + col);
+                    }
+                }
+                if (slot < valid) put(slot);
+            }
+            __syncthreads();
+        }
+        w += b1 - b0;
+    }
+}
+
+constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
+
+template <class R, int DP>
+hipError_t launch(const AttendArgs& a, hipStream_t st) {
+    return launch_on(cache_attend_kernel<R, DP>, dim3(a.groups, a.c.heads), dim3(kThreads), lds_bytes(DP), st, a);
+}
+template <class R>
+hipError_t launch(const AttendArgs& a, hipStream_t st) {
+    return a.c.d_head <= 64 ? launch<R, 64>(a, st) : a.c.d_head <= 128 ? launch<R, 128>(a, st) : launch<R, 256>(a, st);
+}
+
+}  // namespace
+
+namespace bild {
+
+hipError_t attend_init(int d_head) {
+    const void* const wide[] = {(const void*)cache_attend_kernel<RowF32, 256>, (const void*)cache_attend_kernel<RowBf16, 256>, (const void*)cache_attend_kernel<RowF16, 256>};
+    return d_head <= 128 ? hipSuccess : raise_lds_limit(wide, (int)lds_bytes(256));
+}
+
+size_t attend_part_floats(int heads, int d_head) {
+    return (size_t)heads * attend_groups(heads) * 2 * kTile * part_row(d_head <= 64 ? 64 : d_head <= 128 ? 128 : 256);
+}
+
+}  // namespace bild
+
+extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* call, void* hip_stream) {
+    if (!c || !call) return BILD_EINVAL;
+    const bild_cache_attend_call& k = *call;
+    const CacheView& v = c->view;
+    if (!k.q || !k.out || !row_type(k.dtype) || k.layer < 0 || k.layer >= v.layers || k.window < 0 || k.sinks < 0 || !std::isfinite(k.scale)) return BILD_EINVAL;
+    if (k.n < 1 || k.n > v.sequences || k.rows < 1 || (k.starts && k.tokens < 1) || (k.causal != 0 && k.causal != 1) || (!k.causal && k.window)) return BILD_EINVAL;
+    if (k.heads < 1 || k.heads % v.heads || k.heads / v.heads > 64) return BILD_EINVAL;
+    const int64_t tokens = k.starts ? k.tokens : (int64_t)k.n * k.rows;
+    if (tokens * k.heads > 0x7FFFFFFF) return BILD_EINVAL;
+    AttendArgs a;
+    std::memset((void*)&a, 0, sizeof(a));
+    a.c = v;
+    a.r = {k.sequences, k.starts, k.n, k.rows, (int)tokens};
+    a.q = k.q;
+    a.out = k.out;
+    a.lse = k.lse;
+    a.q_token = k.q_token;
+    a.q_head = k.q_head;
+    a.out_token = k.out_token;
+    a.out_head = k.out_head;
+    a.layer = k.layer;
+    a.heads = k.heads;
+    a.group = k.heads / v.heads;
+    a.window = k.window;
+    a.sinks = k.window ? k.sinks : 0;
+    a.causal = k.causal;
+    a.scale = (float)((double)k.scale * 1.4426950408889634 * 512.0 / 127.0);
+    a.groups = attend_groups(v.heads);
+    a.least = 8;
+    a.part = c->part;
+    a.arrived = c->arrived;
+    const OnDevice on(c->device);
+    if (!on.ok) return BILD_EHIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const hipError_t err = k.dtype == BILD_DT_F32 ? launch<RowF32>(a, st) : k.dtype == BILD_DT_BF16 ? launch<RowBf16>(a, st) : launch<RowF16>(a, st);
+    return err == hipSuccess ? BILD_OK : BILD_EHIP;
+}
