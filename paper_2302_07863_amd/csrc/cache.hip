@@ -416,7 +416,7 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
         a.r.span(i, first, count);
         nth = slot - (first >> c.page_shift) - 2 * i;
     } else {
-        const int per = ((a.r.rows - 1) >> c.page_shift) + 2;
+        const int per = ((a.r.rows + T - 2) >> c.page_shift) + 1;
         i = slot / per;
         nth = slot - i * per;
         a.r.span(i, first, count);
@@ -601,7 +601,7 @@ extern "C" int bild_cache_append(bild_cache* c, const bild_cache_append_call* ca
     const bild_cache_append_call& k = *call;
     if (!k.k || !k.v || k.reserved != 0 || !row_type(k.dtype) || k.layer < 0 || k.layer >= c->view.layers) return BILD_EINVAL;
     if (k.n < 1 || k.n > c->view.sequences || k.rows < 1 || (k.starts && k.tokens < 1)) return BILD_EINVAL;
-    const int64_t slots = k.starts ? (k.tokens >> c->view.page_shift) + 2 * (int64_t)k.n : k.n * (int64_t)(((k.rows - 1) >> c->view.page_shift) + 2);
+    const int64_t slots = k.starts ? (k.tokens >> c->view.page_shift) + 2 * (int64_t)k.n : k.n * ((((int64_t)k.rows + c->view.page_tokens - 2) >> c->view.page_shift) + 1);
     if ((!k.starts && (int64_t)k.n * k.rows > 0x7FFFFFFF) || slots > 0x7FFFFFFF) return BILD_EINVAL;
     const AppendArgs a = {c->view, {k.sequences, k.starts, k.n, k.rows, k.starts ? k.tokens : k.n * k.rows}, {k.k, k.v}, {k.k_token, k.v_token}, {k.k_head, k.v_head}, k.layer, c->words};
     const OnDevice on(c->device);

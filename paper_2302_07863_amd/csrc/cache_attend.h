@@ -1,0 +1,67 @@
+// What the kernels of bild_cache_attend share: cache_attend.hip (a few rows a sequence), cache_prompt.hip (prompts).
+#pragma once
+#include "cache.h"
+#include "rows_common.h"
+
+namespace bild {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+
+constexpr int kBlock = 32;     // keys of a step of the matrix cores' second product: a page has whole ones
+constexpr float kLn2 = 0.6931471805599453f;
+// Weights are powers of two relative to a maximum that is moved only when a score is beyond it by this much: they stay below 2^8, far from fp16's end.
+constexpr float kSlack = 8.f;
+
+struct AttendArgs {
+    CacheView c;
+    CacheRows r;
+    const void* q;
+    void* out;
+    float* lse;
+    int64_t q_token, q_head, out_token, out_head;
+    int layer, heads, group;
+    int window, sinks, causal;
+    float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
+    int prompt_from;      // rows of a sequence, times `group`, from which on it is the kernel for prompts'
+    int groups, least;  // workgroups of a key head; what one takes at least
+    float* part;
+    unsigned* arrived;
+};
+
+// Codes as fp16, times 2^-9: a byte permutation puts two codes ^ 0x80 where they are the bits of subnormals, (c + 128) 2^-24, and a packed product and sum, times 2^15 less 2^-2, makes them
+// c 2^-9: exact, an instruction a code.
+__device__ __forceinline__ f16x2 two(uint32_t x) {
+    const f16x2 by = {(_Float16)32768.f, (_Float16)32768.f}, off = {(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), by, off);
+}
+struct Halves {
+    f16x2 v[4];
+};
+__device__ __forceinline__ f16x8 eight(f16x2 a, f16x2 b, f16x2 c, f16x2 d) { return __builtin_bit_cast(f16x8, Halves{{a, b, c, d}}); }
+// eight codes (already ^ 0x80) side by side
+__device__ __forceinline__ f16x8 eight_of(uint32_t a, uint32_t b) {
+    return eight(two(__builtin_amdgcn_perm(0u, a, 0x0c010c00u)), two(__builtin_amdgcn_perm(0u, a, 0x0c030c02u)), two(__builtin_amdgcn_perm(0u, b, 0x0c010c00u)),
+                 two(__builtin_amdgcn_perm(0u, b, 0x0c030c02u)));
+}
+// byte k of two words
+__device__ __forceinline__ f16x2 pair_of(uint32_t a, uint32_t b, int k) { return two(__builtin_amdgcn_perm(b, a, 0x0c000c00u | (unsigned)(4 + k) << 16 | (unsigned)k)); }
+
+
+// Rows of q as fp16 times a power of two that puts the largest magnitude below 2^15 (0, infinities and NaN: 1).
+__device__ __forceinline__ int up_of(float big) {
+    int up = 0;
+    if (big > 0.f && big < INFINITY) {
+        frexpf(big, &up);
+        up = 15 - up;
+    }
+    return up;
+}
+
+hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st);
+hipError_t cache_prompt_init(int d_head);
+constexpr int kPromptRows = 128;  // of a tile of the kernel for prompts
+
+}  // namespace bild

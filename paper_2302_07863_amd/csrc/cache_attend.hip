@@ -4,8 +4,8 @@
 //
 // Bound, for a few rows a sequence: HBM, a byte a value, each key and value read once for all rows and query heads of its key head.  Sixteen such rows are one operand of the matrix
 // cores.  Scores come out transposed, S^T = K Q^T, so that a lane has eight consecutive keys of one row, which is what the second product, O^T = V^T P^T, takes from it: weights
-// go from one to the other in registers.  Codes become fp16 in one byte permutation for two (code ^ 0x80 as the bits of a subnormal) and one packed product and sum, for the values' transposition
-// into the bargain: the pairs that the permutation joins are two tokens' codes.  (c + 128) 2^-24 * 2^15 - 2^-2 = c 2^-9: every code is exact.  A page's scale is applied to
+// go from one to the other in registers.  Codes become fp16 by a byte permutation and a packed product and sum (cache_attend.h),
+// with the values' transposition into the bargain: the pairs that the permutation joins are two tokens' codes.  A page's scale is applied to
 // scores and to partial sums in fp32.
 //
 // Work is cut where it is: the 32-token blocks of all sequences and row tiles lie in one line, of which each workgroup of a key head takes an equal piece, wherever sequences begin or
@@ -16,58 +16,22 @@
 #include <cmath>
 #include <cstring>
 
-#include "cache.h"
+#include "cache_attend.h"
 #include "last_in.h"
-#include "rows_common.h"
 
 using namespace bild;
 
 namespace {
 
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kBlock = 32;     // keys of a step
 constexpr int kTile = 16;      // rows of a tile
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// Weights are powers of two relative to a maximum that is moved only when a score is beyond it by this much: they stay below 2^8, far from fp16's end.
-constexpr float kSlack = 8.f;
-
-struct AttendArgs {
-    CacheView c;
-    CacheRows r;
-    const void* q;
-    void* out;
-    float* lse;
-    int64_t q_token, q_head, out_token, out_head;
-    int layer, heads, group;
-    int window, sinks, causal;
-    float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
-    int groups, least;  // workgroups of a key head; blocks that one takes at least
-    float* part;
-    unsigned* arrived;
-};
+#ifndef START
+#define START 6
+#endif
+constexpr int kStart = START;
 
 // Floats of a row of partial results: the sums over the values, maximum, sum of weights.
 constexpr int part_row(int DP) { return DP + 4; }
-
-__device__ __forceinline__ f16x2 two(uint32_t x) {
-    const f16x2 by = {(_Float16)32768.f, (_Float16)32768.f}, off = {(_Float16)-0.25f, (_Float16)-0.25f};
-    return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), by, off);
-}
-struct Halves {
-    f16x2 v[4];
-};
-__device__ __forceinline__ f16x8 eight(f16x2 a, f16x2 b, f16x2 c, f16x2 d) { return __builtin_bit_cast(f16x8, Halves{{a, b, c, d}}); }
-// eight codes (already ^ 0x80) side by side
-__device__ __forceinline__ f16x8 eight_of(uint32_t a, uint32_t b) {
-    return eight(two(__builtin_amdgcn_perm(0u, a, 0x0c010c00u)), two(__builtin_amdgcn_perm(0u, a, 0x0c030c02u)), two(__builtin_amdgcn_perm(0u, b, 0x0c010c00u)),
-                 two(__builtin_amdgcn_perm(0u, b, 0x0c030c02u)));
-}
-// byte k of two words
-__device__ __forceinline__ f16x2 pair_of(uint32_t a, uint32_t b, int k) { return two(__builtin_amdgcn_perm(b, a, 0x0c000c00u | (unsigned)(4 + k) << 16 | (unsigned)k)); }
 
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
@@ -75,6 +39,8 @@ __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __built
 struct Seq {
     int s, first, count, length;  // which, its rows, its positions
     int tiles, sink_blocks, low_block, blocks;
+    // what a tile counts for in the line: its blocks, and as many as would be read while a workgroup gets there and joins what its waves have
+    __device__ int cost() const { return blocks + kStart; }
 };
 __device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
     Seq q;
@@ -82,7 +48,8 @@ __device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
     a.r.span(i, q.first, q.count);
     if (q.s < 0) q.count = 0;
     q.length = q.s < 0 ? 0 : min(max(a.c.lengths[q.s], 0), a.c.cap());
-    q.tiles = (int)(((int64_t)q.count * a.group + kTile - 1) / kTile);
+    const int64_t rows = (int64_t)q.count * a.group;
+    q.tiles = rows < a.prompt_from ? (int)((rows + kTile - 1) / kTile) : 0;
     q.low_block = a.window ? max(q.length - q.count - a.window + 1, 0) / kBlock : 0;
     q.sink_blocks = a.window ? min((int)(((int64_t)a.sinks + kBlock - 1) / kBlock), q.low_block) : 0;
     q.blocks = max(q.sink_blocks + (q.length + kBlock - 1) / kBlock - q.low_block, 1);  // (one that has none is written all the same)
@@ -106,6 +73,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
     __shared__ float tops[kWaves * kTile], weights[kWaves * kTile];
     __shared__ long long scan_sums[kWaves];
     __shared__ int found;
+    __shared__ Seq found_seq;
     __shared__ long long found_at;
     __shared__ unsigned share;
     const CacheView& c = a.c;
@@ -117,9 +85,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
     {
         const int per = (a.r.n + kThreads - 1) / kThreads, i0 = min(tid * per, a.r.n), i1 = min(i0 + per, a.r.n);
         long long mine = 0;
+        Seq last;
         for (int i = i0; i < i1; ++i) {
-            const Seq q = sequence_at(a, i);
-            mine += (long long)q.tiles * q.blocks;
+            last = sequence_at(a, i);
+            mine += (long long)last.tiles * last.cost();
         }
         long long x = mine;
 #pragma unroll
@@ -142,13 +111,16 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
         if (w0 >= line) return;
         if (before <= w0 && w0 < before + mine) {
             int i = i0;
-            for (;; ++i) {
-                const Seq q = sequence_at(a, i);
-                const long long next = before + (long long)q.tiles * q.blocks;
-                if (w0 < next) break;
-                before = next;
-            }
+            Seq q = last;
+            if (per > 1)
+                for (;; ++i) {
+                    q = sequence_at(a, i);
+                    const long long next = before + (long long)q.tiles * q.cost();
+                    if (w0 < next) break;
+                    before = next;
+                }
             found = i;
+            found_seq = q;
             found_at = before;
         }
         __syncthreads();
@@ -156,50 +128,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
     const long long chunk = max((line + a.groups - 1) / a.groups, (long long)a.least);
     int i = __builtin_amdgcn_readfirstlane(found);
     long long at = found_at;
-    Seq sq = sequence_at(a, i);
+    Seq sq = found_seq;
 
     for (long long w = w0; w < w1;) {
-        while (w >= at + (long long)sq.tiles * sq.blocks) {
-            at += (long long)sq.tiles * sq.blocks;
+        while (w >= at + (long long)sq.tiles * sq.cost()) {
+            at += (long long)sq.tiles * sq.cost();
             sq = sequence_at(a, ++i);
         }
-        const int tile = (int)((w - at) / sq.blocks), b0 = (int)((w - at) - (long long)tile * sq.blocks), b1 = (int)min((long long)sq.blocks, b0 + (w1 - w));
-        const long long unit = at + (long long)tile * sq.blocks;  // where the tile begins
+        const int cost = sq.cost(), tile = (int)((w - at) / cost), c0 = (int)((w - at) - (long long)tile * cost), c1 = (int)min((long long)cost, c0 + (w1 - w));
+        const long long unit = at + (long long)tile * cost;  // where the tile begins
+        const int b0 = (int)((long long)c0 * sq.blocks / cost), b1 = (int)((long long)c1 * sq.blocks / cost);
         // ---- rows
         const int rows = sq.count * a.group, idx = tile * kTile + n16, mine = min(idx, rows - 1), j = mine / a.group, e = mine - j * a.group;
         const int pos = a.causal ? sq.length - sq.count + j : sq.length - 1, low = a.window ? pos - a.window : -1;
-        f16x8 q[TERMS][KS];
-        float row_scale;
-        {
-            const V* x = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
-            RowVec<R, 8> raw[KS];
-            float big = 0.f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
-                raw[s].load(x + off);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) big = fmaxf(big, off + t >= begin ? fabsf(R::up(raw[s].v[t])) : 0.f);
-            }
-            big = quad_rows_max(big);
-            int up = 0;
-            if (big > 0.f && big < INFINITY) {
-                frexpf(big, &up);
-                up = 15 - up;
-            }
-            row_scale = ldexpf(1.f, -up);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    // (a piece behind the head's end begins earlier, and what another lane has as well is 0 here)
-                    const float v = off + t >= begin ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
-                    q[0][s][t] = (_Float16)v;
-                    if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
-                }
-            }
-        }
         // the positions that the tile's rows see
         const int j0 = tile * kTile / a.group, j1 = min((tile * kTile + kTile - 1) / a.group, sq.count - 1);
         const int first_pos = a.causal ? sq.length - sq.count + j0 : sq.length - 1, last_pos = a.causal ? sq.length - sq.count + j1 : sq.length - 1;
@@ -218,6 +159,35 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
                 v_scale = c.scales[c.plane(pages, a.layer, 1, head)] * (512.f / 127.f);
             }
         };
+        if (b0 + wave < b1) look_up(b0 + wave);
+        f16x8 q[TERMS][KS];
+        float row_scale;
+        {
+            const V* x = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
+            RowVec<R, 8> raw[KS];
+            float big = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
+                raw[s].load(x + off);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) big = fmaxf(big, off + t >= begin ? fabsf(R::up(raw[s].v[t])) : 0.f);
+            }
+            big = quad_rows_max(big);
+            const int up = up_of(big);
+            row_scale = ldexpf(1.f, -up);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    // (a piece behind the head's end begins earlier, and what another lane has as well is 0 here)
+                    const float v = off + t >= begin ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
+                    q[0][s][t] = (_Float16)v;
+                    if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
+                }
+            }
+        }
         float top = -INFINITY, sum = 0.f;
         f32x4 acc[NJ];
 #pragma unroll
@@ -315,7 +285,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
         };
         // ---- the wave's blocks, the next one's codes on their way
         Codes<DP> one, other;
-        int nth = 64, b = b0 + wave - kWaves;  // of the looked up ones
+        int nth = 0, b = b0 + wave - kWaves;  // of the looked up ones
         struct Next {
             int blk;  // -1: no more
             float ks, vs;
@@ -327,13 +297,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
                     look_up(b);
                     nth = 0;
                 }
-                const int page = __builtin_amdgcn_readlane(pages, nth);
-                r.ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k_scale), nth));
-                r.vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v_scale), nth));
-                ++nth;
+                const int page = __builtin_amdgcn_readlane(pages, nth), was = nth++;
                 if (page >= 0) {
                     r.blk = block_at(b);
                     load(x, page, r.blk);
+                    // (the scales were asked for before: whoever waits for them does not wait for these codes)
+                    r.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), was));
+                    r.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), was));
                     break;
                 }
             }
@@ -386,13 +356,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
             if (col < d) y.store(out + min(col, d - NJ));  // (a last piece that is cut begins earlier, as its loads did: the lane before writes the same there)
             if (a.lse && col == 0) a.lse[t_at * a.heads + h] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
         };
-        const bool whole = b0 == 0 && b1 == sq.blocks;
+        const bool whole = c0 == 0 && c1 == cost;
         if (whole) {
             if (slot < valid) put(slot);
             __syncthreads();
         } else {
             // the workgroups that share the tile: in the first of them it begins last, in the others first
-            const int from = (int)(unit / chunk), to = (int)((unit + sq.blocks - 1) / chunk);
+            const int from = (int)(unit / chunk), to = (int)((unit + cost - 1) / chunk);
             constexpr int kRow = part_row(DP);
             const int64_t place = ((int64_t)head * a.groups + blockIdx.x) * 2 + (blockIdx.x == from);
             const auto mem = make_rsrc(a.part + place * kTile * kRow, sizeof(float) * kTile * kRow);
@@ -445,9 +415,12 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
             }
             __syncthreads();
         }
-        w += b1 - b0;
+        w += c1 - c0;
     }
 }
+
+// Rows (times query heads of a key head) of a sequence, and tiles in all, from which on prompts take the kernel made for them.
+constexpr int kPromptFrom = 64, kPromptTiles = 128;
 
 constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
 
@@ -466,6 +439,7 @@ namespace bild {
 
 hipError_t attend_init(int d_head) {
     const void* const wide[] = {(const void*)cache_attend_kernel<RowF32, 256>, (const void*)cache_attend_kernel<RowBf16, 256>, (const void*)cache_attend_kernel<RowF16, 256>};
+    if (const hipError_t e = cache_prompt_init(d_head); e != hipSuccess) return e;
     return d_head <= 128 ? hipSuccess : raise_lds_limit(wide, (int)lds_bytes(256));
 }
 
@@ -503,12 +477,21 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     a.causal = k.causal;
     a.scale = (float)((double)k.scale * 1.4426950408889634 * 512.0 / 127.0);
     a.groups = attend_groups(v.heads);
-    a.least = 8;
+#ifndef LEAST
+#define LEAST 8
+#endif
+    a.least = LEAST + kStart;
+    // (fewer tiles than the chip has room for leave it empty: their keys are cut into pieces instead)
+    const int64_t tiles = k.starts ? tokens * a.group / kPromptRows + k.n : k.n * (((int64_t)k.rows * a.group + kPromptRows - 1) / kPromptRows);
+    const bool prompts = (int64_t)k.rows * a.group >= kPromptFrom && tokens * a.group / kPromptRows * v.heads >= kPromptTiles;
+    a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;
     a.part = c->part;
     a.arrived = c->arrived;
     const OnDevice on(c->device);
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (prompts && launch_cache_prompt(a, k.dtype, tiles, st) != hipSuccess) return BILD_EHIP;
+    if (prompts && (!k.starts || k.n == 1)) return BILD_OK;  // (all are prompts)
     const hipError_t err = k.dtype == BILD_DT_F32 ? launch<RowF32>(a, st) : k.dtype == BILD_DT_BF16 ? launch<RowBf16>(a, st) : launch<RowF16>(a, st);
     return err == hipSuccess ? BILD_OK : BILD_EHIP;
 }

@@ -1,0 +1,336 @@
+// Attention of prompts over the cache in 8 bits (bild_cache_attend): sequences with many rows.
+//
+// Bound: the matrix cores, and beside them the exponentials.  A workgroup has 128 rows (rows times the query heads of a key head) of a sequence and walks over its keys, 64 at a time: their codes
+// come from memory into registers while the tile before is multiplied, become fp16 on their way into LDS (once for all rows), the values transposed.  A wave has 32 rows; scores come out as
+// S^T = K Q^T, so that weights stay in registers as the operand of O^T = V^T P^T: lane l has row l % 32 and of each 16 keys the eight of its half, and the values lie in LDS in that order of keys.
+// Chunks of 16 bytes are swapped within a row of LDS by the row's number, so that neither product's reads meet in a bank.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "cache_attend.h"
+
+using namespace bild;
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kThreads = 256, kKeys = 64;
+
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float max_xor32(float v) {
+    uint32_t a, b;
+    pair_xor32(__float_as_uint(v), a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+
+// PAGES: pages of a tile of keys.
+template <class R, int DP, int PAGES>
+__global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1 : 2) void cache_prompt_kernel(const AttendArgs a) {
+    constexpr bool TWO = R::kDtype == BILD_DT_F32;
+    constexpr int TERMS = TWO ? 2 : 1, QS = DP / 16, ND = DP / 32, KC = DP / 64, VI = (DP + 127) / 128, ROWC = DP / 8;
+    constexpr int kBuffer = 2 * kKeys * DP;  // fp16 values of a tile's keys and values
+    typedef typename R::type V;
+    extern __shared__ __attribute__((aligned(16))) _Float16 lds[];  // two buffers: keys [64][DP], values [DP][64]
+    const CacheView& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n32 = lane & 31, half = lane >> 5, d = c.d_head;
+    const int head = blockIdx.x % c.heads;  // (dies take workgroups in turn: those of a head have its keys in few L2s)
+    // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles; the last rows, which see most, come first
+    int i, first, count, tile;
+    {
+        const int slot = (int)((gridDim.x - 1 - blockIdx.x) / c.heads);
+        if (a.r.starts) {
+            int lo = 0, hi = a.r.n;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                a.r.span(mid, first, count);
+                if ((int)((int64_t)first * a.group / kPromptRows) + mid <= slot) lo = mid; else hi = mid;
+            }
+            i = lo;
+            a.r.span(i, first, count);
+            tile = slot - (int)((int64_t)first * a.group / kPromptRows) - i;
+        } else {
+            const int per = (int)(((int64_t)a.r.rows * a.group + kPromptRows - 1) / kPromptRows);
+            i = slot / per;
+            tile = slot - i * per;
+            a.r.span(i, first, count);
+        }
+    }
+    const int rows = count * a.group;
+    if (tile < 0 || tile * kPromptRows >= rows || rows < a.prompt_from) return;
+    const int s = a.r.sequence(i, c.sequences);
+    if (s < 0) return;
+    const int length = min(max(c.lengths[s], 0), c.cap());
+    const int idx0 = tile * kPromptRows + wave * 32, idx = min(idx0 + n32, rows - 1), j = idx / a.group, e = idx - j * a.group;
+    const auto pos_of = [&](int at) { return a.causal ? length - count + at : length - 1; };
+    const int pos = pos_of(j), low = a.window ? pos - a.window : -1;
+    // ---- the keys that any row of the tile sees, in tiles
+    const int wg_first = pos_of(tile * kPromptRows / a.group), wg_last = pos_of(min(tile * kPromptRows + kPromptRows - 1, rows - 1) / a.group);
+    const int low_tile = a.window ? max(wg_first - a.window + 1, 0) / kKeys : 0;
+    const int sink_tiles = a.window ? min((int)(((int64_t)a.sinks + kKeys - 1) / kKeys), low_tile) : 0;
+    const int tiles = sink_tiles + max((min(wg_last + 1, length) + kKeys - 1) / kKeys - low_tile, 0);
+    const auto tile_at = [&](int t) { return t < sink_tiles ? t : t - sink_tiles + low_tile; };
+    // (of the wave's rows)
+    const int first_pos = pos_of(min(idx0, rows - 1) / a.group), last_pos = pos_of(min(idx0 + 31, rows - 1) / a.group);
+
+    // ---- pages and scales of the next 64 tiles, a lane a tile
+    int pages[PAGES];
+    float k_scale[PAGES], v_scale[PAGES];
+    const auto look_up = [&](int t0) {
+        const int t = t0 + lane, key0 = tile_at(t) * kKeys;
+#pragma unroll
+        for (int p = 0; p < PAGES; ++p) {
+            const int k0 = key0 + p * kBlock;
+            pages[p] = -1;
+            k_scale[p] = v_scale[p] = 0.f;
+            if (t < tiles && k0 < length) pages[p] = c.table[(int64_t)s * c.max_pages + (k0 >> c.page_shift)];
+            if (!c.has(pages[p])) pages[p] = -1;
+            if (pages[p] >= 0) {
+                k_scale[p] = c.scales[c.plane(pages[p], a.layer, 0, head)];
+                v_scale[p] = c.scales[c.plane(pages[p], a.layer, 1, head)] * (512.f / 127.f);
+            }
+        }
+    };
+    look_up(0);
+    // ---- rows
+    f16x8 q[TERMS][QS];
+    float row_scale;
+    {
+        const V* x = (const V*)a.q + (int64_t)(first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
+        RowVec<R, 8> raw[QS];
+        float big = 0.f;
+#pragma unroll
+        for (int t = 0; t < QS; ++t) {
+            const int begin = 16 * t + 8 * half;
+            raw[t].load(x + min(begin, d - 8));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) big = fmaxf(big, begin < d ? fabsf(R::up(raw[t].v[u])) : 0.f);
+        }
+        big = max_xor32(big);
+        const int up = up_of(big);
+        row_scale = ldexpf(fabsf(a.scale), -up);
+#pragma unroll
+        for (int t = 0; t < QS; ++t)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                // (the scale's sign goes into the rows: what scores are multiplied by is not negative)
+                const float y = 16 * t + 8 * half < d ? ldexpf(R::up(raw[t].v[u]), up) : 0.f, v = a.scale < 0.f ? -y : y;
+                q[0][t][u] = (_Float16)v;
+                if (TWO) q[TERMS - 1][t][u] = (_Float16)(v - (float)q[0][t][u]);
+            }
+    }
+
+    // ---- codes on their way from memory to LDS
+    u32x4 kc[KC];
+    uint32_t vc[VI][8];
+    const auto request = [&](int t) {  // (looked up; a page that is not there: any that is in the pool, and no weight)
+        const int key0 = tile_at(t) * kKeys;
+#pragma unroll
+        for (int u = 0; u < KC; ++u) {
+            const int item = u * kThreads + tid, key = item / (DP / 16), ch = item % (DP / 16);
+            int page = __builtin_amdgcn_readlane(pages[0], t & 63);
+            if (PAGES == 2 && key >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], t & 63);
+            const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 0, head) * c.plane_bytes() + ((key0 + key) & (c.page_tokens - 1)) * d + min(16 * ch, d - 16);
+            kc[u] = __builtin_bit_cast(u32x4, *(const Piece<16, 8>*)from);
+        }
+#pragma unroll
+        for (int u = 0; u < VI; ++u) {
+            const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4);
+            if (group >= 8) continue;
+            const int k0 = 16 * (group >> 1) + 4 * (group & 1);
+            int page = __builtin_amdgcn_readlane(pages[0], t & 63);
+            if (PAGES == 2 && k0 >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], t & 63);
+            const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 1, head) * c.plane_bytes() + ((key0 + k0) & (c.page_tokens - 1)) * d + min(4 * dg, d - 4);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) vc[u][y] = *(const uint32_t*)(from + ((y & 3) + 8 * (y >> 2)) * d);
+        }
+    };
+    const auto k_at = [&](int key, int ch) { return key * DP + 8 * (ch ^ (DP == 64 ? (key >> 1) & 7 : key & 15)); };
+    const auto v_at = [&](int dim, int ch) { return kKeys * DP + dim * kKeys + 8 * (ch ^ ((dim >> 1) & 7)); };
+    const auto deliver = [&](int buffer) {
+        _Float16* to = lds + buffer * kBuffer;
+#pragma unroll
+        for (int u = 0; u < KC; ++u) {
+            const int item = u * kThreads + tid, key = item / (DP / 16), ch = item % (DP / 16);
+            const u32x4 y = kc[u] ^ 0x80808080u;
+            const bool cut = 16 * ch > d - 16;  // (a last piece that is half as long begins earlier: what belongs in its place is its second half)
+            *(f16x8*)(to + k_at(key, 2 * ch)) = eight_of(cut ? y[2] : y[0], cut ? y[3] : y[1]);
+            *(f16x8*)(to + k_at(key, 2 * ch + 1)) = eight_of(y[2], y[3]);
+        }
+#pragma unroll
+        for (int u = 0; u < VI; ++u) {
+            const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4);
+            if (group >= 8) continue;
+            uint32_t y[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z) y[z] = vc[u][z] ^ 0x80808080u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *(f16x8*)(to + v_at(4 * dg + k, group)) = eight(pair_of(y[0], y[1], k), pair_of(y[2], y[3], k), pair_of(y[4], y[5], k), pair_of(y[6], y[7], k));
+        }
+    };
+
+    float top = -INFINITY, sum = 0.f;
+    f32x16 acc[ND];
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+    if (tiles > 0) {
+        request(0);
+        deliver(0);
+    }
+    lds_barrier();
+    for (int t = 0; t < tiles; ++t) {
+        const int key0 = tile_at(t) * kKeys;
+        bool there[PAGES];
+        float ks[PAGES], vs[PAGES];
+#pragma unroll
+        for (int p = 0; p < PAGES; ++p) {
+            there[p] = __builtin_amdgcn_readlane(pages[p], t & 63) >= 0;
+            ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale[p]), t & 63));
+            vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale[p]), t & 63));
+        }
+        if (t + 1 < tiles) {
+            if (((t + 1) & 63) == 0) look_up(t + 1);
+            request(t + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const _Float16* at = lds + (t & 1) * kBuffer;
+        const bool seen = key0 <= last_pos && (!a.window || key0 + kKeys - 1 > first_pos - a.window || key0 < a.sinks) && (there[0] || there[PAGES - 1]);
+        if (seen) {
+            f32x16 z[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[m][r] = 0.f;
+#pragma unroll
+                for (int u = 0; u < QS; ++u) {
+                    const f16x8 k = *(const f16x8*)(at + k_at(32 * m + n32, 2 * u + half));
+#pragma unroll
+                    for (int w = 0; w < TERMS; ++w) z[m] = mma(k, q[w][u], z[m]);
+                }
+            }
+            const bool full = key0 + kKeys - 1 <= first_pos && (!a.window || key0 > last_pos - a.window || key0 + kKeys <= a.sinks) && there[0] && there[PAGES - 1];
+            float big = -INFINITY, by[2] = {ks[0] * row_scale, ks[PAGES - 1] * row_scale};
+            if (full) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    float most = z[m][0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) most = fmaxf(most, z[m][r]);
+                    big = fmaxf(big, most * by[m]);
+                }
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = key0 + 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
+                        const bool sees = key <= pos && (key > low || key < a.sinks) && there[m * (PAGES - 1)];
+                        z[m][r] = sees ? z[m][r] * by[m] : -INFINITY;
+                        big = fmaxf(big, z[m][r]);
+                    }
+                by[0] = by[1] = 1.f;
+            }
+            big = max_xor32(big);
+            if (__any(big > top + kSlack)) {
+                const float now = big > top + kSlack ? big : top, less = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                sum *= less;
+#pragma unroll
+                for (int u = 0; u < ND; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[u][r] *= less;
+                top = now;
+            }
+            const float base = top == -INFINITY ? 0.f : top;
+            f16x8 w[TERMS][4];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[m][r], by[m], -base));
+                    sum += p;
+                    const int st = 2 * m + (r >> 3), u = r & 7;
+                    w[0][st][u] = (_Float16)p;
+                    if (TWO) w[TERMS - 1][st][u] = (_Float16)(p - (float)w[0][st][u]);
+                }
+#pragma unroll
+            for (int u = 0; u < ND; ++u) {
+                f32x16 part;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) part[r] = 0.f;
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const f16x8 v = *(const f16x8*)(at + v_at(32 * u + n32, 2 * st + half));
+#pragma unroll
+                    for (int x = 0; x < TERMS; ++x) part = mma(v, w[x][st], part);
+                    if (PAGES == 2 && st == 1) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            acc[u][r] = __builtin_fmaf(part[r], vs[0], acc[u][r]);
+                            part[r] = 0.f;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[u][r] = __builtin_fmaf(part[r], vs[PAGES - 1], acc[u][r]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 < tiles) deliver((t + 1) & 1);
+        lds_barrier();
+    }
+    // ---- results
+    uint32_t x, y;
+    pair_xor32(__float_as_uint(sum), x, y);
+    sum = __uint_as_float(x) + __uint_as_float(y);
+    if (idx0 + n32 >= rows) return;
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    const int h = head * a.group + e;
+    V* out = (V*)a.out + (int64_t)(first + j) * a.out_token + (int64_t)h * a.out_head;
+#pragma unroll
+    for (int u = 0; u < ND; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int dim = 32 * u + 2 * r + 4 * half;
+            RowVec<R, 4> o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o.v[k] = R::down(acc[u][r + k] * by);
+            if (dim < d) o.store(out + dim);
+        }
+    if (a.lse && half == 0) a.lse[(int64_t)(first + j) * a.heads + h] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+}
+
+constexpr size_t lds_bytes(int DP) { return (size_t)2 * 2 * kKeys * DP * 2; }
+
+template <class R, int DP>
+hipError_t launch(const AttendArgs& a, dim3 grid, hipStream_t st) {
+    return a.c.page_tokens == 32 ? launch_on(cache_prompt_kernel<R, DP, 2>, grid, dim3(kThreads), lds_bytes(DP), st, a)
+                                 : launch_on(cache_prompt_kernel<R, DP, 1>, grid, dim3(kThreads), lds_bytes(DP), st, a);
+}
+template <class R>
+hipError_t launch(const AttendArgs& a, dim3 grid, hipStream_t st) {
+    return a.c.d_head <= 64 ? launch<R, 64>(a, grid, st) : a.c.d_head <= 128 ? launch<R, 128>(a, grid, st) : launch<R, 256>(a, grid, st);
+}
+
+}  // namespace
+
+namespace bild {
+
+hipError_t cache_prompt_init(int d_head) {
+    const void* const half[] = {(const void*)cache_prompt_kernel<RowF32, 128, 1>, (const void*)cache_prompt_kernel<RowBf16, 128, 1>, (const void*)cache_prompt_kernel<RowF16, 128, 1>,
+                                (const void*)cache_prompt_kernel<RowF32, 128, 2>, (const void*)cache_prompt_kernel<RowBf16, 128, 2>, (const void*)cache_prompt_kernel<RowF16, 128, 2>};
+    const void* const full[] = {(const void*)cache_prompt_kernel<RowF32, 256, 1>, (const void*)cache_prompt_kernel<RowBf16, 256, 1>, (const void*)cache_prompt_kernel<RowF16, 256, 1>,
+                                (const void*)cache_prompt_kernel<RowF32, 256, 2>, (const void*)cache_prompt_kernel<RowBf16, 256, 2>, (const void*)cache_prompt_kernel<RowF16, 256, 2>};
+    return d_head <= 64 ? hipSuccess : d_head <= 128 ? raise_lds_limit(half, (int)lds_bytes(128)) : raise_lds_limit(full, (int)lds_bytes(256));
+}
+
+hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st) {
+    const dim3 grid((unsigned)(a.c.heads * tiles));
+    return dtype == BILD_DT_F32 ? launch<RowF32>(a, grid, st) : dtype == BILD_DT_BF16 ? launch<RowBf16>(a, grid, st) : launch<RowF16>(a, grid, st);
+}
+
+}  // namespace bild

@@ -8,7 +8,7 @@ import paper_2302_07863_amd as pkg
 from paper_2302_07863_amd import binding as b
 from tests.cached import Held, Oracle, invariants, values
 from tests.hipmem import DeviceArray
-from tests.rows import BF16, F16, F32, Graph, Rows, Stream, close, unpack
+from tests.rows import BF16, F16, F32, Graph, Rows, Stream, close, pack, unpack
 
 pytestmark = pytest.mark.gpu
 
@@ -270,6 +270,46 @@ def test_prompts(d, group, dtype, rows):
     attend(t, rng, 0, [rows, 3], group, dtype, window=70, sinks=4)
 
 
+@pytest.mark.parametrize("page", [32, 64, 128])
+@pytest.mark.parametrize("d,dtype", [(128, BF16), (64, F16), (80, BF16), (72, F32), (256, F16), (136, BF16), (248, F32), (16, F16), (128, F32)])
+def test_prompts_that_fill_the_chip(page, d, dtype):
+    """Rows times query heads that are not whole tiles, cached positions in front, a window whose sinks end inside a tile of keys."""
+    t, rng = filled(page + d, [190, 77], pages=16, page=page, heads=16, d=d, max_pages=7)
+    attend(t, rng, 0, [133], 8, dtype, sequences=[0], scale=-0.1 if d == 80 else None)
+    attend(t, rng, 0, [77, 61], 8, dtype, sequences=[1, 0], window=50, sinks=37)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 1), (300, 0), (130, 100)])
+def test_prompts_between_single_rows(window, sinks):
+    """Ragged: prompts, single rows, none, sequences that are not there, lengths shorter than the rows."""
+    lengths = [700, 40, 1, 0, 333, 90, 257]
+    t, rng = filled(31, lengths, pages=60, page=64, heads=8, d=64, max_pages=12)
+    attend(t, rng, 0, [520, 1, 1, 1, 12, 99, 0], 4, BF16, window=window, sinks=sinks)
+    # (of a page that is not there nothing counts)
+    t.o.table[0, 3], t.o.table[0, 8], t.o.table[5, 0] = -1, 99999, -5
+    t = Held(t.o)
+    attend(t, rng, 0, [520, 1, 1, 1, 12, 99, 0], 4, F16, window=window, sinks=sinks)
+    if not window:
+        attend(t, rng, 0, [300, 1, 2, 0, 64, 90, 3], 4, F32, causal=False)
+
+
+def test_prompts_with_rows_that_are_not_finite():
+    t, rng = filled(32, [200], pages=10, d=64, heads=16)
+    words, x = values(rng, (200, 128 * 64), BF16)
+    x = x.astype(np.float64).reshape(200, 128, 64)
+    bad = np.zeros((200, 128), bool)
+    for r, h, v in ((0, 0, np.nan), (77, 5, np.inf), (130, 127, -np.inf)):
+        words.reshape(200, 128, 64)[r, h, 9] = pack(np.float32([v]), BF16)[0]
+        bad[r, h] = True
+        x[r, h] = 0
+    q, out = Rows(words), Rows(np.zeros_like(words))
+    t.cache.attend(0, BF16, 1, 200, 128, q.ptr, out.ptr, 0.125)
+    want, _, tol, _ = t.o.attend(0, x, [200], 0.125, dtype=BF16)
+    got = unpack(out.get(), BF16).reshape(200, 128, 64)
+    assert np.all(np.isnan(got[bad]))
+    close(got[~bad], want[~bad], tol[~bad])
+
+
 def test_without_order():
     t, rng = filled(4, [100, 1, 0, 250], pages=30, d=64)
     for dtype in (F32, BF16):
@@ -308,7 +348,6 @@ def test_pages_that_are_not_there_count_for_nobody():
 def test_a_row_that_is_not_finite_leaves_the_others_alone(dtype, bad):
     t, rng = filled(9, [100], pages=30, d=64, heads=1)
     words, x = values(rng, (4, 2 * 64), dtype)
-    from tests.rows import pack
     words[1, 5] = pack(np.float32([bad]), dtype)[0]
     q, out, lse = Rows(words), Rows(np.zeros_like(words)), Rows(np.zeros((4, 2), np.float32))
     t.cache.attend(0, dtype, 1, 4, 2, q.ptr, out.ptr, 0.125, lse=lse.ptr)
