@@ -36,6 +36,7 @@ UNITS = [
     ("rules.hip", "rules.o", []),
     ("cache.hip", "cache.o", []),
     ("cache_attend.hip", "cache_attend.o", []),
+    ("cache_attend_tall.hip", "cache_attend_tall.o", []),
     ("cache_prompt.hip", "cache_prompt.o", []),
     ("beams.hip", "beams.o", []),
     ("layout.cpp", "layout.o", []),

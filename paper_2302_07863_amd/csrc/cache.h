@@ -60,7 +60,10 @@ struct bild_cache {
 
 namespace bild {
 
-constexpr int kAttendGroups = 512;                       // workgroups of a launch, but for one a key head
+#ifndef GROUPS
+#define GROUPS 256
+#endif
+constexpr int kAttendGroups = GROUPS;                       // workgroups of a launch, but for one a key head
 inline int attend_groups(int heads) { return (kAttendGroups + heads - 1) / heads; }  // of a key head
 hipError_t attend_init(int d_head);                      // what its kernels need of the current device
 size_t attend_part_floats(int heads, int d_head);        // of bild_cache::part

@@ -7,6 +7,7 @@ namespace bild {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 
@@ -60,6 +61,40 @@ __device__ __forceinline__ int up_of(float big) {
     return up;
 }
 
+constexpr int kTile = 16;      // rows of a tile of the kernels for few rows
+#ifndef START
+#define START 6
+#endif
+constexpr int kStart = START;
+
+// A sequence's share of the work.
+struct Seq {
+    int s, first, count, length;  // which, its rows, its positions
+    int tiles, sink_blocks, low_block, blocks;
+    // what a tile counts for in the line: its blocks, and as many as would be read while a workgroup gets there and joins what its waves have
+    __device__ int cost() const { return blocks + kStart; }
+};
+__device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
+    Seq q;
+    q.s = a.r.sequence(i, a.c.sequences);
+    a.r.span(i, q.first, q.count);
+    if (q.s < 0) q.count = 0;
+    q.length = q.s < 0 ? 0 : min(max(a.c.lengths[q.s], 0), a.c.cap());
+    const int64_t rows = (int64_t)q.count * a.group;
+    q.tiles = rows < a.prompt_from ? (int)((rows + kTile - 1) / kTile) : 0;
+    q.low_block = a.window ? max(q.length - q.count - a.window + 1, 0) / kBlock : 0;
+    q.sink_blocks = a.window ? min((int)(((int64_t)a.sinks + kBlock - 1) / kBlock), q.low_block) : 0;
+    q.blocks = max(q.sink_blocks + (q.length + kBlock - 1) / kBlock - q.low_block, 1);  // (one that has none is written all the same)
+    return q;
+}
+
+// Floats of a row of partial results: the sums over the values, maximum, sum of weights.
+constexpr int part_row(int DP) { return DP + 4; }
+
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+hipError_t launch_cache_attend_tall(const AttendArgs& a, int dtype, hipStream_t st);  // heads above 128
+hipError_t cache_attend_tall_init();
 hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st);
 hipError_t cache_prompt_init(int d_head);
 constexpr int kPromptRows = 128;  // of a tile of the kernel for prompts

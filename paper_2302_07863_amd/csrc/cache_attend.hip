@@ -23,37 +23,18 @@ using namespace bild;
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kTile = 16;      // rows of a tile
-#ifndef START
-#define START 6
-#endif
-constexpr int kStart = START;
+// (twice as many workgroups of half as many waves have twice as many parts to join)
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
-// Floats of a row of partial results: the sums over the values, maximum, sum of weights.
-constexpr int part_row(int DP) { return DP + 4; }
+// (quotients of what is uniform and nearly always below 2^32: a 64-bit division is a hundred instructions)
+__device__ __forceinline__ int quotient(long long a, long long b) {
+    return a < (1ll << 32) && b < (1ll << 32) ? (int)((uint32_t)a / (uint32_t)b) : (int)(a / b);
+}
 
-__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
-// A sequence's share of the work.
-struct Seq {
-    int s, first, count, length;  // which, its rows, its positions
-    int tiles, sink_blocks, low_block, blocks;
-    // what a tile counts for in the line: its blocks, and as many as would be read while a workgroup gets there and joins what its waves have
-    __device__ int cost() const { return blocks + kStart; }
-};
-__device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
-    Seq q;
-    q.s = a.r.sequence(i, a.c.sequences);
-    a.r.span(i, q.first, q.count);
-    if (q.s < 0) q.count = 0;
-    q.length = q.s < 0 ? 0 : min(max(a.c.lengths[q.s], 0), a.c.cap());
-    const int64_t rows = (int64_t)q.count * a.group;
-    q.tiles = rows < a.prompt_from ? (int)((rows + kTile - 1) / kTile) : 0;
-    q.low_block = a.window ? max(q.length - q.count - a.window + 1, 0) / kBlock : 0;
-    q.sink_blocks = a.window ? min((int)(((int64_t)a.sinks + kBlock - 1) / kBlock), q.low_block) : 0;
-    q.blocks = max(q.sink_blocks + (q.length + kBlock - 1) / kBlock - q.low_block, 1);  // (one that has none is written all the same)
-    return q;
+// A lane's value, for all of them: what the work is cut by has to be known to be the same in all lanes, or every load of codes would be a loop over the bases it might have.
+__device__ __forceinline__ long long lane_of(long long x, int lane) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane);
+    return (long long)((uint64_t)hi << 32 | lo);
 }
 
 // Registers of a block's codes.
@@ -64,38 +45,92 @@ struct Codes {
     uint32_t v[8][WV];  // eight values, NJ codes of each
 };
 
+template <int N>
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t mem, int off, const float (&o)[N]) {
+    if constexpr (N == 2) {
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(o[0]), __float_as_uint(o[1])}, mem, off, 0, kPartAux);
+    } else {
+#pragma unroll
+        for (int t = 0; t < N; t += 4)
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[t]), __float_as_uint(o[t + 1]), __float_as_uint(o[t + 2]), __float_as_uint(o[t + 3])}, mem, off + 4 * t, 0, kPartAux);
+    }
+}
+template <int N>
+__device__ __forceinline__ void get_part(__amdgpu_buffer_rsrc_t mem, int off, float (&o)[N]) {
+    if constexpr (N == 2) {
+        const auto y = __builtin_amdgcn_raw_buffer_load_b64(mem, off, 0, kPartAux);
+        o[0] = __uint_as_float(y[0]);
+        o[1] = __uint_as_float(y[1]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < N; t += 4) {
+            const auto y = __builtin_amdgcn_raw_buffer_load_b128(mem, off + 4 * t, 0, kPartAux);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[t + u] = __uint_as_float(y[u]);
+        }
+    }
+}
+
 template <class R, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendArgs a) {
     constexpr bool TWO = R::kDtype == BILD_DT_F32;  // rows and weights in two fp16 parts
     constexpr int NK = DP / 64, KS = DP / 32, NJ = DP / 16, WV = NJ / 4, TERMS = TWO ? 2 : 1, LD = DP + 4;
+    constexpr int kCols = kThreads / kTile, NC = DP / kCols;  // threads of a row of results, columns of each
     typedef typename R::type V;
-    extern __shared__ __attribute__((aligned(16))) float sums[];  // [4 waves or 16 slots][16 rows][LD], then maxima and sums of weights
+    extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves or slots][16 rows][LD]
     __shared__ float tops[kWaves * kTile], weights[kWaves * kTile];
     __shared__ long long scan_sums[kWaves];
     __shared__ int found;
-    __shared__ Seq found_seq;
     __shared__ long long found_at;
     __shared__ unsigned share;
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
     const int head = blockIdx.y, d = c.d_head;
 
-    // where this workgroup's piece of the line begins
-    long long w0, w1, line;
-    {
-        const int per = (a.r.n + kThreads - 1) / kThreads, i0 = min(tid * per, a.r.n), i1 = min(i0 + per, a.r.n);
-        long long mine = 0;
-        Seq last;
-        for (int i = i0; i < i1; ++i) {
-            last = sequence_at(a, i);
-            mine += (long long)last.tiles * last.cost();
-        }
-        long long x = mine;
+    // where this workgroup's piece of the line begins; up to 64 sequences, a lane a sequence, each wave finds out for itself
+    long long line, chunk, w0, at;
+    int i;
+    Seq mine_seq;
+    const bool in_lanes = a.r.n <= 64;
+    const auto seq_of = [&](int k) {
+        if (!in_lanes) return sequence_at(a, k);
+        Seq q;
+        q.s = __builtin_amdgcn_readlane(mine_seq.s, k);
+        q.first = __builtin_amdgcn_readlane(mine_seq.first, k);
+        q.count = __builtin_amdgcn_readlane(mine_seq.count, k);
+        q.length = __builtin_amdgcn_readlane(mine_seq.length, k);
+        q.tiles = __builtin_amdgcn_readlane(mine_seq.tiles, k);
+        q.sink_blocks = __builtin_amdgcn_readlane(mine_seq.sink_blocks, k);
+        q.low_block = __builtin_amdgcn_readlane(mine_seq.low_block, k);
+        q.blocks = __builtin_amdgcn_readlane(mine_seq.blocks, k);
+        return q;
+    };
+    const auto up_to = [&](long long x) {  // inclusive prefix sums of a wave
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const long long y = __shfl_up(x, o, 64);
             if (lane >= o) x += y;
         }
+        return x;
+    };
+    if (in_lanes) {
+        mine_seq = sequence_at(a, min(lane, a.r.n - 1));
+        if (lane >= a.r.n) mine_seq.tiles = 0;
+        const long long mine = (long long)mine_seq.tiles * mine_seq.cost(), x = up_to(mine);
+        line = lane_of(x, 63);
+        chunk = max((long long)quotient(line + a.groups - 1, a.groups), (long long)a.least);
+        w0 = blockIdx.x * chunk;
+        if (w0 >= line) return;
+        i = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(w0 < x)));
+        at = lane_of(x - mine, i);
+    } else {
+        const int per = (a.r.n + kThreads - 1) / kThreads, i0 = min(tid * per, a.r.n), i1 = min(i0 + per, a.r.n);
+        long long mine = 0;
+        for (int k = i0; k < i1; ++k) {
+            const Seq q = sequence_at(a, k);
+            mine += (long long)q.tiles * q.cost();
+        }
+        const long long x = up_to(mine);
         if (lane == 63) scan_sums[wave] = x;
         __syncthreads();
         long long before = x - mine;
@@ -105,39 +140,38 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
             before += w < wave ? scan_sums[w] : 0;
             line += scan_sums[w];
         }
-        const long long chunk = max((line + a.groups - 1) / a.groups, (long long)a.least);
+        line = lane_of(line, 0);
+        chunk = max((long long)quotient(line + a.groups - 1, a.groups), (long long)a.least);
         w0 = blockIdx.x * chunk;
-        w1 = min(w0 + chunk, line);
         if (w0 >= line) return;
         if (before <= w0 && w0 < before + mine) {
-            int i = i0;
-            Seq q = last;
-            if (per > 1)
-                for (;; ++i) {
-                    q = sequence_at(a, i);
-                    const long long next = before + (long long)q.tiles * q.cost();
-                    if (w0 < next) break;
-                    before = next;
-                }
-            found = i;
-            found_seq = q;
+            int k = i0;
+            for (;; ++k) {
+                const Seq q = sequence_at(a, k);
+                const long long next = before + (long long)q.tiles * q.cost();
+                if (w0 < next) break;
+                before = next;
+            }
+            found = k;
             found_at = before;
         }
         __syncthreads();
+        i = __builtin_amdgcn_readfirstlane(found);
+        at = lane_of(found_at, 0);
     }
-    const long long chunk = max((line + a.groups - 1) / a.groups, (long long)a.least);
-    int i = __builtin_amdgcn_readfirstlane(found);
-    long long at = found_at;
-    Seq sq = found_seq;
+    const long long w1 = min(w0 + chunk, line);
+    Seq sq = seq_of(i);
 
     for (long long w = w0; w < w1;) {
         while (w >= at + (long long)sq.tiles * sq.cost()) {
             at += (long long)sq.tiles * sq.cost();
-            sq = sequence_at(a, ++i);
+            sq = seq_of(++i);
         }
-        const int cost = sq.cost(), tile = (int)((w - at) / cost), c0 = (int)((w - at) - (long long)tile * cost), c1 = (int)min((long long)cost, c0 + (w1 - w));
+        const int cost = sq.cost(), tile = quotient(w - at, cost), c0 = (int)((w - at) - (long long)tile * cost), c1 = (int)min((long long)cost, c0 + (w1 - w));
         const long long unit = at + (long long)tile * cost;  // where the tile begins
-        const int b0 = (int)((long long)c0 * sq.blocks / cost), b1 = (int)((long long)c1 * sq.blocks / cost);
+        // (the same numbers give the same bounds to the workgroups on either side)
+        const auto block_of = [&](int at_cost) { return at_cost == cost ? sq.blocks : (int)((double)at_cost * sq.blocks / cost); };
+        const int b0 = block_of(c0), b1 = block_of(c1);
         // ---- rows
         const int rows = sq.count * a.group, idx = tile * kTile + n16, mine = min(idx, rows - 1), j = mine / a.group, e = mine - j * a.group;
         const int pos = a.causal ? sq.length - sq.count + j : sq.length - 1, low = a.window ? pos - a.window : -1;
@@ -165,24 +199,27 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
         {
             const V* x = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
             RowVec<R, 8> raw[KS];
+            // (a piece behind the head's end begins earlier, by eights; what another lane has as well is 0 here)
+            const auto has = [&](int s) { return 8 * (s & 1) >= 64 * (s >> 1) + 16 * g - min(64 * (s >> 1) + 16 * g, d - 16); };
             float big = 0.f;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
-                raw[s].load(x + off);
+            for (int s = 0; s < KS; ++s) raw[s].load(x + min(64 * (s >> 1) + 16 * g, d - 16) + 8 * (s & 1));
 #pragma unroll
-                for (int t = 0; t < 8; ++t) big = fmaxf(big, off + t >= begin ? fabsf(R::up(raw[s].v[t])) : 0.f);
+            for (int s = 0; s < KS; ++s) {
+                float most = 0.f;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) most = fmaxf(most, fabsf(R::up(raw[s].v[t])));
+                big = fmaxf(big, has(s) ? most : 0.f);
             }
             big = quad_rows_max(big);
             const int up = up_of(big);
             row_scale = ldexpf(1.f, -up);
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const int begin = 64 * (s >> 1) + 16 * g, off = min(begin, d - 16) + 8 * (s & 1);
+                const bool here = has(s);
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    // (a piece behind the head's end begins earlier, and what another lane has as well is 0 here)
-                    const float v = off + t >= begin ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
+                    const float v = here ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
                     q[0][s][t] = (_Float16)v;
                     if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
                 }
@@ -318,59 +355,73 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
             use(other, y.blk, y.ks, y.vs);
         }
 
-        // ---- the waves' results joined: a slot of 16 threads a row
+        // ---- the waves' results joined: a slot of kCols threads a row
         sum = quad_rows_sum(sum);
+        const int slot = tid / kCols, col = tid % kCols * NC, valid = min(kTile, rows - tile * kTile);
+        if (n16 < valid) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float* to = sums + (wave * kTile + n16) * LD + (4 * g + r) * NJ;
+            for (int r = 0; r < 4; ++r) {
+                float* to = sums + (wave * kTile + n16) * LD + (4 * g + r) * NJ;
 #pragma unroll
-            for (int t = 0; t < NJ; t += 4) *(float4*)(to + t) = make_float4(acc[t][r], acc[t + 1][r], acc[t + 2][r], acc[t + 3][r]);
+                for (int t = 0; t < NJ; t += 4) *(float4*)(to + t) = make_float4(acc[t][r], acc[t + 1][r], acc[t + 2][r], acc[t + 3][r]);
+            }
+            if (g == 0) {
+                tops[wave * kTile + n16] = top;
+                weights[wave * kTile + n16] = sum;
+            }
         }
-        if (g == 0) {
-            tops[wave * kTile + n16] = top;
-            weights[wave * kTile + n16] = sum;
-        }
-        __syncthreads();
-        const int slot = tid >> 4, col = (tid & 15) * NJ, valid = min(kTile, rows - tile * kTile);
-        float m = -INFINITY, l = 0.f, o[NJ];
+        lds_barrier();
+        float m = -INFINITY, l = 0.f, o[NC];
 #pragma unroll
-        for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+        for (int t = 0; t < NC; ++t) o[t] = 0.f;
         const auto fold = [&](float pm, float pl, const float* po) {  // (parts that have seen nothing: of weight 0)
             const float now = fmaxf(m, pm), base = now == -INFINITY ? 0.f : now;
             const float was = __builtin_amdgcn_exp2f(m - base), is = __builtin_amdgcn_exp2f(pm - base);
             l = l * was + pl * is;
 #pragma unroll
-            for (int t = 0; t < NJ; ++t) o[t] = o[t] * was + po[t] * is;
+            for (int t = 0; t < NC; ++t) o[t] = o[t] * was + po[t] * is;
             m = now;
         };
+        if (slot < valid)
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) fold(tops[k * kTile + slot], weights[k * kTile + slot], sums + (k * kTile + slot) * LD + col);
+            for (int k = 0; k < kWaves; ++k) fold(tops[k * kTile + slot], weights[k * kTile + slot], sums + (k * kTile + slot) * LD + col);
         const auto put = [&](int row) {
             const int jr = (tile * kTile + row) / a.group, er = tile * kTile + row - jr * a.group, h = head * a.group + er;
             const int64_t t_at = sq.first + jr;
             const float by = l == 0.f ? 0.f : 1.f / l;
-            RowVec<R, NJ> y;
+            // (a last piece of values that is cut began earlier: so many columns hold what the piece before has)
+            const int cut = max(col / NJ * NJ + NJ - d, 0), dim = col - cut;
+            if (col / NJ * NJ < d) {
+                V* out = (V*)a.out + t_at * a.out_token + (int64_t)h * a.out_head + dim;
+                if constexpr (NC >= 4) {
 #pragma unroll
-            for (int t = 0; t < NJ; ++t) y.v[t] = R::down(o[t] * by);
-            V* out = (V*)a.out + t_at * a.out_token + (int64_t)h * a.out_head;
-            if (col < d) y.store(out + min(col, d - NJ));  // (a last piece that is cut begins earlier, as its loads did: the lane before writes the same there)
+                    for (int t = 0; t < NC; t += 4) {
+                        RowVec<R, 4> y;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) y.v[u] = R::down(o[t + u] * by);
+                        y.store(out + t);
+                    }
+                } else {
+                    RowVec<R, 2> y;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) y.v[u] = R::down(o[u] * by);
+                    y.store(out);
+                }
+            }
             if (a.lse && col == 0) a.lse[t_at * a.heads + h] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
         };
         const bool whole = c0 == 0 && c1 == cost;
         if (whole) {
             if (slot < valid) put(slot);
-            __syncthreads();
+            lds_barrier();
         } else {
             // the workgroups that share the tile: in the first of them it begins last, in the others first
-            const int from = (int)(unit / chunk), to = (int)((unit + cost - 1) / chunk);
+            const int from = quotient(unit, chunk), to = quotient(unit + cost - 1, chunk);
             constexpr int kRow = part_row(DP);
             const int64_t place = ((int64_t)head * a.groups + blockIdx.x) * 2 + (blockIdx.x == from);
             const auto mem = make_rsrc(a.part + place * kTile * kRow, sizeof(float) * kTile * kRow);
             if (slot < valid) {
-#pragma unroll
-                for (int t = 0; t < NJ; t += 4)
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[t]), __float_as_uint(o[t + 1]), __float_as_uint(o[t + 2]), __float_as_uint(o[t + 3])}, mem,
-                                                           (slot * kRow + col + t) * 4, 0, kPartAux);
+                put_part<NC>(mem, (slot * kRow + col) * 4, o);
                 if (col == 0) __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(m), __float_as_uint(l), 0u, 0u}, mem, (slot * kRow + DP) * 4, 0, kPartAux);
             }
             if (last_in(a.arrived + (int64_t)head * a.groups + from, (unsigned)(to - from + 1), &share)) {
@@ -381,23 +432,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
                 m = -INFINITY;
                 l = 0.f;
 #pragma unroll
-                for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+                for (int t = 0; t < NC; ++t) o[t] = 0.f;
                 for (int p = from + sub; p <= to && row < valid; p += apart) {
                     const int64_t where = ((int64_t)head * a.groups + p) * 2 + (p == from);
                     const auto src = make_rsrc(a.part + where * kTile * kRow, sizeof(float) * kTile * kRow);
-                    float po[NJ];
+                    float po[NC];
                     const u32x4 ml = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (row * kRow + DP) * 4, 0, kPartAux));
-#pragma unroll
-                    for (int t = 0; t < NJ; t += 4) {
-                        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, (row * kRow + col + t) * 4, 0, kPartAux));
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) po[t + u] = __uint_as_float(y[u]);
-                    }
+                    get_part<NC>(src, (row * kRow + col) * 4, po);
                     fold(__uint_as_float(ml[0]), __uint_as_float(ml[1]), po);
                 }
                 if (apart > 1) {
 #pragma unroll
-                    for (int t = 0; t < NJ; t += 4) *(float4*)(sums + slot * LD + col + t) = make_float4(o[t], o[t + 1], o[t + 2], o[t + 3]);
+                    for (int t = 0; t < NC; ++t) sums[slot * LD + col + t] = o[t];
                     if (col == 0) {
                         tops[slot] = m;
                         weights[slot] = l;
@@ -407,7 +453,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void cache_attend_kern
                         m = -INFINITY;
                         l = 0.f;
 #pragma unroll
-                        for (int t = 0; t < NJ; ++t) o[t] = 0.f;
+                        for (int t = 0; t < NC; ++t) o[t] = 0.f;
                         for (int k = 0; k < apart; ++k) fold(tops[k * lanes + slot], weights[k * lanes + slot], sums + (k * lanes + slot) * LD + col);
                     }
                 }
@@ -430,7 +476,7 @@ hipError_t launch(const AttendArgs& a, hipStream_t st) {
 }
 template <class R>
 hipError_t launch(const AttendArgs& a, hipStream_t st) {
-    return a.c.d_head <= 64 ? launch<R, 64>(a, st) : a.c.d_head <= 128 ? launch<R, 128>(a, st) : launch<R, 256>(a, st);
+    return a.c.d_head <= 64 ? launch<R, 64>(a, st) : launch<R, 128>(a, st);
 }
 
 }  // namespace
@@ -438,9 +484,9 @@ hipError_t launch(const AttendArgs& a, hipStream_t st) {
 namespace bild {
 
 hipError_t attend_init(int d_head) {
-    const void* const wide[] = {(const void*)cache_attend_kernel<RowF32, 256>, (const void*)cache_attend_kernel<RowBf16, 256>, (const void*)cache_attend_kernel<RowF16, 256>};
+    const void* const half[] = {(const void*)cache_attend_kernel<RowF32, 128>, (const void*)cache_attend_kernel<RowBf16, 128>, (const void*)cache_attend_kernel<RowF16, 128>};
     if (const hipError_t e = cache_prompt_init(d_head); e != hipSuccess) return e;
-    return d_head <= 128 ? hipSuccess : raise_lds_limit(wide, (int)lds_bytes(256));
+    return d_head <= 64 ? hipSuccess : d_head <= 128 ? raise_lds_limit(half, (int)lds_bytes(128)) : cache_attend_tall_init();
 }
 
 size_t attend_part_floats(int heads, int d_head) {
@@ -491,7 +537,8 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
     if (prompts && launch_cache_prompt(a, k.dtype, tiles, st) != hipSuccess) return BILD_EHIP;
-    if (prompts && (!k.starts || k.n == 1)) return BILD_OK;  // (all are prompts)
+    if (prompts && !k.starts) return BILD_OK;  // (all are prompts; with starts, how many rows a sequence has is known to the kernels alone)
+    if (v.d_head > 128) return launch_cache_attend_tall(a, k.dtype, st) == hipSuccess ? BILD_OK : BILD_EHIP;
     const hipError_t err = k.dtype == BILD_DT_F32 ? launch<RowF32>(a, st) : k.dtype == BILD_DT_BF16 ? launch<RowBf16>(a, st) : launch<RowF16>(a, st);
     return err == hipSuccess ? BILD_OK : BILD_EHIP;
 }
