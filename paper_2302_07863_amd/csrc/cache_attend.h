@@ -63,7 +63,7 @@ __device__ __forceinline__ int up_of(float big) {
 
 constexpr int kTile = 16;      // rows of a tile of the kernels for few rows
 #ifndef START
-#define START 6
+#define START 16
 #endif
 constexpr int kStart = START;
 

@@ -24,11 +24,31 @@ using namespace bild;
 namespace {
 
 // (twice as many workgroups of half as many waves have twice as many parts to join)
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+#ifndef NWAVES
+#define NWAVES 8
+#endif
+constexpr int kWaves = NWAVES, kThreads = 64 * kWaves;
 
 // (quotients of what is uniform and nearly always below 2^32: a 64-bit division is a hundred instructions)
-__device__ __forceinline__ int quotient(long long a, long long b) {
-    return a < (1ll << 32) && b < (1ll << 32) ? (int)((uint32_t)a / (uint32_t)b) : (int)(a / b);
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return a < (1ll << 32) && b < (1ll << 32) ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Inclusive prefix sums of a wave: within rows of 16 lanes, then the rows before.
+__device__ __forceinline__ int prefix_sum(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast31 into rows 2 and 3
+    return v;
+}
+
+// What each workgroup takes of a line: equal pieces, none less than `least` unless it is all there is.
+__device__ __forceinline__ long long piece_of(long long line, int groups, int least) {
+    const long long pieces = min(max(quotient(line, least), 1ll), (long long)groups);
+    return quotient(line + pieces - 1, pieces);
 }
 
 // A lane's value, for all of them: what the work is cut by has to be known to be the same in all lanes, or every load of codes would be a loop over the bases it might have.
@@ -106,6 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         return q;
     };
     const auto up_to = [&](long long x) {  // inclusive prefix sums of a wave
+        if (!__any(x >= 1 << 25)) return (long long)prefix_sum((int)x);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const long long y = __shfl_up(x, o, 64);
@@ -118,7 +139,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         if (lane >= a.r.n) mine_seq.tiles = 0;
         const long long mine = (long long)mine_seq.tiles * mine_seq.cost(), x = up_to(mine);
         line = lane_of(x, 63);
-        chunk = max((long long)quotient(line + a.groups - 1, a.groups), (long long)a.least);
+        chunk = piece_of(line, a.groups, a.least);
         w0 = blockIdx.x * chunk;
         if (w0 >= line) return;
         i = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(w0 < x)));
@@ -141,7 +162,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             line += scan_sums[w];
         }
         line = lane_of(line, 0);
-        chunk = max((long long)quotient(line + a.groups - 1, a.groups), (long long)a.least);
+        chunk = piece_of(line, a.groups, a.least);
         w0 = blockIdx.x * chunk;
         if (w0 >= line) return;
         if (before <= w0 && w0 < before + mine) {
@@ -162,12 +183,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
     const long long w1 = min(w0 + chunk, line);
     Seq sq = seq_of(i);
 
+    int turn = 0;
     for (long long w = w0; w < w1;) {
         while (w >= at + (long long)sq.tiles * sq.cost()) {
             at += (long long)sq.tiles * sq.cost();
             sq = seq_of(++i);
         }
-        const int cost = sq.cost(), tile = quotient(w - at, cost), c0 = (int)((w - at) - (long long)tile * cost), c1 = (int)min((long long)cost, c0 + (w1 - w));
+        const int cost = sq.cost(), tile = (int)quotient(w - at, cost), c0 = (int)((w - at) - (long long)tile * cost), c1 = (int)min((long long)cost, c0 + (w1 - w));
         const long long unit = at + (long long)tile * cost;  // where the tile begins
         // (the same numbers give the same bounds to the workgroups on either side)
         const auto block_of = [&](int at_cost) { return at_cost == cost ? sq.blocks : (int)((double)at_cost * sq.blocks / cost); };
@@ -182,8 +204,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         // ---- a page and its scales for each of the next 64 blocks of this wave, a lane a block
         int pages = -1;
         float k_scale = 0.f, v_scale = 0.f;
+        // a tile that is no more than a wave's share of the piece is one wave's alone, the next one the next wave's
+        const bool whole = c0 == 0 && c1 == cost, alone = whole && sq.blocks <= max(chunk / kWaves, 2ll);
+        if (alone && (turn++ & (kWaves - 1)) != wave) {
+            w += c1 - c0;
+            continue;
+        }
+        const int step = alone ? 1 : kWaves, begin = alone ? b0 : b0 + wave;
         const auto look_up = [&](int b) {
-            const int mine_at = b + kWaves * lane, blk = block_at(mine_at), p0 = blk * kBlock;
+            const int mine_at = b + step * lane, blk = block_at(mine_at), p0 = blk * kBlock;
             pages = -1;
             if (mine_at < b1 && p0 < sq.length && p0 <= last_pos && (!a.window || p0 + kBlock - 1 > first_pos - a.window || p0 < a.sinks))
                 pages = c.table[(int64_t)sq.s * c.max_pages + (p0 >> c.page_shift)];
@@ -193,38 +222,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
                 v_scale = c.scales[c.plane(pages, a.layer, 1, head)] * (512.f / 127.f);
             }
         };
-        if (b0 + wave < b1) look_up(b0 + wave);
-        f16x8 q[TERMS][KS];
-        float row_scale;
-        {
-            const V* x = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
-            RowVec<R, 8> raw[KS];
-            // (a piece behind the head's end begins earlier, by eights; what another lane has as well is 0 here)
-            const auto has = [&](int s) { return 8 * (s & 1) >= 64 * (s >> 1) + 16 * g - min(64 * (s >> 1) + 16 * g, d - 16); };
-            float big = 0.f;
+        if (begin < b1) look_up(begin);
+        const V* x_row = (const V*)a.q + (int64_t)(sq.first + j) * a.q_token + (int64_t)(head * a.group + e) * a.q_head;
+        RowVec<R, 8> raw[KS];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) raw[s].load(x + min(64 * (s >> 1) + 16 * g, d - 16) + 8 * (s & 1));
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                float most = 0.f;
-#pragma unroll
-                for (int t = 0; t < 8; ++t) most = fmaxf(most, fabsf(R::up(raw[s].v[t])));
-                big = fmaxf(big, has(s) ? most : 0.f);
-            }
-            big = quad_rows_max(big);
-            const int up = up_of(big);
-            row_scale = ldexpf(1.f, -up);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const bool here = has(s);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    const float v = here ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
-                    q[0][s][t] = (_Float16)v;
-                    if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
-                }
-            }
-        }
+        for (int s = 0; s < KS; ++s) raw[s].load(x_row + min(64 * (s >> 1) + 16 * g, d - 16) + 8 * (s & 1));
         float top = -INFINITY, sum = 0.f;
         f32x4 acc[NJ];
 #pragma unroll
@@ -259,6 +261,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
                 }
             }
         };
+        f16x8 q[TERMS][KS];
+        float row_scale = 1.f;
         const auto use = [&](Codes<DP>& x, int blk, float ks, float vs) {
             f32x4 z[2];
 #pragma unroll
@@ -322,14 +326,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         };
         // ---- the wave's blocks, the next one's codes on their way
         Codes<DP> one, other;
-        int nth = 0, b = b0 + wave - kWaves;  // of the looked up ones
+        int nth = 0, b = begin - step;  // of the looked up ones
         struct Next {
             int blk;  // -1: no more
             float ks, vs;
         };
         const auto next = [&](Codes<DP>& x) {
             Next r = {-1, 0.f, 0.f};
-            for (b += kWaves; b < b1; b += kWaves) {
+            for (b += step; b < b1; b += step) {
                 if (nth == 64) {
                     look_up(b);
                     nth = 0;
@@ -347,6 +351,32 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             return r;
         };
         Next x = next(one);
+        // (the rows while the first codes are on their way)
+        {
+            // (a piece behind the head's end begins earlier, by eights; what another lane has as well is 0 here)
+            const auto has = [&](int s) { return 8 * (s & 1) >= 64 * (s >> 1) + 16 * g - min(64 * (s >> 1) + 16 * g, d - 16); };
+            float big = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                float most = 0.f;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) most = fmaxf(most, fabsf(R::up(raw[s].v[t])));
+                big = fmaxf(big, has(s) ? most : 0.f);
+            }
+            big = quad_rows_max(big);
+            const int up = up_of(big);
+            row_scale = ldexpf(1.f, -up);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool here = has(s);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const float v = here ? ldexpf(R::up(raw[s].v[t]), up) : 0.f;
+                    q[0][s][t] = (_Float16)v;
+                    if (TWO) q[TERMS - 1][s][t] = (_Float16)(v - (float)q[0][s][t]);
+                }
+            }
+        }
         while (x.blk >= 0) {
             const Next y = next(other);
             use(one, x.blk, x.ks, x.vs);
@@ -357,6 +387,25 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 
         // ---- the waves' results joined: a slot of kCols threads a row
         sum = quad_rows_sum(sum);
+        if (alone) {
+            if (idx < rows) {
+                const int64_t t_at = sq.first + j;
+                const int h = head * a.group + e;
+                const float by = sum == 0.f ? 0.f : 1.f / sum;
+                V* out = (V*)a.out + t_at * a.out_token + (int64_t)h * a.out_head;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int dim = (4 * g + r) * NJ;
+                    RowVec<R, NJ> y;
+#pragma unroll
+                    for (int t = 0; t < NJ; ++t) y.v[t] = R::down(acc[t][r] * by);
+                    if (dim < d) y.store(out + dim);
+                }
+                if (a.lse && g == 0) a.lse[t_at * a.heads + h] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+            }
+            w += c1 - c0;
+            continue;
+        }
         const int slot = tid / kCols, col = tid % kCols * NC, valid = min(kTile, rows - tile * kTile);
         if (n16 < valid) {
 #pragma unroll
@@ -382,9 +431,24 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             for (int t = 0; t < NC; ++t) o[t] = o[t] * was + po[t] * is;
             m = now;
         };
-        if (slot < valid)
+        if (slot < valid) {
+            float tk[kWaves], by[kWaves];
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) fold(tops[k * kTile + slot], weights[k * kTile + slot], sums + (k * kTile + slot) * LD + col);
+            for (int k = 0; k < kWaves; ++k) {
+                tk[k] = tops[k * kTile + slot];
+                m = fmaxf(m, tk[k]);
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                by[k] = __builtin_amdgcn_exp2f(tk[k] - base);
+                l = __builtin_fmaf(weights[k * kTile + slot], by[k], l);
+            }
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k)
+#pragma unroll
+                for (int t = 0; t < NC; ++t) o[t] = __builtin_fmaf(sums[(k * kTile + slot) * LD + col + t], by[k], o[t]);
+        }
         const auto put = [&](int row) {
             const int jr = (tile * kTile + row) / a.group, er = tile * kTile + row - jr * a.group, h = head * a.group + er;
             const int64_t t_at = sq.first + jr;
@@ -410,13 +474,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             }
             if (a.lse && col == 0) a.lse[t_at * a.heads + h] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
         };
-        const bool whole = c0 == 0 && c1 == cost;
         if (whole) {
             if (slot < valid) put(slot);
             lds_barrier();
         } else {
             // the workgroups that share the tile: in the first of them it begins last, in the others first
-            const int from = quotient(unit, chunk), to = quotient(unit + cost - 1, chunk);
+            const int from = (int)quotient(unit, chunk), to = (int)quotient(unit + cost - 1, chunk);
             constexpr int kRow = part_row(DP);
             const int64_t place = ((int64_t)head * a.groups + blockIdx.x) * 2 + (blockIdx.x == from);
             const auto mem = make_rsrc(a.part + place * kTile * kRow, sizeof(float) * kTile * kRow);
@@ -524,9 +587,9 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     a.scale = (float)((double)k.scale * 1.4426950408889634 * 512.0 / 127.0);
     a.groups = attend_groups(v.heads);
 #ifndef LEAST
-#define LEAST 8
+#define LEAST 20
 #endif
-    a.least = LEAST + kStart;
+    a.least = LEAST;
     // (fewer tiles than the chip has room for leave it empty: their keys are cut into pieces instead)
     const int64_t tiles = k.starts ? tokens * a.group / kPromptRows + k.n : k.n * (((int64_t)k.rows * a.group + kPromptRows - 1) / kPromptRows);
     const bool prompts = (int64_t)k.rows * a.group >= kPromptFrom && tokens * a.group / kPromptRows * v.heads >= kPromptTiles;
