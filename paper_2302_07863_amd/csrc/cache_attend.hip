@@ -91,10 +91,13 @@ __device__ __forceinline__ void get_part(__amdgpu_buffer_rsrc_t mem, int off, fl
     }
 }
 
-template <class R, int DP>
+// ONCE: no other tile has the same keys.
+template <class R, int DP, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendArgs a) {
     constexpr bool TWO = R::kDtype == BILD_DT_F32;  // rows and weights in two fp16 parts
     constexpr int NK = DP / 64, KS = DP / 32, NJ = DP / 16, WV = NJ / 4, TERMS = TWO ? 2 : 1, LD = DP + 4;
+    // Codes that are read once do not push others out of the caches (us: 32 heads x 65537 positions 103 / 89; where tiles share them, 60 rows of 4 heads over 2000 positions 80 / 96)
+    constexpr int kAux = ONCE ? 2 : 0;  // nt
     constexpr int kCols = kThreads / kTile, NC = DP / kCols;  // threads of a row of results, columns of each
     typedef typename R::type V;
     extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves or slots][16 rows][LD]
@@ -243,19 +246,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 #pragma unroll
                 for (int t = 0; t < NK; ++t) {
                     // (rows begin at multiples of 8 bytes)
-                    x.k[h][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, (key + 4 * h) * d + min(64 * t + 16 * g, d - 16), base, 0));
+                    x.k[h][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, (key + 4 * h) * d + min(64 * t + 16 * g, d - 16), base, kAux));
                 }
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const int off = (8 * g + t) * d + min(n16 * NJ, d - NJ);
                 if constexpr (WV == 1) {
-                    x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, base, 0);
+                    x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, base, kAux);
                 } else if constexpr (WV == 2) {
-                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, base, 0);
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, base, kAux);
                     x.v[t][0] = (uint32_t)y[0];
                     x.v[t][1] = (uint32_t)y[1];
                 } else {
-                    const auto y = __builtin_amdgcn_raw_buffer_load_b128(v, off, base, 0);
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b128(v, off, base, kAux);
 #pragma unroll
                     for (int w4 = 0; w4 < 4; ++w4) x.v[t][w4] = (uint32_t)y[w4];
                 }
@@ -533,13 +536,15 @@ constexpr int kPromptFrom = 64, kPromptTiles = 128;
 
 constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
 
-template <class R, int DP>
+template <class R, int DP, bool ONCE>
 hipError_t launch(const AttendArgs& a, hipStream_t st) {
-    return launch_on(cache_attend_kernel<R, DP>, dim3(a.groups, a.c.heads), dim3(kThreads), lds_bytes(DP), st, a);
+    return launch_on(cache_attend_kernel<R, DP, ONCE>, dim3(a.groups, a.c.heads), dim3(kThreads), lds_bytes(DP), st, a);
 }
 template <class R>
 hipError_t launch(const AttendArgs& a, hipStream_t st) {
-    return a.c.d_head <= 64 ? launch<R, 64>(a, st) : launch<R, 128>(a, st);
+    const bool once = (int64_t)a.r.rows * a.group <= kTile;
+    if (a.c.d_head <= 64) return once ? launch<R, 64, true>(a, st) : launch<R, 64, false>(a, st);
+    return once ? launch<R, 128, true>(a, st) : launch<R, 128, false>(a, st);
 }
 
 }  // namespace
@@ -547,7 +552,8 @@ hipError_t launch(const AttendArgs& a, hipStream_t st) {
 namespace bild {
 
 hipError_t attend_init(int d_head) {
-    const void* const half[] = {(const void*)cache_attend_kernel<RowF32, 128>, (const void*)cache_attend_kernel<RowBf16, 128>, (const void*)cache_attend_kernel<RowF16, 128>};
+    const void* const half[] = {(const void*)cache_attend_kernel<RowF32, 128, true>,  (const void*)cache_attend_kernel<RowBf16, 128, true>,  (const void*)cache_attend_kernel<RowF16, 128, true>,
+                                (const void*)cache_attend_kernel<RowF32, 128, false>, (const void*)cache_attend_kernel<RowBf16, 128, false>, (const void*)cache_attend_kernel<RowF16, 128, false>};
     if (const hipError_t e = cache_prompt_init(d_head); e != hipSuccess) return e;
     return d_head <= 64 ? hipSuccess : d_head <= 128 ? raise_lds_limit(half, (int)lds_bytes(128)) : cache_attend_tall_init();
 }
