@@ -24,10 +24,7 @@ using namespace bild;
 namespace {
 
 // (twice as many workgroups of half as many waves have twice as many parts to join)
-#ifndef NWAVES
-#define NWAVES 8
-#endif
-constexpr int kWaves = NWAVES, kThreads = 64 * kWaves;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
 // (quotients of what is uniform and nearly always below 2^32: a 64-bit division is a hundred instructions)
 __device__ __forceinline__ long long quotient(long long a, long long b) {
@@ -328,7 +325,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             }
         };
         // ---- the wave's blocks, the next one's codes on their way
-        Codes<DP> one, other;
+        Codes<DP> one;
         int nth = 0, b = begin - step;  // of the looked up ones
         struct Next {
             int blk;  // -1: no more
@@ -381,11 +378,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             }
         }
         while (x.blk >= 0) {
-            const Next y = next(other);
             use(one, x.blk, x.ks, x.vs);
-            if (y.blk < 0) break;
             x = next(one);
-            use(other, y.blk, y.ks, y.vs);
         }
 
         // ---- the waves' results joined: a slot of kCols threads a row
