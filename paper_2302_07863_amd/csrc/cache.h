@@ -1,5 +1,7 @@
 // The cache in 8 bits as its kernels see it (cache.hip: pages and appending; cache_attend.hip: attention).
 #pragma once
+#include <algorithm>
+
 #include "operators.h"
 
 namespace bild {
@@ -67,6 +69,6 @@ constexpr int kAttendGroups = GROUPS;                       // workgroups of a l
 inline int attend_groups(int heads) { return (kAttendGroups + heads - 1) / heads; }  // of a key head
 hipError_t attend_init(int d_head);                      // what its kernels need of the current device
 size_t attend_part_floats(int heads, int d_head);        // of bild_cache::part
-inline size_t attend_counts(int heads) { return (size_t)heads * attend_groups(heads); }
+inline size_t attend_counts(int heads) { return std::max((size_t)heads * attend_groups(heads), (size_t)512); }
 
 }  // namespace bild

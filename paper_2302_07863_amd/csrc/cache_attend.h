@@ -28,6 +28,7 @@ struct AttendArgs {
     float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
     int prompt_from;      // rows of a sequence, times `group`, from which on it is the kernel for prompts'
     int groups, least;  // workgroups of a key head; what one takes at least
+    int splits;         // of a prompt tile's keys
     float* part;
     unsigned* arrived;
 };
@@ -97,6 +98,8 @@ hipError_t launch_cache_attend_tall(const AttendArgs& a, int dtype, hipStream_t 
 hipError_t cache_attend_tall_init();
 hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st);
 hipError_t cache_prompt_init(int d_head);
-constexpr int kPromptRows = 128;  // of a tile of the kernel for prompts
+size_t prompt_part_floats(int d_head);
+constexpr int kPromptRows = 128;   // of a tile of the kernel for prompts
+constexpr int kPromptParts = 512;  // most workgroups of a launch that shares tiles' keys: two a compute unit
 
 }  // namespace bild

@@ -525,8 +525,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
     }
 }
 
-// Rows (times query heads of a key head) of a sequence, and tiles in all, from which on prompts take the kernel made for them.
-constexpr int kPromptFrom = 64, kPromptTiles = 128;
+// Rows (times query heads of a key head) of a sequence from which on they take the kernel for prompts: a whole tile of it, or half a one where there is much of it, rows times query heads of all
+// sequences.  (us, this kernel / that one: 16 rows of 4 heads over 2000 positions, 32 sequences of 8 key heads 95 / 69, 64 rows over 8000, 32 key heads 50 / 53, 20 of 4 over 4000, 8 key heads 23 / 33;
+// 60 of 4 over 2000, 8 sequences 86 / 46; 8 of 4 over 2000, 32 sequences 55 / 70.)
+constexpr int kPromptFrom = 64, kPromptWork = 4096, kMaxSplits = 16;
 
 constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
 
@@ -553,7 +555,7 @@ hipError_t attend_init(int d_head) {
 }
 
 size_t attend_part_floats(int heads, int d_head) {
-    return (size_t)heads * attend_groups(heads) * 2 * kTile * part_row(d_head <= 64 ? 64 : d_head <= 128 ? 128 : 256);
+    return std::max((size_t)heads * attend_groups(heads) * 2 * kTile * part_row(d_head <= 64 ? 64 : d_head <= 128 ? 128 : 256), prompt_part_floats(d_head));
 }
 
 }  // namespace bild
@@ -590,10 +592,11 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
 #define LEAST 20
 #endif
     a.least = LEAST;
-    // (fewer tiles than the chip has room for leave it empty: their keys are cut into pieces instead)
     const int64_t tiles = k.starts ? tokens * a.group / kPromptRows + k.n : k.n * (((int64_t)k.rows * a.group + kPromptRows - 1) / kPromptRows);
-    const bool prompts = (int64_t)k.rows * a.group >= kPromptFrom && tokens * a.group / kPromptRows * v.heads >= kPromptTiles;
+    const bool prompts = (int64_t)k.rows * a.group >= kPromptRows || ((int64_t)k.rows * a.group >= kPromptFrom && tokens * k.heads >= kPromptWork);
     a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;
+    // (fewer tiles than the chip has room for: several workgroups share a tile's keys)
+    a.splits = (int)std::min(std::max(kPromptParts / (tiles * v.heads), (int64_t)1), (int64_t)kMaxSplits);
     a.part = c->part;
     a.arrived = c->arrived;
     const OnDevice on(c->device);

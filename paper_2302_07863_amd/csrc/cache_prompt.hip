@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "cache_attend.h"
+#include "last_in.h"
 
 using namespace bild;
 
@@ -18,6 +19,10 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256, kKeys = 64;
+#ifndef SPL
+#define SPL 4
+#endif
+constexpr int kSplitLeast = SPL;  // tiles of keys that a workgroup has at least
 
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float max_xor32(float v) {
@@ -36,11 +41,13 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     extern __shared__ __attribute__((aligned(16))) _Float16 lds[];  // two buffers: keys [64][DP], values [DP][64]
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n32 = lane & 31, half = lane >> 5, d = c.d_head;
+    __shared__ unsigned share;
     const int head = blockIdx.x % c.heads;  // (dies take workgroups in turn: those of a head have its keys in few L2s)
-    // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles; the last rows, which see most, come first
+    const int unit = (int)((gridDim.x - 1 - blockIdx.x) / c.heads), split = unit % a.splits;  // (the last rows, which see most, come first)
+    // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles
     int i, first, count, tile;
     {
-        const int slot = (int)((gridDim.x - 1 - blockIdx.x) / c.heads);
+        const int slot = unit / a.splits;
         if (a.r.starts) {
             int lo = 0, hi = a.r.n;
             while (hi - lo > 1) {
@@ -70,7 +77,11 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     const int wg_first = pos_of(tile * kPromptRows / a.group), wg_last = pos_of(min(tile * kPromptRows + kPromptRows - 1, rows - 1) / a.group);
     const int low_tile = a.window ? max(wg_first - a.window + 1, 0) / kKeys : 0;
     const int sink_tiles = a.window ? min((int)(((int64_t)a.sinks + kKeys - 1) / kKeys), low_tile) : 0;
-    const int tiles = sink_tiles + max((min(wg_last + 1, length) + kKeys - 1) / kKeys - low_tile, 0);
+    const int all_tiles = sink_tiles + max((min(wg_last + 1, length) + kKeys - 1) / kKeys - low_tile, 0);
+    // where there are few tiles of rows, several workgroups share a tile's keys
+    const int splits = min(a.splits, max(all_tiles / kSplitLeast, 1));
+    if (split >= splits) return;
+    const int t0 = all_tiles * split / splits, tiles = all_tiles * (split + 1) / splits;
     const auto tile_at = [&](int t) { return t < sink_tiles ? t : t - sink_tiles + low_tile; };
     // (of the wave's rows)
     const int first_pos = pos_of(min(idx0, rows - 1) / a.group), last_pos = pos_of(min(idx0 + 31, rows - 1) / a.group);
@@ -93,7 +104,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             }
         }
     };
-    look_up(0);
+    look_up(t0);
     // ---- rows
     f16x8 q[TERMS][QS];
     float row_scale;
@@ -130,8 +141,8 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
 #pragma unroll
         for (int u = 0; u < KC; ++u) {
             const int item = u * kThreads + tid, key = item / (DP / 16), ch = item % (DP / 16);
-            int page = __builtin_amdgcn_readlane(pages[0], t & 63);
-            if (PAGES == 2 && key >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], t & 63);
+            int page = __builtin_amdgcn_readlane(pages[0], (t - t0) & 63);
+            if (PAGES == 2 && key >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], (t - t0) & 63);
             const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 0, head) * c.plane_bytes() + ((key0 + key) & (c.page_tokens - 1)) * d + min(16 * ch, d - 16);
             kc[u] = __builtin_bit_cast(u32x4, *(const Piece<16, 8>*)from);
         }
@@ -140,8 +151,8 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4);
             if (group >= 8) continue;
             const int k0 = 16 * (group >> 1) + 4 * (group & 1);
-            int page = __builtin_amdgcn_readlane(pages[0], t & 63);
-            if (PAGES == 2 && k0 >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], t & 63);
+            int page = __builtin_amdgcn_readlane(pages[0], (t - t0) & 63);
+            if (PAGES == 2 && k0 >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], (t - t0) & 63);
             const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 1, head) * c.plane_bytes() + ((key0 + k0) & (c.page_tokens - 1)) * d + min(4 * dg, d - 4);
 #pragma unroll
             for (int y = 0; y < 8; ++y) vc[u][y] = *(const uint32_t*)(from + ((y & 3) + 8 * (y >> 2)) * d);
@@ -178,23 +189,23 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     for (int t = 0; t < ND; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
-    if (tiles > 0) {
-        request(0);
-        deliver(0);
+    if (t0 < tiles) {
+        request(t0);
+        deliver(t0 & 1);
     }
     lds_barrier();
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = t0; t < tiles; ++t) {
         const int key0 = tile_at(t) * kKeys;
         bool there[PAGES];
         float ks[PAGES], vs[PAGES];
 #pragma unroll
         for (int p = 0; p < PAGES; ++p) {
-            there[p] = __builtin_amdgcn_readlane(pages[p], t & 63) >= 0;
-            ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale[p]), t & 63));
-            vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale[p]), t & 63));
+            there[p] = __builtin_amdgcn_readlane(pages[p], (t - t0) & 63) >= 0;
+            ks[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale[p]), (t - t0) & 63));
+            vs[p] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale[p]), (t - t0) & 63));
         }
         if (t + 1 < tiles) {
-            if (((t + 1) & 63) == 0) look_up(t + 1);
+            if (((t + 1 - t0) & 63) == 0) look_up(t + 1);
             request(t + 1);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -287,6 +298,47 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     uint32_t x, y;
     pair_xor32(__float_as_uint(sum), x, y);
     sum = __uint_as_float(x) + __uint_as_float(y);
+    if (splits > 1) {
+        // a lane's values lie in memory as it has them, 1 KiB a store of a wave: the last of the tile's workgroups has the same lanes
+        constexpr int kPart = kPromptRows * (DP + 4);  // floats: see prompt_part_floats
+        const int64_t tile_at = (int64_t)(unit / a.splits) * c.heads + head;
+        const auto place = [&](int sp) { return make_rsrc(a.part + (tile_at * a.splits + sp) * kPart, sizeof(float) * kPart); };
+        const auto mine = place(split);
+#pragma unroll
+        for (int u = 0; u < ND; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[u][4 * r]), __float_as_uint(acc[u][4 * r + 1]), __float_as_uint(acc[u][4 * r + 2]), __float_as_uint(acc[u][4 * r + 3])},
+                                                       mine, (((wave * ND + u) * 4 + r) * 64 + lane) * 16, 0, kPartAux);
+        if (half == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(top), __float_as_uint(sum)}, mine, (kPromptRows * DP + 2 * (wave * 32 + n32)) * 4, 0, kPartAux);
+        if (!last_in(a.arrived + tile_at, (unsigned)splits, &share)) return;
+        float m = -INFINITY, l = 0.f;
+        for (int sp = 0; sp < splits; ++sp) {
+            const auto ml = __builtin_amdgcn_raw_buffer_load_b64(place(sp), (kPromptRows * DP + 2 * (wave * 32 + n32)) * 4, 0, kPartAux);
+            m = fmaxf(m, __uint_as_float(ml[0]));
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int u = 0; u < ND; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[u][r] = 0.f;
+        for (int sp = 0; sp < splits; ++sp) {
+            const auto from = place(sp);
+            const auto ml = __builtin_amdgcn_raw_buffer_load_b64(from, (kPromptRows * DP + 2 * (wave * 32 + n32)) * 4, 0, kPartAux);
+            const float by = __builtin_amdgcn_exp2f(__uint_as_float(ml[0]) - base);
+            l = __builtin_fmaf(__uint_as_float(ml[1]), by, l);
+#pragma unroll
+            for (int u = 0; u < ND; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const auto o = __builtin_amdgcn_raw_buffer_load_b128(from, (((wave * ND + u) * 4 + r) * 64 + lane) * 16, 0, kPartAux);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[u][4 * r + k] = __builtin_fmaf(__uint_as_float(o[k]), by, acc[u][4 * r + k]);
+                }
+        }
+        top = m;
+        sum = l;
+    }
     if (idx0 + n32 >= rows) return;
     const float by = sum == 0.f ? 0.f : 1.f / sum;
     const int h = head * a.group + e;
@@ -328,8 +380,10 @@ hipError_t cache_prompt_init(int d_head) {
     return d_head <= 64 ? hipSuccess : d_head <= 128 ? raise_lds_limit(half, (int)lds_bytes(128)) : raise_lds_limit(full, (int)lds_bytes(256));
 }
 
+size_t prompt_part_floats(int d_head) { return (size_t)kPromptParts * kPromptRows * ((d_head <= 64 ? 64 : d_head <= 128 ? 128 : 256) + 4); }
+
 hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st) {
-    const dim3 grid((unsigned)(a.c.heads * tiles));
+    const dim3 grid((unsigned)(a.c.heads * tiles * a.splits));
     return dtype == BILD_DT_F32 ? launch<RowF32>(a, grid, st) : dtype == BILD_DT_BF16 ? launch<RowBf16>(a, grid, st) : launch<RowF16>(a, grid, st);
 }
 
