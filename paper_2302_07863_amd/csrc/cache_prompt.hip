@@ -16,6 +16,16 @@ using namespace bild;
 
 namespace {
 
+#ifndef AHEAD
+#define AHEAD 4
+#endif
+#if AHEAD
+#define SCHED_S { __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0); _Pragma("unroll") for (int i_ = 0; i_ < 2 * QS - AHEAD; ++i_) { __builtin_amdgcn_sched_group_barrier(0x8, TERMS, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); } __builtin_amdgcn_sched_group_barrier(0x8, AHEAD * TERMS, 0); }
+#define SCHED_V { }
+#else
+#define SCHED_S
+#define SCHED_V
+#endif
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256, kKeys = 64;
@@ -43,11 +53,11 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n32 = lane & 31, half = lane >> 5, d = c.d_head;
     __shared__ unsigned share;
     const int head = blockIdx.x % c.heads;  // (dies take workgroups in turn: those of a head have its keys in few L2s)
-    const int unit = (int)((gridDim.x - 1 - blockIdx.x) / c.heads), split = unit % a.splits;  // (the last rows, which see most, come first)
+    const int place_at = (int)((gridDim.x - 1 - blockIdx.x) / c.heads), split = place_at % a.splits;  // (the last rows, which see most, come first)
     // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles
     int i, first, count, tile;
     {
-        const int slot = unit / a.splits;
+        const int slot = place_at / a.splits;
         if (a.r.starts) {
             int lo = 0, hi = a.r.n;
             while (hi - lo > 1) {
@@ -133,29 +143,38 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             }
     }
 
-    // ---- codes on their way from memory to LDS
+    // ---- codes on their way from memory to LDS: where a thread's pieces lie in a page, and (the same for a wave) which page of a tile they are of
     u32x4 kc[KC];
     uint32_t vc[VI][8];
+    int k_off[KC], v_off[VI];
+#pragma unroll
+    for (int u = 0; u < KC; ++u) {
+        const int item = u * kThreads + tid, key = item / (DP / 16), ch = item % (DP / 16);
+        k_off[u] = (PAGES == 2 ? key & (kBlock - 1) : key) * d + min(16 * ch, d - 16);
+    }
+#pragma unroll
+    for (int u = 0; u < VI; ++u) {
+        const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4), k0 = 16 * (group >> 1) + 4 * (group & 1);
+        v_off[u] = (PAGES == 2 ? k0 & (kBlock - 1) : k0) * d + min(4 * dg, d - 4);
+    }
     const auto request = [&](int t) {  // (looked up; a page that is not there: any that is in the pool, and no weight)
-        const int key0 = tile_at(t) * kKeys;
+        const int base = PAGES == 2 ? 0 : (tile_at(t) * kKeys & (c.page_tokens - 1)) * d;
+        const auto plane = [&](int which, int half_of) {
+            const int page = max(__builtin_amdgcn_readlane(pages[half_of], (t - t0) & 63), 0);
+            return make_rsrc(c.codes + c.plane(page, a.layer, which, head) * c.plane_bytes(), (size_t)c.plane_bytes());
+        };
 #pragma unroll
         for (int u = 0; u < KC; ++u) {
-            const int item = u * kThreads + tid, key = item / (DP / 16), ch = item % (DP / 16);
-            int page = __builtin_amdgcn_readlane(pages[0], (t - t0) & 63);
-            if (PAGES == 2 && key >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], (t - t0) & 63);
-            const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 0, head) * c.plane_bytes() + ((key0 + key) & (c.page_tokens - 1)) * d + min(16 * ch, d - 16);
-            kc[u] = __builtin_bit_cast(u32x4, *(const Piece<16, 8>*)from);
+            const int first_key = (u * kThreads + wave * 64) / (DP / 16);
+            kc[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(plane(0, PAGES == 2 && first_key >= kBlock ? PAGES - 1 : 0), k_off[u], base, 0));
         }
 #pragma unroll
         for (int u = 0; u < VI; ++u) {
-            const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4);
-            if (group >= 8) continue;
-            const int k0 = 16 * (group >> 1) + 4 * (group & 1);
-            int page = __builtin_amdgcn_readlane(pages[0], (t - t0) & 63);
-            if (PAGES == 2 && k0 >= kBlock) page = __builtin_amdgcn_readlane(pages[PAGES - 1], (t - t0) & 63);
-            const int8_t* from = c.codes + c.plane(max(page, 0), a.layer, 1, head) * c.plane_bytes() + ((key0 + k0) & (c.page_tokens - 1)) * d + min(4 * dg, d - 4);
+            const int first_group = (u * kThreads + wave * 64) / (DP / 4);
+            if (first_group >= 8) continue;
+            const auto from = plane(1, PAGES == 2 && first_group >= 4 ? PAGES - 1 : 0);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) vc[u][y] = *(const uint32_t*)(from + ((y & 3) + 8 * (y >> 2)) * d);
+            for (int y = 0; y < 8; ++y) vc[u][y] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(from, v_off[u], base + ((y & 3) + 8 * (y >> 2)) * d, 0);
         }
     };
     const auto k_at = [&](int key, int ch) { return key * DP + 8 * (ch ^ (DP == 64 ? (key >> 1) & 7 : key & 15)); };
@@ -183,7 +202,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         }
     };
 
-    float top = -INFINITY, sum = 0.f;
+    float top = -INFINITY, sum = 0.f, unit = 0.f, most_v = 0.f;  // (the sums over the values are in `unit`s)
     f32x16 acc[ND];
 #pragma unroll
     for (int t = 0; t < ND; ++t)
@@ -214,37 +233,37 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         if (seen) {
             f32x16 z[2];
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) z[m][r] = 0.f;
 #pragma unroll
-                for (int u = 0; u < QS; ++u) {
+            for (int u = 0; u < QS; ++u)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
                     const f16x8 k = *(const f16x8*)(at + k_at(32 * m + n32, 2 * u + half));
 #pragma unroll
                     for (int w = 0; w < TERMS; ++w) z[m] = mma(k, q[w][u], z[m]);
                 }
-            }
+            SCHED_S
+            // (what scores are multiplied by is not 0, so that hidden ones stay -infinity: where it would be, the scores are 0)
+            const float by[2] = {fmaxf(ks[0] * row_scale, 1.17549435e-38f), fmaxf(ks[PAGES - 1] * row_scale, 1.17549435e-38f)};
             const bool full = key0 + kKeys - 1 <= first_pos && (!a.window || key0 > last_pos - a.window || key0 + kKeys <= a.sinks) && there[0] && there[PAGES - 1];
-            float big = -INFINITY, by[2] = {ks[0] * row_scale, ks[PAGES - 1] * row_scale};
-            if (full) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    float most = z[m][0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r) most = fmaxf(most, z[m][r]);
-                    big = fmaxf(big, most * by[m]);
-                }
-            } else {
+            if (!full) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = key0 + 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
-                        const bool sees = key <= pos && (key > low || key < a.sinks) && there[m * (PAGES - 1)];
-                        z[m][r] = sees ? z[m][r] * by[m] : -INFINITY;
-                        big = fmaxf(big, z[m][r]);
+                        z[m][r] = key <= pos && (key > low || key < a.sinks) && there[m * (PAGES - 1)] ? z[m][r] : -INFINITY;
                     }
-                by[0] = by[1] = 1.f;
+            }
+            float big = -INFINITY;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                float most = z[m][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most = fmaxf(most, z[m][r]);
+                big = fmaxf(big, most * by[m]);
             }
             big = max_xor32(big);
             if (__any(big > top + kSlack)) {
@@ -257,37 +276,44 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
                 top = now;
             }
             const float base = top == -INFINITY ? 0.f : top;
-            f16x8 w[TERMS][4];
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int p = 0; p < PAGES; ++p) {
+                // a page's scale goes into its weights, relative to a power of two that the sums are kept in units of
+                const float v = vs[p];
+                if (__builtin_amdgcn_readfirstlane(v > unit || (v > 0.f && v < unit * 0.0625f))) {
+                    most_v = fmaxf(most_v, v);
+                    const float now = fmaxf(__uint_as_float((__float_as_uint(v) + 0x7FFFFFu) & 0x7F800000u), most_v * 8.27180613e-25f), less = unit / now;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[m][r], by[m], -base));
-                    sum += p;
-                    const int st = 2 * m + (r >> 3), u = r & 7;
-                    w[0][st][u] = (_Float16)p;
-                    if (TWO) w[TERMS - 1][st][u] = (_Float16)(p - (float)w[0][st][u]);
+                    for (int u = 0; u < ND; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[u][r] *= less;
+                    unit = now;
                 }
+                const float part = v > 0.f ? v / unit : 1.f, off = __builtin_amdgcn_logf(part) - base;
+                constexpr int ST = 4 / PAGES;
+                f16x8 w[TERMS][ST];
+                float sums[2] = {0.f, 0.f};
 #pragma unroll
-            for (int u = 0; u < ND; ++u) {
-                f32x16 part;
+                for (int st = 0; st < ST; ++st) {
+                    const int m = (p * ST + st) >> 1;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) part[r] = 0.f;
-#pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const f16x8 v = *(const f16x8*)(at + v_at(32 * u + n32, 2 * st + half));
-#pragma unroll
-                    for (int x = 0; x < TERMS; ++x) part = mma(v, w[x][st], part);
-                    if (PAGES == 2 && st == 1) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            acc[u][r] = __builtin_fmaf(part[r], vs[0], acc[u][r]);
-                            part[r] = 0.f;
-                        }
+                    for (int u = 0; u < 8; ++u) {
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[m][8 * (st & 1) + u], by[m], off));
+                        sums[u & 1] += e;
+                        w[0][st][u] = (_Float16)e;
+                        if (TWO) w[TERMS - 1][st][u] = (_Float16)(e - (float)w[0][st][u]);
                     }
                 }
+                sum = __builtin_fmaf(sums[0] + sums[1], 1.f / part, sum);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[u][r] = __builtin_fmaf(part[r], vs[PAGES - 1], acc[u][r]);
+                for (int st = 0; st < ST; ++st)
+#pragma unroll
+                    for (int u = 0; u < ND; ++u) {
+                        const f16x8 y = *(const f16x8*)(at + v_at(32 * u + n32, 2 * (p * ST + st) + half));
+#pragma unroll
+                        for (int x = 0; x < TERMS; ++x) acc[u] = mma(y, w[x][st], acc[u]);
+                    }
+                SCHED_V
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -298,10 +324,14 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     uint32_t x, y;
     pair_xor32(__float_as_uint(sum), x, y);
     sum = __uint_as_float(x) + __uint_as_float(y);
+#pragma unroll
+    for (int u = 0; u < ND; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[u][r] *= unit;
     if (splits > 1) {
         // a lane's values lie in memory as it has them, 1 KiB a store of a wave: the last of the tile's workgroups has the same lanes
         constexpr int kPart = kPromptRows * (DP + 4);  // floats: see prompt_part_floats
-        const int64_t tile_at = (int64_t)(unit / a.splits) * c.heads + head;
+        const int64_t tile_at = (int64_t)(place_at / a.splits) * c.heads + head;
         const auto place = [&](int sp) { return make_rsrc(a.part + (tile_at * a.splits + sp) * kPart, sizeof(float) * kPart); };
         const auto mine = place(split);
 #pragma unroll
