@@ -82,13 +82,21 @@ __global__ __launch_bounds__(kThreads) void beams_read_kernel(const BeamsArgs a)
         mine[p] = m;
         top = fmaxf(top, m);
     }
-    const float base = top == -INFINITY ? 0.f : top;
     float s = 0.f;
+    if (fabsf(top) < kFar || top == -INFINITY) {
+        const float whole = whole_above(top);
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s += fexp_full(x[p].z[e] - base);
-    s = wave_sum(s);
+            for (int e = 0; e < E; ++e) s += term(x[p].z[e], whole);
+        s = to_base(wave_sum(s), top);
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += fexp_full(x[p].z[e] - top);
+        s = wave_sum(s);
+    }
     if (lane == 0) {
         a.sums[((int64_t)row * a.parts + blockIdx.x) * kWaves + wave] = make_float2(top, s);
 #pragma unroll
@@ -101,7 +109,8 @@ __global__ __launch_bounds__(kThreads) void beams_read_kernel(const BeamsArgs a)
 
 struct Candidate {
     double rank;
-    int beam, id;
+    float z;
+    int beam, id, unused;
 };
 __device__ __forceinline__ bool better(const Candidate& x, const Candidate& y) {
     return x.rank > y.rank || (x.rank == y.rank && (x.beam < y.beam || (x.beam == y.beam && x.id < y.id)));
@@ -109,93 +118,127 @@ __device__ __forceinline__ bool better(const Candidate& x, const Candidate& y) {
 
 template <class R>
 __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArgs a) {
-    constexpr int E = 16 / R::kBytes, CHUNK = 64 * E;
+    constexpr int E = 16 / R::kBytes, CHUNK = 64 * E, KEPT = 4;  // maxima that a thread keeps from the first pass over them for the second
     typedef typename R::type V;
     __shared__ double base[kMaxBeams], over[kMaxBeams];  // rank = (base + z) / over
+    __shared__ float base_f[kMaxBeams], by_f[kMaxBeams]; // nearly: (base_f + z) * by_f
     __shared__ float group_tops[64];
-    __shared__ float reach;
-    __shared__ int n_chunks, n_list;
+    __shared__ int n_chunks, n_list, far;
     __shared__ int chunk_list[kListed];
     __shared__ Candidate list[kListed + kMaxChoices + kMaxBeams];
     __shared__ Candidate best[kMaxChoices];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row0 = (int64_t)blockIdx.x * a.beams;
     const V* logits = (const V*)a.logits + row0 * a.ld;
-    if (tid == 0) n_chunks = n_list = 0;
+    const int chunks = a.chunks, all = a.beams * chunks;
+    const float* tops = a.tops + row0 * chunks;
+    if (tid == 0) n_chunks = n_list = far = 0;
+    lds_barrier();
+    // (maxima that a thread looks at: neighbours in groups apart)
+    const int u_first = (tid >> 4) + 64 * (tid & 15);
+    float kept[KEPT];
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) kept[k] = tops[min(u_first + k * kPickThreads, all - 1)];
     // ---- what each beam's logits are ranked by
     for (int b = wave; b < a.beams; b += kPickWaves) {
         const float2* part = a.sums + (row0 + b) * a.parts * kWaves;
         const int n = a.parts * kWaves;
+        const float score = a.scores[row0 + b];
+        const bool ended = a.finished && a.finished[row0 + b] != 0;
+        const int length = a.lengths ? a.lengths[row0 + b] : 0;
+        float2 x[KEPT];
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) x[k] = part[min(lane + 64 * k, n - 1)];
         float m = -INFINITY;
-        for (int p = lane; p < n; p += 64) m = fmaxf(m, part[p].x);
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) m = fmaxf(m, x[k].x);
+        for (int p = lane + 64 * KEPT; p < n; p += 64) m = fmaxf(m, part[p].x);
         m = wave_max(m);
         const float from = m == -INFINITY ? 0.f : m;
         double s = 0.0;
-        for (int p = lane; p < n; p += 64) s += (double)(part[p].y * fexp_full(part[p].x - from));
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k)
+            if (lane + 64 * k < n) s += (double)(x[k].y * fexp_full(x[k].x - from));
+        for (int p = lane + 64 * KEPT; p < n; p += 64) s += (double)(part[p].y * fexp_full(part[p].x - from));
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+        const double at = (double)score - ((double)m + log(s));
+        const double to = a.penalty == 0.f ? 1.0 : pow((double)max(ended ? length : length + 1, 1), (double)a.penalty);
         if (lane == 0) {
-            const float score = a.scores[row0 + b];
-            const bool ended = a.finished && a.finished[row0 + b] != 0;
-            const int length = a.lengths ? a.lengths[row0 + b] : 0;
-            const double at = (double)score - ((double)m + log(s));
             base[b] = !ended && fabs(at) < INFINITY ? at : NAN;  // (NaN: this beam's logits offer nothing)
-            over[b] = a.penalty == 0.f ? 1.0 : pow((double)max(ended ? length : length + 1, 1), (double)a.penalty);
+            over[b] = to;
+            const bool live = !ended && fabs(at) < INFINITY;
+            base_f[b] = live ? (float)at : NAN;
+            by_f[b] = (float)(1.0 / to);
+            if (live && !(fabs(at) < 1e30 && to < 1e30 && to > 1e-30)) far = 1;  // (beyond what fp32 can sort)
         }
     }
     __syncthreads();
-    const int chunks = a.chunks, all = a.beams * chunks;
-    const float* tops = a.tops + row0 * chunks;
     const auto rank_of = [&](int b, float z) { return (base[b] + (double)z) / over[b]; };
-    // ---- a rank that `choices` chunks reach: of 64 groups' maxima the choices-th
+    // ---- a rank that `choices` chunks reach: of 64 groups' maxima the choices-th.  In fp32: a sum, a product and what the numbers in them are rounded by are off by less than
+    // 2^-21 of the largest of them, so that who is below it by twice that is not among the best.
+    // (least: -infinity where there are not as many groups; sums beyond fp32 stay in)
+    const auto nearly = [&](int b, float z) { return (base_f[b] + z) * by_f[b]; };
+    const auto slack = [&](int b, float z) { return (fabsf(base_f[b]) + fabsf(z)) * by_f[b] * 9.5367431640625e-7f; };  // 2^-20
+    const auto may = [&](int b, float z, float least) { return z > -INFINITY && base_f[b] == base_f[b] && !(nearly(b, z) + slack(b, z) < least); };
     {
         float top = -INFINITY;
-        for (int u = (tid >> 4) + 64 * (tid & 15); u < all; u += kPickThreads) top = fmaxf(top, (float)rank_of(u / chunks, tops[u]));  // (neighbours in groups apart)
+        const auto see = [&](int u, float z) {
+            const int b = u / chunks;
+            top = fmaxf(top, nearly(b, z) - slack(b, z));
+        };
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k)
+            if (u_first + k * kPickThreads < all) see(u_first + k * kPickThreads, kept[k]);
+        for (int u = u_first + KEPT * kPickThreads; u < all; u += kPickThreads) see(u, tops[u]);
+#pragma unroll
         for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
         if ((lane & 15) == 0) group_tops[tid >> 4] = top;
     }
-    __syncthreads();
-    if (wave == 0) {
+    lds_barrier();
+    float least = -INFINITY;
+    {
         const float mine = group_tops[lane];
         int before = 0;
+#pragma unroll
         for (int k = 0; k < 64; ++k) {
-            const float other = __shfl(mine, k, 64);
+            const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), k));
             before += other > mine || (other == mine && k < lane);
         }
-        if (before == a.choices - 1) reach = mine;
+        least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), (int)__builtin_ctzll(__ballot(before == a.choices - 1))));
     }
-    __syncthreads();
-    const float least = reach;
-    for (int u = tid; u < all; u += kPickThreads) {
-        const float r = (float)rank_of(u / chunks, tops[u]);
-        if (r >= least && r > -INFINITY) {
+    const auto take = [&](int u, float z) {
+        if (may(u / chunks, z, least)) {
             const int at = atomicAdd(&n_chunks, 1);
             if (at < kListed) chunk_list[at] = u;
         }
-    }
-    __syncthreads();
-    const auto add = [&](int b, int id, float z) {
-        const double r = rank_of(b, z);
-        if ((float)r >= least && r > -INFINITY) {
-            const int at = atomicAdd(&n_list, 1);
-            if (at < kListed) list[at] = {r, b, id};
-        }
     };
-    if (n_chunks <= kListed)
-        for (int u = wave; u < n_chunks; u += kPickWaves) {
-            const int b = chunk_list[u] / chunks, i = (chunk_list[u] - b * chunks) * CHUNK + lane * E;
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+        if (u_first + k * kPickThreads < all) take(u_first + k * kPickThreads, kept[k]);
+    for (int u = u_first + KEPT * kPickThreads; u < all; u += kPickThreads) take(u, tops[u]);
+    lds_barrier();
+    const int found = far ? kListed + 1 : n_chunks;
+    if (found <= kListed)
+        for (int u = wave; u < found; u += kPickWaves) {
+            const int c = chunk_list[u], b = c / chunks, i = (c - b * chunks) * CHUNK + lane * E;
             Piece16<R> x;
             x.load(logits + (int64_t)b * a.ld, i, a.vocab);
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (i + e < a.vocab) add(b, i + e, x.z[e]);
+            for (int e = 0; e < E; ++e) {
+                if (i + e < a.vocab && may(b, x.z[e], least)) {
+                    const int at = atomicAdd(&n_list, 1);
+                    if (at < kListed) list[at] = {rank_of(b, x.z[e]), x.z[e], b, i + e, 0};
+                }
+            }
         }
-    __syncthreads();
+    lds_barrier();
     // beams that have ended
     const auto ended_beams = [&] {
         if (tid < a.beams && a.finished && a.finished[row0 + tid] != 0) {
-            const double r = (double)a.scores[row0 + tid] / over[tid];
-            if (r > -INFINITY) list[atomicAdd(&n_list, 1)] = {r, tid, a.pad};
+            const float score = a.scores[row0 + tid];
+            const double r = (double)score / over[tid];
+            if (r > -INFINITY) list[atomicAdd(&n_list, 1)] = {r, score, tid, a.pad, 0};
         }
     };
     // the first of the list in order, `best`; afterwards they are the list
@@ -208,7 +251,8 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
         }
         __syncthreads();
     };
-    if (n_chunks <= kListed && n_list <= kListed) {
+    if (found <= kListed && n_list <= kListed) {
+        lds_barrier();  // (everybody has seen the list's length)
         ended_beams();
         __syncthreads();
         settle(n_list);
@@ -226,7 +270,7 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
             const int mine = u0 + lane;
             // (the best that a chunk can have: its largest at its first id)
             const auto hopes = [&](int v) {
-                const Candidate x = {rank_of(v / chunks, tops[v]), v / chunks, v % chunks * CHUNK};
+                const Candidate x = {rank_of(v / chunks, tops[v]), 0.f, v / chunks, v % chunks * CHUNK, 0};
                 return x.rank > -INFINITY && (n < a.choices || better(x, best[n - 1]));
             };
             // (the list changes from chunk to chunk: looked at again where it is a chunk's turn)
@@ -237,7 +281,8 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
                 if (tid == 0) n_list = n;
                 __syncthreads();
                 for (int at = i + tid; at < min(i + CHUNK, a.vocab); at += kPickThreads) {
-                    const Candidate x = {rank_of(b, R::up(logits[(int64_t)b * a.ld + at])), b, at};
+                    const float z = R::up(logits[(int64_t)b * a.ld + at]);
+                    const Candidate x = {rank_of(b, z), z, b, at, 0};
                     if (x.rank > -INFINITY && (n < a.choices || better(x, best[n - 1]))) list[atomicAdd(&n_list, 1)] = x;
                 }
                 __syncthreads();
@@ -254,11 +299,10 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     const int64_t out0 = (int64_t)blockIdx.x * a.choices;
     if (tid < a.choices) {
         const bool none = tid >= have;
-        const Candidate x = none ? Candidate{0.0, -1, -1} : best[tid];
+        const Candidate x = none ? Candidate{0.0, 0.f, -1, -1, 0} : best[tid];
         const bool ended = !none && a.finished && a.finished[row0 + x.beam] != 0;
         const int length = none || !a.lengths ? 0 : a.lengths[row0 + x.beam];
-        double sum = -INFINITY;
-        if (!none) sum = ended ? (double)a.scores[row0 + x.beam] : base[x.beam] + (double)R::up(logits[(int64_t)x.beam * a.ld + x.id]);
+        const double sum = none ? -INFINITY : ended ? (double)x.z : base[x.beam] + (double)x.z;  // (of one that has ended z is its score)
         a.out_scores[out0 + tid] = (float)sum;
         a.out_parents[out0 + tid] = x.beam;
         a.out_tokens[out0 + tid] = x.id;

@@ -150,6 +150,18 @@ def test_logits_far_from_zero():
         select(z + np.float32(shift) if abs(shift) < 1e6 else np.round(z) + np.float32(shift), F32, 1, 4, 8, np.array([-1.0, -2.0, -1.5, -9.0]))
 
 
+@pytest.mark.parametrize("penalty", [40.0, -40.0, 200.0, -200.0, 1.0])
+def test_penalties_and_scores_far_apart(penalty):
+    """Ranks beyond what fp32 holds are sorted all the same."""
+    rng = np.random.default_rng(11)
+    z = rng.standard_normal((4, 3000)).astype(np.float32)
+    lengths = np.array([3, 4, 5, 3], np.int32)
+    select(z, F32, 1, 4, 8, np.array([-1.0, -2.0, -1.5, -9.0]), lengths, penalty=penalty)
+    select(z, F32, 1, 4, 8, np.array([-1e30, -2e38, -1.5, -3e38]), lengths, penalty=penalty)
+    z[2, 7:] = -1e37
+    select(z, F32, 1, 4, 64, np.array([-1.0, -2.0, -1.5, -9.0]), lengths, penalty=1.0)
+
+
 def test_replays_and_batches_below_the_most():
     rng = np.random.default_rng(10)
     words = pack(rng.standard_normal((12, 3001)), BF16)
