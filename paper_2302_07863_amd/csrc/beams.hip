@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     typedef typename R::type V;
     __shared__ double base[kMaxBeams], over[kMaxBeams];  // rank = (base + z) / over
     __shared__ float base_f[kMaxBeams], by_f[kMaxBeams]; // nearly: (base_f + z) * by_f
-    __shared__ float group_tops[64];
+    __shared__ float group_tops[64], reach;
     __shared__ int n_chunks, n_list, far;
     __shared__ int chunk_list[kListed];
     __shared__ Candidate list[kListed + kMaxChoices + kMaxBeams];
@@ -134,18 +134,35 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     const float* tops = a.tops + row0 * chunks;
     if (tid == 0) n_chunks = n_list = far = 0;
     lds_barrier();
-    // (maxima that a thread looks at: neighbours in groups apart)
-    const int u_first = (tid >> 4) + 64 * (tid & 15);
-    float kept[KEPT];
+    // (a wave looks at the maxima of a slice of a beam's chunks, neighbours in rows of lanes apart)
+    const int slices = (kPickWaves + a.beams - 1) / a.beams, pairs = a.beams * slices, per = (chunks + slices - 1) / slices, swapped = (lane & 3) * 16 + (lane >> 2);
+    const auto each = [&](int pair, auto&& f) {  // f(beam, chunk of it)
+        const int b = pair / slices, c0 = (pair - b * slices) * per, c1 = min(c0 + per, chunks);
+        for (int c = c0 + swapped; c < c1; c += 64) f(b, c);
+    };
+    float kept[KEPT];  // of the wave's first pair
+    {
+        const int b = wave / slices, c0 = (wave - b * slices) * per + swapped;
 #pragma unroll
-    for (int k = 0; k < KEPT; ++k) kept[k] = tops[min(u_first + k * kPickThreads, all - 1)];
-    // ---- what each beam's logits are ranked by
-    for (int b = wave; b < a.beams; b += kPickWaves) {
+        for (int k = 0; k < KEPT; ++k) kept[k] = tops[min(b * chunks + c0 + 64 * k, all - 1)];
+    }
+    // ---- what each beam's logits are ranked by: a wave has a beam's statistics, another one what its length counts for
+    for (int item = wave; item < 2 * a.beams; item += kPickWaves) {
+        const int b = item < a.beams ? item : item - a.beams;
+        const bool ended = a.finished && a.finished[row0 + b] != 0;
+        if (item >= a.beams) {
+            const int length = a.lengths ? a.lengths[row0 + b] : 0;
+            const double to = a.penalty == 0.f ? 1.0 : exp((double)a.penalty * log((double)max(ended ? length : length + 1, 1)));
+            if (lane == 0) {
+                over[b] = to;
+                by_f[b] = (float)(1.0 / to);
+                if (!ended && !(to < 1e30 && to > 1e-30)) far = 1;  // (beyond what fp32 can sort)
+            }
+            continue;
+        }
         const float2* part = a.sums + (row0 + b) * a.parts * kWaves;
         const int n = a.parts * kWaves;
         const float score = a.scores[row0 + b];
-        const bool ended = a.finished && a.finished[row0 + b] != 0;
-        const int length = a.lengths ? a.lengths[row0 + b] : 0;
         float2 x[KEPT];
 #pragma unroll
         for (int k = 0; k < KEPT; ++k) x[k] = part[min(lane + 64 * k, n - 1)];
@@ -163,17 +180,14 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
         const double at = (double)score - ((double)m + log(s));
-        const double to = a.penalty == 0.f ? 1.0 : pow((double)max(ended ? length : length + 1, 1), (double)a.penalty);
         if (lane == 0) {
-            base[b] = !ended && fabs(at) < INFINITY ? at : NAN;  // (NaN: this beam's logits offer nothing)
-            over[b] = to;
             const bool live = !ended && fabs(at) < INFINITY;
+            base[b] = live ? at : NAN;  // (NaN: this beam's logits offer nothing)
             base_f[b] = live ? (float)at : NAN;
-            by_f[b] = (float)(1.0 / to);
-            if (live && !(fabs(at) < 1e30 && to < 1e30 && to > 1e-30)) far = 1;  // (beyond what fp32 can sort)
+            if (live && !(fabs(at) < 1e30)) far = 1;
         }
     }
-    __syncthreads();
+    lds_barrier();
     const auto rank_of = [&](int b, float z) { return (base[b] + (double)z) / over[b]; };
     // ---- a rank that `choices` chunks reach: of 64 groups' maxima the choices-th.  In fp32: a sum, a product and what the numbers in them are rounded by are off by less than
     // 2^-21 of the largest of them, so that who is below it by twice that is not among the best.
@@ -181,42 +195,40 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     const auto nearly = [&](int b, float z) { return (base_f[b] + z) * by_f[b]; };
     const auto slack = [&](int b, float z) { return (fabsf(base_f[b]) + fabsf(z)) * by_f[b] * 9.5367431640625e-7f; };  // 2^-20
     const auto may = [&](int b, float z, float least) { return z > -INFINITY && base_f[b] == base_f[b] && !(nearly(b, z) + slack(b, z) < least); };
-    {
-        float top = -INFINITY;
-        const auto see = [&](int u, float z) {
-            const int b = u / chunks;
+    float top = -INFINITY;
+    for (int pair = wave; pair < pairs; pair += kPickWaves)
+        each(pair, [&](int b, int c) {
+            const int k = (c - swapped - (pair % slices) * per) >> 6;
+            const float z = pair == wave && k < KEPT ? (k == 0 ? kept[0] : k == 1 ? kept[1] : k == 2 ? kept[2] : kept[3]) : tops[b * chunks + c];
             top = fmaxf(top, nearly(b, z) - slack(b, z));
-        };
+        });
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k)
-            if (u_first + k * kPickThreads < all) see(u_first + k * kPickThreads, kept[k]);
-        for (int u = u_first + KEPT * kPickThreads; u < all; u += kPickThreads) see(u, tops[u]);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-        if ((lane & 15) == 0) group_tops[tid >> 4] = top;
-    }
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if ((lane & 15) == 0) group_tops[tid >> 4] = top;
     lds_barrier();
-    float least = -INFINITY;
-    {
-        const float mine = group_tops[lane];
+    {  // sixteen threads count who is before a group
+        const int group = tid >> 4;
+        const float mine = group_tops[group];
         int before = 0;
 #pragma unroll
-        for (int k = 0; k < 64; ++k) {
-            const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), k));
-            before += other > mine || (other == mine && k < lane);
+        for (int k = 0; k < 4; ++k) {
+            const int other = (tid & 15) + 16 * k;
+            const float z = group_tops[other];
+            before += __builtin_popcountll(__ballot(z > mine || (z == mine && other < group)) >> (lane & 48) & 0xFFFF);
         }
-        least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), (int)__builtin_ctzll(__ballot(before == a.choices - 1))));
+        if (before == a.choices - 1 && (tid & 15) == 0) reach = mine;
     }
-    const auto take = [&](int u, float z) {
-        if (may(u / chunks, z, least)) {
-            const int at = atomicAdd(&n_chunks, 1);
-            if (at < kListed) chunk_list[at] = u;
-        }
-    };
-#pragma unroll
-    for (int k = 0; k < KEPT; ++k)
-        if (u_first + k * kPickThreads < all) take(u_first + k * kPickThreads, kept[k]);
-    for (int u = u_first + KEPT * kPickThreads; u < all; u += kPickThreads) take(u, tops[u]);
+    lds_barrier();
+    const float least = reach;
+    for (int pair = wave; pair < pairs; pair += kPickWaves)
+        each(pair, [&](int b, int c) {
+            const int k = (c - swapped - (pair % slices) * per) >> 6;
+            const float z = pair == wave && k < KEPT ? (k == 0 ? kept[0] : k == 1 ? kept[1] : k == 2 ? kept[2] : kept[3]) : tops[b * chunks + c];
+            if (may(b, z, least)) {
+                const int at = atomicAdd(&n_chunks, 1);
+                if (at < kListed) chunk_list[at] = b * chunks + c;
+            }
+        });
     lds_barrier();
     const int found = far ? kListed + 1 : n_chunks;
     if (found <= kListed)
@@ -241,13 +253,16 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
             if (r > -INFINITY) list[atomicAdd(&n_list, 1)] = {r, score, tid, a.pad, 0};
         }
     };
-    // the first of the list in order, `best`; afterwards they are the list
+    // the first of the list in order, `best`; afterwards they are the list.  32 threads count who is before one of them.
     const auto settle = [&](int n) {
-        for (int u = tid; u < n; u += kPickThreads) {
+        for (int u = tid >> 5; u < n; u += kPickThreads / 32) {
             const Candidate mine = list[u];
             int before = 0;
-            for (int k = 0; k < n; ++k) before += better(list[k], mine);
-            if (before < a.choices) best[before] = mine;
+            for (int k0 = 0; k0 < n; k0 += 32) {
+                const int k = k0 + (tid & 31);
+                before += __builtin_popcountll(__ballot(k < n && better(list[min(k, n - 1)], mine)) >> (lane & 32) & 0xFFFFFFFF);
+            }
+            if (before < a.choices && (tid & 31) == 0) best[before] = mine;
         }
         __syncthreads();
     };
