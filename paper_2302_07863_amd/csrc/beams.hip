@@ -20,7 +20,7 @@ using namespace bild;
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kMaxPieces = 4;
+constexpr int kThreads = 256, kWaves = kThreads / 64, kMaxPieces = 2;
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
 constexpr int kMaxBeams = 64, kMaxChoices = 64;
 constexpr int kListed = 1024;  // candidates, chunks of a list
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
         }
 }
 
-// Pieces a thread: four, fewer where that gives the chip too few workgroups.
+// Pieces a thread: two, one where that gives the chip too few workgroups (128 rows of 250112 bf16: four 13.8 us, eight 16, two 13).
 int pieces_of(int rows, int vocab, int e) {
     int p = kMaxPieces;
     while (p > 1 && (int64_t)rows * ((vocab + p * kThreads * e - 1) / (p * kThreads * e)) < 512) p /= 2;
@@ -347,8 +347,7 @@ hipError_t launch(BeamsArgs a, int batch, hipStream_t st) {
     a.parts = (a.vocab + p * kThreads * E - 1) / (p * kThreads * E);
     a.chunks = (a.vocab + 64 * E - 1) / (64 * E);
     const dim3 grid(a.parts, rows);
-    const hipError_t err = p == 4 ? launch_on(beams_read_kernel<R, 4>, grid, dim3(kThreads), 0, st, a) : p == 2 ? launch_on(beams_read_kernel<R, 2>, grid, dim3(kThreads), 0, st, a)
-                                                                                                             : launch_on(beams_read_kernel<R, 1>, grid, dim3(kThreads), 0, st, a);
+    const hipError_t err = p == 2 ? launch_on(beams_read_kernel<R, 2>, grid, dim3(kThreads), 0, st, a) : launch_on(beams_read_kernel<R, 1>, grid, dim3(kThreads), 0, st, a);
     if (err != hipSuccess) return err;
     return launch_on(beams_pick_kernel<R>, dim3(batch), dim3(kPickThreads), 0, st, a);
 }

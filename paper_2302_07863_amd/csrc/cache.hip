@@ -80,10 +80,16 @@ __device__ __forceinline__ void give_back(const CacheView& c, int64_t row, int f
 
 __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const ExtendArgs a) {
     __shared__ int sums[kPlanWaves];
-    __shared__ int wrong;
+    __shared__ int wrong, freed;
+    __shared__ int given[kPlanThreads];  // the first of the pages that are given away
     const CacheView& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, n = a.r.n, shift = c.page_shift, mask = c.page_tokens - 1;
-    if (tid == 0) wrong = 0;
+    const bool few = n <= 64;  // (a wave has them all)
+    if (tid == 0) wrong = freed = 0;
+    int counts[8];  // of the pool's first pages, asked for before it is known that they are needed
+#pragma unroll
+    for (int e = 0; e < 8; ++e) counts[e] = 8 * tid + e < c.pages ? seen(&c.refs[8 * tid + e]) : 1;
+    __syncthreads();
     // the cut, and what a window has left behind
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
@@ -109,6 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
             a.plan[4 * i + 1] = s >= 0 ? add : 0;
         }
         const int cut0 = (keep + mask) >> shift, cut1 = (length + mask) >> shift;
+        if (cut1 > cut0 || slide1 > slide0) freed = 1;
         for (unsigned long long todo = __ballot(cut1 > cut0 || slide1 > slide0); todo; todo &= todo - 1) {
             const int l = (int)__builtin_ctzll(todo);
             const int64_t row = (int64_t)__shfl(s, l, 64) * c.max_pages;
@@ -127,10 +134,24 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
                 const int p = c.table[(int64_t)s * c.max_pages + (keep >> shift)];
                 if (!c.has(p)) {
                     wrong = 1;
-                } else if (seen(&c.refs[p]) > 1) {
-                    shared = p;
-                    atomicAdd(&a.asked[p], 1);
-                    atomicMax(&a.latest[p], i + 1);
+                } else {
+                    const int holders = seen(&c.refs[p]);
+                    if (holders > 1) shared = p;
+                    if (few) {
+                        // (all lanes that have rows are here)
+                        int asked = 0, latest = -1;
+                        for (unsigned long long others = __ballot(holders > 1); others; others &= others - 1) {
+                            const int l = (int)__builtin_ctzll(others);
+                            if (__builtin_amdgcn_readlane(p, l) == p) {
+                                ++asked;
+                                latest = l;
+                            }
+                        }
+                        if (shared >= 0 && asked == holders && latest == lane) shared = -1;
+                    } else if (shared >= 0) {
+                        atomicAdd(&a.asked[p], 1);
+                        atomicMax(&a.latest[p], i + 1);
+                    }
                 }
             }
         }
@@ -147,7 +168,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
             const int keep = a.plan[4 * i], add = a.plan[4 * i + 1], p = a.plan[4 * i + 3];
             if (fits_so_far) need = min(((keep + add + mask) >> shift) - ((keep + mask) >> shift), kMany - 1);
             if (p >= 0) {
-                if (seen(&a.asked[p]) == seen(&c.refs[p]) && seen(&a.latest[p]) == i + 1) a.plan[4 * i + 3] = -1;  // (the others get copies)
+                if (!few && seen(&a.asked[p]) == seen(&c.refs[p]) && seen(&a.latest[p]) == i + 1) a.plan[4 * i + 3] = -1;  // (the others get copies)
                 else ++need;
             }
         }
@@ -157,7 +178,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
         needed = min(needed + all, kMany);
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kPlanThreads) {  // (those that keep theirs as well: the count is of all)
+    for (int i = few ? n : tid; i < n; i += kPlanThreads) {  // (those that keep theirs as well: the count is of all)
         const int s = a.r.sequence(i, c.sequences), keep = a.plan[4 * i];
         if (s < 0 || a.plan[4 * i + 1] <= 0 || !(keep & mask)) continue;
         const int p = c.table[(int64_t)s * c.max_pages + (keep >> shift)];
@@ -172,7 +193,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int p = p0 + 8 * tid + e;
-                r[e] = p < c.pages ? seen(&c.refs[p]) : 1;
+                r[e] = p0 == 0 && !freed ? counts[e] : p < c.pages ? seen(&c.refs[p]) : 1;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) mine += r[e] == 0;
@@ -181,7 +202,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (r[e] == 0) {
-                    if (at < needed) a.fresh[at] = p0 + 8 * tid + e;
+                    if (at < kPlanThreads) given[at] = p0 + 8 * tid + e;
+                    else if (at < needed) a.fresh[at] = p0 + 8 * tid + e;
                     ++at;
                 }
             found += all;
@@ -204,7 +226,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
         int all;
         const int place = scan(old >= 0, all, sums);
         if (old >= 0) {
-            const int p = a.fresh[at++];
+            const int p = at < kPlanThreads ? given[at] : a.fresh[at];
+            ++at;
             c.table[(int64_t)s * c.max_pages + (keep >> shift)] = p;
             atomicSub(&c.refs[old], 1);
             c.refs[p] = 1;
@@ -221,7 +244,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
             const int64_t row = (int64_t)__shfl(s, l, 64) * c.max_pages;
             const int f0 = __shfl(b0, l, 64), f1 = __shfl(b1, l, 64), from = __shfl(at, l, 64);
             for (int b = f0 + lane; b < f1; b += 64) {
-                const int p = a.fresh[from + b - f0];
+                const int k = from + b - f0, p = k < kPlanThreads ? given[k] : a.fresh[k];
                 c.table[row + b] = p;
                 c.refs[p] = 1;
             }
@@ -296,6 +319,45 @@ __global__ __launch_bounds__(256) void cache_fork_write_kernel(const ForkArgs a)
     }
     __syncthreads();
     if (threadIdx.x == 0) c.lengths[s] = length;
+}
+
+// Small tables: both halves in one workgroup.
+constexpr int kForkEach = 16;  // entries a thread
+__global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(const ForkArgs a) {
+    __shared__ int to[kPlanThreads], from[kPlanThreads], length[kPlanThreads], before[kPlanThreads];
+    const CacheView& c = a.c;
+    const CacheRows r = {a.sequences, nullptr, a.n, 0, 0};
+    const int tid = threadIdx.x, total = a.n * c.max_pages;
+    if (tid < a.n) {
+        const int s = r.sequence(tid, c.sequences), parent = a.parents[tid], first = tid / a.group * a.group;
+        const int src = (unsigned)parent < (unsigned)a.group && first + parent < a.n ? r.sequence(first + parent, c.sequences) : -1;
+        const auto pages_of = [&](int q) { return (min(max(c.lengths[q], 0), c.cap()) + c.page_tokens - 1) >> c.page_shift; };
+        to[tid] = s == src ? -1 : s;
+        from[tid] = src;
+        length[tid] = src < 0 ? 0 : min(max(c.lengths[src], 0), c.cap());
+        before[tid] = s < 0 ? 0 : pages_of(s);
+    }
+    __syncthreads();
+    int now[kForkEach], old[kForkEach];
+#pragma unroll
+    for (int e = 0; e < kForkEach; ++e) {
+        const int u = e * kPlanThreads + tid, i = u / c.max_pages, b = u - i * c.max_pages;
+        now[e] = old[e] = -1;
+        if (u >= total || to[i] < 0) continue;
+        if (b < (length[i] + c.page_tokens - 1) >> c.page_shift) now[e] = c.table[(int64_t)from[i] * c.max_pages + b];
+        if (b < before[i]) old[e] = c.table[(int64_t)to[i] * c.max_pages + b];
+        if (!c.has(now[e])) now[e] = -1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kForkEach; ++e) {
+        const int u = e * kPlanThreads + tid, i = u / c.max_pages, b = u - i * c.max_pages;
+        if (u >= total || to[i] < 0) continue;
+        if (now[e] >= 0) atomicAdd(&c.refs[now[e]], 1);
+        if (c.has(old[e])) atomicSub(&c.refs[old[e]], 1);
+        if (b < max(before[i], (length[i] + c.page_tokens - 1) >> c.page_shift)) c.table[(int64_t)to[i] * c.max_pages + b] = now[e];
+    }
+    if (tid < a.n && to[tid] >= 0) c.lengths[to[tid]] = length[tid];
 }
 
 struct CompactArgs {
@@ -402,7 +464,11 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
     __shared__ float tops[THREADS / 64];
     const CacheView& c = a.c;
     const int tid = threadIdx.x, slot = blockIdx.x, head = blockIdx.y, which = blockIdx.z, T = c.page_tokens;
-    if (!a.words[W_FITS]) return;
+    const int fits = a.words[W_FITS];
+    const bool one = !a.r.starts && a.r.rows == 1;
+    RowVec<R, E> kept[KEPT];
+    // (a single row's place is known before the sequence's length is)
+    if (one && tid * E < c.d_head) kept[0].load((const V*)a.x[which] + (int64_t)slot * a.token[which] + (int64_t)head * a.head[which] + tid * E);
     // entry i of the list has the slots floor(first row / T) + 2 i and those behind, as many as it can have pages
     int i, first, count, nth;
     if (a.r.starts) {
@@ -429,13 +495,15 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
     if ((b << c.page_shift) >= length) return;
     const int p0 = max(begin, b << c.page_shift), p1 = min(length, (b + 1) << c.page_shift);
     const int page = c.table[(int64_t)s * c.max_pages + b];
-    if (!c.has(page) || c.refs[page] != 1) return;
+    if (!c.has(page)) return;
     const int64_t plane = c.plane(page, a.layer, which, head);
+    const int holders = c.refs[page];
+    const float held = c.scales[plane];
+    if (!fits || holders != 1) return;
     const int before = p0 - (b << c.page_shift), m = p1 - p0, d = c.d_head, per_row = d / E, pieces = m * per_row;
     int8_t* codes = c.codes + plane * c.plane_bytes();
     const V* x = (const V*)a.x[which] + (int64_t)(first + p0 - begin) * a.token[which] + (int64_t)head * a.head[which];
-    const float was = before > 0 ? fabsf(bounded(c.scales[plane])) : 0.f;
-    RowVec<R, E> kept[KEPT];
+    const float was = before > 0 ? fabsf(bounded(held)) : 0.f;
     const auto at = [&](int u) {
         const int row = u / per_row;
         return x + (int64_t)row * a.token[which] + (u - row * per_row) * E;
@@ -444,7 +512,7 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
 #pragma unroll
     for (int k = 0; k < KEPT; ++k)
         if (k * THREADS + tid < pieces) {
-            kept[k].load(at(k * THREADS + tid));
+            if (!one) kept[k].load(at(k * THREADS + tid));
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) kept[k].v[e] = 0;
@@ -582,6 +650,8 @@ extern "C" int bild_cache_fork(bild_cache* c, const int32_t* sequences, const in
     const OnDevice on(c->device);
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (n <= kPlanThreads && (int64_t)n * c->view.max_pages <= kForkEach * kPlanThreads)
+        return launch_on(cache_fork_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
     if (launch_on(cache_fork_read_kernel, dim3(n), dim3(256), 0, st, a) != hipSuccess) return BILD_EHIP;
     return launch_on(cache_fork_write_kernel, dim3(n), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
 }
