@@ -31,11 +31,16 @@ struct ExtendArgs {
     const int* cut;
     int* granted;
     int window, sinks;
-    int *plan;             // [sequences][4]: length after the cut, new rows, pages needed before it in the list, page to be copied (-1: none)
+    int *plan;             // [sequences][4], 16-byte aligned: entries
     int *fresh;            // [pages]: the free pages that are given away, lowest first
     int *asked, *latest;   // [pages], zero between launches: how many of a shared page's holders want to write into it, the last of these + 1
     int* copies;           // [sequences][3]: from, to, positions
     int* words;
+};
+
+// Entry i of a list: its sequence, length after the cut, new rows, pages needed before it in the list, shared page that has to be copied (-1: none).
+struct Entry {
+    int keep, add, before, shared, s;
 };
 
 __device__ __forceinline__ int seen(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -90,6 +95,17 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
 #pragma unroll
     for (int e = 0; e < 8; ++e) counts[e] = 8 * tid + e < c.pages ? seen(&c.refs[8 * tid + e]) : 1;
     __syncthreads();
+    // (a thread's first entry stays in registers, further ones of long lists go through memory)
+    Entry mine = {0, 0, 0, -1, -1};
+    const auto entry = [&](int i) {
+        if (i < kPlanThreads) return mine;
+        const int4 q = *(const int4*)(a.plan + 4 * (int64_t)i);
+        return Entry{q.x, q.y, q.z, q.w, a.r.sequence(i, c.sequences)};
+    };
+    const auto put = [&](int i, const Entry& q) {
+        if (i < kPlanThreads) mine = q;
+        else *(int4*)(a.plan + 4 * (int64_t)i) = make_int4(q.keep, q.add, q.before, q.shared);
+    };
     // the cut, and what a window has left behind
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
@@ -110,10 +126,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
             }
             if (keep != length) c.lengths[s] = keep;
         }
-        if (i < n) {
-            a.plan[4 * i] = keep;
-            a.plan[4 * i + 1] = s >= 0 ? add : 0;
-        }
+        if (i < n) put(i, {keep, s >= 0 ? add : 0, 0, -1, s});
         const int cut0 = (keep + mask) >> shift, cut1 = (length + mask) >> shift;
         if (cut1 > cut0 || slide1 > slide0) freed = 1;
         for (unsigned long long todo = __ballot(cut1 > cut0 || slide1 > slide0); todo; todo &= todo - 1) {
@@ -126,7 +139,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
     __syncthreads();
     // pages that are shared and would be written
     for (int i = tid; i < n; i += kPlanThreads) {
-        const int s = a.r.sequence(i, c.sequences), keep = a.plan[4 * i], add = a.plan[4 * i + 1];
+        Entry q = entry(i);
+        const int s = q.s, keep = q.keep, add = q.add;
         int shared = -1;
         if (s >= 0 && add > 0) {
             if ((int64_t)keep + add > c.cap()) wrong = 1;
@@ -155,7 +169,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
                 }
             }
         }
-        a.plan[4 * i + 3] = shared;
+        q.shared = shared;
+        put(i, q);
     }
     __threadfence_block();
     __syncthreads();
@@ -164,24 +179,27 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid;
         int need = 0;
+        Entry q = {0, 0, 0, -1, -1};
         if (i < n) {
-            const int keep = a.plan[4 * i], add = a.plan[4 * i + 1], p = a.plan[4 * i + 3];
+            q = entry(i);
+            const int keep = q.keep, add = q.add, p = q.shared;
             if (fits_so_far) need = min(((keep + add + mask) >> shift) - ((keep + mask) >> shift), kMany - 1);
             if (p >= 0) {
-                if (!few && seen(&a.asked[p]) == seen(&c.refs[p]) && seen(&a.latest[p]) == i + 1) a.plan[4 * i + 3] = -1;  // (the others get copies)
+                if (!few && seen(&a.asked[p]) == seen(&c.refs[p]) && seen(&a.latest[p]) == i + 1) q.shared = -1;  // (the others get copies)
                 else ++need;
             }
         }
         int all;
         const int before = scan(need, all, sums);
-        if (i < n) a.plan[4 * i + 2] = needed + before;
+        q.before = needed + before;
+        if (i < n) put(i, q);
         needed = min(needed + all, kMany);
     }
     __syncthreads();
     for (int i = few ? n : tid; i < n; i += kPlanThreads) {  // (those that keep theirs as well: the count is of all)
-        const int s = a.r.sequence(i, c.sequences), keep = a.plan[4 * i];
-        if (s < 0 || a.plan[4 * i + 1] <= 0 || !(keep & mask)) continue;
-        const int p = c.table[(int64_t)s * c.max_pages + (keep >> shift)];
+        const Entry q = entry(i);
+        if (q.s < 0 || q.add <= 0 || !(q.keep & mask)) continue;
+        const int p = c.table[(int64_t)q.s * c.max_pages + (q.keep >> shift)];
         if (c.has(p)) a.asked[p] = a.latest[p] = 0;
     }
     // the free pages, lowest first
@@ -215,14 +233,11 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
     // they are handed out
     int copies = 0;
     for (int i0 = 0; fits && i0 < n; i0 += kPlanThreads) {
-        const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
-        int keep = 0, add = 0, at = 0, old = -1;
-        if (s >= 0) {
-            keep = a.plan[4 * i];
-            add = a.plan[4 * i + 1];
-            at = a.plan[4 * i + 2];
-            old = a.plan[4 * i + 3];
-        }
+        const int i = i0 + tid;
+        Entry q = {0, 0, 0, -1, -1};
+        if (i < n) q = entry(i);
+        const int s = q.s, keep = q.keep, add = q.add, old = s >= 0 ? q.shared : -1;
+        int at = q.before;
         int all;
         const int place = scan(old >= 0, all, sums);
         if (old >= 0) {
@@ -422,6 +437,8 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_kernel(const Compa
 }
 
 // Whole pages; the first workgroups' threads turn the tables.
+// (us, 150 pages of 512 KiB: pieces of 4 KiB and 2048, 8192 workgroups 17.5, 15.5; of 16 KiB 27.9)
+constexpr int kPiece = 4096, kMoveGroups = 8192;  // bytes of a turn
 __global__ __launch_bounds__(256) void cache_move_kernel(const CompactArgs a) {
     const CacheView& c = a.c;
     const int tid = threadIdx.x, used = a.words[W_USED], moves = a.words[W_MOVES];
@@ -434,12 +451,14 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const CompactArgs a) {
             if (p >= used && c.has(p)) *entry = a.to[p];
         }
     }
-    const int64_t page_bytes = (int64_t)c.layers * 2 * c.heads * c.plane_bytes(), pieces = (page_bytes + 4095) / 4096;
+    const int64_t page_bytes = (int64_t)c.layers * 2 * c.heads * c.plane_bytes(), pieces = (page_bytes + kPiece - 1) / kPiece;
     const int planes = c.layers * 2 * c.heads;
     for (int64_t u = blockIdx.x; u < moves * pieces; u += gridDim.x) {
         const int k = (int)(u / pieces);
-        const int64_t from = a.moves[2 * k], to = a.moves[2 * k + 1], b = (u - k * pieces) * 4096 + tid * 16;
-        if (b < page_bytes) *(uint4*)(c.codes + to * page_bytes + b) = *(const uint4*)(c.codes + from * page_bytes + b);  // (page_bytes: a multiple of 256)
+        const int64_t from = a.moves[2 * k], to = a.moves[2 * k + 1], b = (u - k * pieces) * kPiece + tid * 16;
+        const int8_t* src = c.codes + from * page_bytes;
+        int8_t* dst = c.codes + to * page_bytes;
+        if (b < page_bytes) *(uint4*)(dst + b) = *(const uint4*)(src + b);  // (a page's bytes: a multiple of 256)
         if (u == k * pieces)
             for (int p = tid; p < planes; p += 256) c.scales[to * planes + p] = c.scales[from * planes + p];
     }
@@ -592,7 +611,7 @@ extern "C" int bild_cache_create(const bild_cache_config* cfg, bild_cache** out)
                g.d_head, g.sequences, g.max_pages};
     const size_t seqs = (size_t)g.sequences, pages = (size_t)g.pages, counts = attend_counts(g.heads);
     // (asked, latest, counts of arrivals and words begin as zeros)
-    const size_t zeros = 2 * pages + counts + W_COUNT, ints = zeros + 7 * seqs + 4 * pages + seqs * (size_t)g.max_pages;
+    const size_t zeros = (2 * pages + counts + W_COUNT + 3) / 4 * 4, ints = zeros + 7 * seqs + 4 * pages + seqs * (size_t)g.max_pages;
     const size_t bytes = (ints * 4 + 255) / 256 * 256, floats = attend_part_floats(g.heads, g.d_head);
     int rc = BILD_OK;
     const int one = 1;
@@ -603,7 +622,7 @@ extern "C" int bild_cache_create(const bild_cache_config* cfg, bild_cache** out)
         c->asked = c->words + W_COUNT;
         c->latest = c->asked + pages;
         c->arrived = (unsigned*)(c->latest + pages);
-        c->plan = (int*)(c->arrived + counts);
+        c->plan = c->words + zeros;
         c->fresh = c->plan + 7 * seqs;
         c->moves = c->fresh + pages;
         c->rows = c->moves + 3 * pages;
@@ -663,7 +682,7 @@ extern "C" int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
     if (launch_on(cache_compact_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) != hipSuccess) return BILD_EHIP;
-    return launch_on(cache_move_kernel, dim3(2048), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
+    return launch_on(cache_move_kernel, dim3(kMoveGroups), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
 }
 
 extern "C" int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* hip_stream) {
