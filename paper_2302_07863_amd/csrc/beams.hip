@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     typedef typename R::type V;
     __shared__ double base[kMaxBeams], over[kMaxBeams];  // rank = (base + z) / over
     __shared__ float base_f[kMaxBeams], by_f[kMaxBeams]; // nearly: (base_f + z) * by_f
-    __shared__ float group_tops[64], reach;
+    __shared__ float group_tops[kPickThreads / 4], reach;
     __shared__ int n_chunks, n_list, far;
     __shared__ int chunk_list[kListed];
     __shared__ Candidate list[kListed + kMaxChoices + kMaxBeams];
@@ -134,8 +134,10 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     const float* tops = a.tops + row0 * chunks;
     if (tid == 0) n_chunks = n_list = far = 0;
     lds_barrier();
-    // (a wave looks at the maxima of a slice of a beam's chunks, neighbours in rows of lanes apart)
-    const int slices = (kPickWaves + a.beams - 1) / a.beams, pairs = a.beams * slices, per = (chunks + slices - 1) / slices, swapped = (lane & 3) * 16 + (lane >> 2);
+    // Groups of 16 or 4 lanes: four times as many as choices at least, or the threshold would be among the low ones of their maxima.  A wave looks at the maxima of a slice of a beam's
+    // chunks, neighbours in groups apart.
+    const int width = a.choices <= 16 ? 16 : 4, groups = kPickThreads / width;
+    const int slices = (kPickWaves + a.beams - 1) / a.beams, pairs = a.beams * slices, per = (chunks + slices - 1) / slices, swapped = lane / width + 64 / width * (lane & (width - 1));
     const auto each = [&](int pair, auto&& f) {  // f(beam, chunk of it)
         const int b = pair / slices, c0 = (pair - b * slices) * per, c1 = min(c0 + per, chunks);
         for (int c = c0 + swapped; c < c1; c += 64) f(b, c);
@@ -189,7 +191,7 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     }
     lds_barrier();
     const auto rank_of = [&](int b, float z) { return (base[b] + (double)z) / over[b]; };
-    // ---- a rank that `choices` chunks reach: of 64 groups' maxima the choices-th.  In fp32: a sum, a product and what the numbers in them are rounded by are off by less than
+    // ---- a rank that `choices` chunks reach: of groups' maxima the choices-th.  In fp32: a sum, a product and what the numbers in them are rounded by are off by less than
     // 2^-21 of the largest of them, so that who is below it by twice that is not among the best.
     // (least: -infinity where there are not as many groups; sums beyond fp32 stay in)
     const auto nearly = [&](int b, float z) { return (base_f[b] + z) * by_f[b]; };
@@ -202,21 +204,19 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
             const float z = pair == wave && k < KEPT ? (k == 0 ? kept[0] : k == 1 ? kept[1] : k == 2 ? kept[2] : kept[3]) : tops[b * chunks + c];
             top = fmaxf(top, nearly(b, z) - slack(b, z));
         });
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    if ((lane & 15) == 0) group_tops[tid >> 4] = top;
+    for (int o = width / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if ((lane & (width - 1)) == 0) group_tops[tid / width] = top;
     lds_barrier();
-    {  // sixteen threads count who is before a group
-        const int group = tid >> 4;
+    {  // the group's threads count who is before it
+        const int group = tid / width;
         const float mine = group_tops[group];
         int before = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int other = (tid & 15) + 16 * k;
+        for (int other = tid & (width - 1); other < groups; other += width) {
             const float z = group_tops[other];
-            before += __builtin_popcountll(__ballot(z > mine || (z == mine && other < group)) >> (lane & 48) & 0xFFFF);
+            before += z > mine || (z == mine && other < group);
         }
-        if (before == a.choices - 1 && (tid & 15) == 0) reach = mine;
+        for (int o = width / 2; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+        if (before == a.choices - 1 && (tid & (width - 1)) == 0) reach = mine;
     }
     lds_barrier();
     const float least = reach;

@@ -89,7 +89,7 @@ def select(words, dtype, batch, beams, choices, scores, lengths=None, finished=N
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("batch,beams,vocab,choices", [(1, 1, 1, 1), (1, 4, 7, 4), (2, 3, 255, 6), (3, 4, 1000, 8), (1, 5, 32128, 5), (2, 8, 50257, 16), (1, 2, 250112, 4), (5, 1, 4097, 64),
+@pytest.mark.parametrize("batch,beams,vocab,choices", [(1, 1, 1, 1), (1, 4, 7, 4), (2, 3, 255, 6), (3, 4, 1000, 8), (1, 5, 32128, 5), (2, 8, 50257, 16), (1, 2, 250112, 4), (5, 1, 4097, 64), (1, 12, 20000, 24), (1, 32, 8192, 64), (2, 5, 1009, 10),
                                                        (1, 64, 513, 64)])
 def test_sizes(dtype, batch, beams, vocab, choices):
     rng = np.random.default_rng(vocab + beams)
