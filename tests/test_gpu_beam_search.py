@@ -1,0 +1,167 @@
+"""A beam search as a program would write it: prompts, 4-bit projections, rotary positions, the cache in 8 bits in pages that beams share, rules on logits, the choice - and every step against
+the definitions in 64 bits, on what the step before has left on the device."""
+import numpy as np
+import pytest
+
+import paper_2302_07863_amd as pkg
+from tests.cached import Held, Oracle, invariants
+from tests.hipmem import DeviceArray
+from tests.rows import F16, F32, U32, close, ruled, scales_of, turned, weights
+from tests.test_gpu_beams import choose
+
+pytestmark = pytest.mark.gpu
+
+D, HQ, HK, DH, VOCAB, BATCH, BEAMS, STEPS = 96, 4, 2, 32, 500, 2, 3, 40
+EOS, PAD = 7, 0
+
+
+def matrix(rng, n, k, spread):
+    codes, scales, _ = pkg.quant_round((spread * rng.standard_normal((n, k))).astype(np.float32), 32)
+    return pkg.Quant(n, k, 32, codes, scales, F16), weights(codes, scales_of(scales, F16), None, k, 32)
+
+
+class Program:
+    def __init__(self, window, sinks):
+        rng = np.random.default_rng(17)
+        self.rng, self.window, self.sinks = rng, window, sinks
+        self.emb = rng.standard_normal((VOCAB, D)).astype(np.float32)
+        self.q, self.k, self.v = (matrix(rng, n, D, 0.15) for n in (HQ * DH, HK * DH, HK * DH))
+        self.head = matrix(rng, VOCAB, HQ * DH, 0.6)
+        self.gain = (1 + 0.1 * rng.standard_normal(D)).astype(np.float32)
+        self.gain_dev = DeviceArray(self.gain)
+        self.rotary = pkg.Rotary(DH, halves=True)
+        self.n = BATCH * BEAMS
+        self.cache = Held(Oracle(70, 32, 1, HK, DH, self.n, 12))
+        self.rules = pkg.Rules(VOCAB, self.n)
+        self.beams = pkg.Beams(VOCAB, BATCH, BEAMS)
+
+    def project(self, m, x_dev, x, rows):
+        quant, w = m
+        y = DeviceArray(nbytes=4 * rows * quant.n)
+        quant.matmul(x_dev.ptr.value, F32, rows, y.ptr.value, F32, gain=self.gain_dev.ptr.value, eps=1e-6)
+        got = y.to_host(np.float32, rows * quant.n).reshape(rows, quant.n)
+        xn = x.astype(np.float64)
+        xn = xn * self.gain / np.sqrt(np.mean(xn * xn, axis=1, keepdims=True) + 1e-6)
+        close(got, xn @ w.T, 2 * D * U32 * (np.abs(xn) @ np.abs(w).T) + 1e-30)
+        return y, got
+
+    def turn(self, y, got, heads, positions, pos_dev):
+        rows = len(positions)
+        self.rotary.apply(DH, F32, rows, pkg.RotaryRows(y.ptr.value, y.ptr.value, heads, heads * DH, DH, heads * DH, DH), positions=pos_dev.ptr.value)
+        out = y.to_host(np.float32, got.size).reshape(rows, heads, DH)
+        f, m = self.rotary.frequencies()
+        size = np.max(np.abs(got.reshape(rows, heads, DH)), axis=2, keepdims=True)
+        close(out, turned(got.reshape(rows, heads, DH).astype(np.float64), positions, f, m, True), 6 * U32 * size + 1e-30)
+        return out
+
+    def rows(self, tokens, counts, sequences, logits_of):
+        """New tokens through the layer; the logits of the rows `logits_of`."""
+        o, total = self.cache.o, len(tokens)
+        ids = DeviceArray(np.asarray(sequences, np.int32))
+        starts = DeviceArray(np.concatenate(([0], np.cumsum(counts))).astype(np.int32))
+        granted = DeviceArray(np.array([9], np.int32))
+        assert o.extend(counts, sequences, window=self.window, sinks=self.sinks)
+        self.cache.cache.extend(len(counts), sequences=ids.ptr.value, starts=starts.ptr.value, granted=granted.ptr.value, window=self.window, sinks=self.sinks)
+        assert granted.to_host(np.int32, 1)[0] == 1
+        positions = np.concatenate([np.arange(o.lengths[s] - c, o.lengths[s]) for s, c in zip(sequences, counts)]).astype(np.int32)
+        x = self.emb[np.asarray(tokens)]
+        x_dev, pos_dev = DeviceArray(x), DeviceArray(positions)
+        yq, q = self.project(self.q, x_dev, x, total)
+        yk, k = self.project(self.k, x_dev, x, total)
+        yv, v = self.project(self.v, x_dev, x, total)
+        q, k = self.turn(yq, q, HQ, positions, pos_dev), self.turn(yk, k, HK, positions, pos_dev)
+        most = int(max(counts))
+        self.cache.cache.append(0, F32, len(counts), most, yk.ptr.value, yv.ptr.value, sequences=ids.ptr.value, starts=starts.ptr.value, tokens=total)
+        o.append(0, k, v.reshape(total, HK, DH), counts, sequences)
+        out = DeviceArray(nbytes=4 * total * HQ * DH)
+        self.cache.cache.attend(0, F32, len(counts), most, HQ, yq.ptr.value, out.ptr.value, DH ** -0.5, sequences=ids.ptr.value, starts=starts.ptr.value, tokens=total,
+                                window=self.window, sinks=self.sinks)
+        got = out.to_host(np.float32, total * HQ * DH).reshape(total, HQ, DH)
+        want, _, tol, _ = o.attend(0, q.astype(np.float64), counts, float(np.float32(DH ** -0.5)), sequences, window=self.window, sinks=self.sinks)
+        close(got, want, tol)
+        self.cache.same()
+        last = got.reshape(total, -1)[logits_of]
+        last_dev, logits = DeviceArray(last), DeviceArray(nbytes=4 * len(logits_of) * VOCAB)
+        self.head[0].matmul(last_dev.ptr.value, F32, len(logits_of), logits.ptr.value, F32)
+        z = logits.to_host(np.float32, len(logits_of) * VOCAB).reshape(-1, VOCAB)
+        close(z, last.astype(np.float64) @ self.head[1].T, 2 * HQ * DH * U32 * (np.abs(last.astype(np.float64)) @ np.abs(self.head[1]).T) + 1e-30)
+        return logits
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (24, 3)])
+def test_beam_search(window, sinks):
+    p = Program(window, sinks)
+    n, rng = p.n, p.rng
+    prompts = [rng.integers(8, VOCAB, 45), rng.integers(8, VOCAB, 32)]
+    heads_of = [b * BEAMS for b in range(BATCH)]
+    logits = p.rows(np.concatenate(prompts), [45, 32], heads_of, [44, 76])
+    # every beam begins as a copy of its sentence's first
+    parents = DeviceArray(np.zeros(n, np.int32))
+    p.cache.o.fork(np.zeros(n, int), None, BEAMS)
+    p.cache.cache.fork(n, parents.ptr.value, group=BEAMS)
+    p.cache.same()
+    z0 = logits.to_host(np.float32, BATCH * VOCAB).reshape(BATCH, VOCAB)
+    logits = DeviceArray(np.repeat(z0, BEAMS, axis=0))
+    scores = np.tile([0.0, -np.inf, -np.inf], BATCH).astype(np.float32)
+    lengths, finished = np.zeros(n, np.int32), np.zeros(n, np.int32)
+    history = np.zeros((n, 0), np.int32)
+    copied = 0
+    for step in range(STEPS):
+        if step:
+            tokens = history[:, -1]
+            logits = p.rows(tokens, [1] * n, list(range(n)), list(range(n)))
+        # a token that was said is less likely
+        if step:
+            said, said_at = DeviceArray(history), DeviceArray(np.full(n, step, np.int32))
+            pen, ruled_dev = DeviceArray(np.array([1.2, 0.0, 0.0], np.float32)), DeviceArray(nbytes=4 * n * VOCAB)
+            before = logits.to_host(np.float32, n * VOCAB).reshape(n, VOCAB)
+            p.rules.apply(logits.ptr.value, F32, n, out=ruled_dev.ptr.value, tokens=said.ptr.value, tokens_stride=step, lengths=said_at.ptr.value, penalties=pen.ptr.value,
+                          penalties_stride=0, max_tokens=step)
+            logits = ruled_dev
+            z = logits.to_host(np.float32, n * VOCAB).reshape(n, VOCAB)
+            for r in range(n):
+                want = ruled(before[r], history[r], step, 0, [np.float32(1.2), 0.0, 0.0])
+                close(z[r], want, U32 * np.abs(want) * 1.001)
+        dev = {k: DeviceArray(v) for k, v in (("scores", scores), ("lengths", lengths), ("finished", finished))}
+        outs = {k: DeviceArray(nbytes=4 * n) for k in ("scores", "parents", "tokens", "lengths", "finished")}
+        past, told = DeviceArray(history if step else np.zeros(1, np.int32)), DeviceArray(nbytes=4 * n * (step + 1))
+        p.beams.select(logits.ptr.value, F32, BATCH, BEAMS, dev["scores"].ptr.value, outs["scores"].ptr.value, outs["parents"].ptr.value, outs["tokens"].ptr.value,
+                       lengths=dev["lengths"].ptr.value, finished=dev["finished"].ptr.value, out_lengths=outs["lengths"].ptr.value, out_finished=outs["finished"].ptr.value,
+                       eos=EOS, pad=PAD, penalty=0.8, history=past.ptr.value, history_stride=step, out_history=told.ptr.value, out_history_stride=step + 1, steps=step)
+        got = {k: v.to_host(np.float32 if k == "scores" else np.int32, n) for k, v in outs.items()}
+        z = logits.to_host(np.float32, n * VOCAB).reshape(n, VOCAB).astype(np.float64)
+        for b in range(BATCH):
+            at = slice(b * BEAMS, (b + 1) * BEAMS)
+            want = choose(z[at], scores[at], BEAMS, lengths[at], finished[at], EOS, PAD, 0.8, history[at])
+            for name in ("parents", "tokens", "lengths", "finished"):
+                assert np.array_equal(got[name][at], want[name]), (step, name)
+            close(got["scores"][at], want["scores"], 2.0 ** -19 + 2.0 ** -22 * np.abs(want["scores"]))
+            assert np.array_equal(told.to_host(np.int32, n * (step + 1)).reshape(n, -1)[at], want["history"])
+        scores, lengths, finished = got["scores"], got["lengths"], got["finished"]
+        history = told.to_host(np.int32, n * (step + 1)).reshape(n, step + 1)
+        p.cache.o.fork(got["parents"], None, BEAMS)
+        p.cache.cache.fork(n, outs["parents"].ptr.value, group=BEAMS)
+        p.cache.same()
+        invariants(p.cache.o)
+        copied += int(np.sum(got["parents"].reshape(BATCH, BEAMS) != np.arange(BEAMS)))
+        if step % 9 == 5:
+            p.cache.o.compact()
+            p.cache.cache.compact()
+            p.cache.same()
+    assert copied > 5 and np.all(np.diff(scores.reshape(BATCH, BEAMS) / np.maximum(lengths.reshape(BATCH, BEAMS), 1) ** 0.8, axis=1) <= 1e-6)
+
+
+def test_reviews_of_drafts():
+    """The other way to use the cache: drafts are appended, a review cuts those it does not accept, and the next drafts take their places."""
+    p = Program(0, 0)
+    rng, o = p.rng, p.cache.o
+    p.rows(rng.integers(0, VOCAB, 70), [40, 30], [1, 4], [0])
+    for accepted in ([3, 0], [7, 1], [0, 5], [2, 2]):
+        counts = [8, 6]
+        p.rows(rng.integers(0, VOCAB, 14), counts, [1, 4], [0])
+        keep = np.array([o.lengths[1] - 8 + accepted[0], o.lengths[4] - 6 + accepted[1]], np.int32)
+        ids, cut = DeviceArray(np.array([1, 4], np.int32)), DeviceArray(keep)
+        assert o.extend([0, 0], [1, 4], cut=keep)
+        p.cache.cache.extend(2, 0, sequences=ids.ptr.value, cut=cut.ptr.value)
+        p.cache.same()
+        assert list(o.lengths[[1, 4]]) == list(keep)
