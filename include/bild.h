@@ -439,7 +439,7 @@ int bild_rules_apply(bild_rules* r, const bild_rules_call* call, void* hip_strea
 /* ---- a cache of keys and values in 8 bits, in pages ----
  * For callers with sequences of their own (batches, beams, drafts): keys and values of any number of sequences in one pool of pages that sequences may share.
  * A page holds page_tokens consecutive positions of a sequence: for each layer, keys and values and each key head their codes in one piece, and a scale, the
- * value that code 127 stands for: code c is c * scale / 127.  The arrays are DEVICE memory of the caller, who may read them, save them and bring them back, and has to keep them
+ * value that code 127 stands for (not negative, at most 2^90): code c is c * scale / 127.  The arrays are DEVICE memory of the caller, who may read them, save them and bring them back, and has to keep them
  * where they are while the handle lives.  An empty cache has lengths and refs of 0 and -1 throughout the table; of a page that no sequence holds, codes and scales are not read.
  * Entries of the table that are no page's number count as none, also where a row would see them; lengths are limited to 0 .. max_pages * page_tokens.
  * Sequences are grown, cut, forked and freed on the device, by numbers that a device array may hold (a beam's parents), so none of these calls waits, and all may be
@@ -488,7 +488,7 @@ int bild_cache_fork(bild_cache* c, const int32_t* sequences /* [n], nullable */,
 int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream);
 
 /* Writes keys and values of one layer for the last rows of each sequence, which bild_cache_extend has made room for.  A page's scale becomes the largest magnitude among its positions, of which
- * those that were there are rounded once more if it grows: codes are the nearest to 127 x / scale (fp32), with scale, the products and quotients in fp32.  Values beyond 2^120 are limited to it, NaN counts as 0.
+ * those that were there are rounded once more if it grows: codes are the nearest to 127 x / scale (fp32), with scale, the products and quotients in fp32.  Magnitudes beyond 2^90 are limited to it, NaN counts as 0.
  * Pages that several sequences hold are not written. */
 typedef struct bild_cache_append_call {
     const void* k;            /* head h of row t at k + t * k_token + h * k_head, its d_head values side by side */
@@ -509,8 +509,9 @@ int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* h
  * and the first `sinks`; without `causal` all of the sequence (window 0 then).
  *   out[t][h] = sum over j of p_j v_j,  p = softmax of scale * q[t][h] k_j,  lse = ln of the sum of e^(scale * q k_j)
  * Query head h has the key head h / (heads / key heads).  A row that sees nothing: out 0, lse -infinity.  Products are those of q as fp16, times a power of two that puts the largest of its row below 2^15
- * (fp32: two fp16 parts), with the codes themselves; weights of the values are fp16 (fp32 rows: two parts); sums are fp32; out is rounded once.  A row whose q has an infinity or NaN, or
- * whose products go beyond fp32, has no finite result and leaves the others alone. */
+ * (fp32: two fp16 parts), with the codes themselves; weights of the values, for many rows with the ratio of their page's scale to others, are fp16 (fp32 rows: two parts); sums are fp32; out is
+ * rounded once.  Where a sequence has many rows, values of a page may count as 0 whose scale is 2^80 times smaller than that of another of its pages.  A row whose q has an infinity or NaN, or
+ * whose products go beyond fp32, has no finite result and leaves the others alone.  out may not overlap q. */
 typedef struct bild_cache_attend_call {
     const void* q;            /* head h of row t at q + t * q_token + h * q_head                  */
     void* out;
@@ -534,7 +535,8 @@ int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* call, void* h
 /* ---- beams ----
  * The best continuations of each of `batch` groups of `beams` rows.  A beam that has not ended goes on with any id v: its sum is scores + logit - lse of its row (lse in fp32, sums in 64 bits from there),
  * its length one more.  One that has ended goes on with `pad` alone, sum and length unchanged.  The `choices` best by sum / max(length, 1)^penalty come out in that order, of equals the lower beam and id first.  Beams
- * whose score is -infinity or NaN, rows without finite lse and ids of logit -infinity offer nothing; choices that nobody offers: parent and token -1, score -infinity, length 0, ended. */
+ * whose score is -infinity or NaN, rows without finite lse and ids of logit -infinity offer nothing; choices that nobody offers: parent and token -1, score -infinity, length 0, ended.
+ * Nothing that is written may overlap what is read. */
 typedef struct bild_beams_call {
     const void* logits;        /* [batch * beams][vocab]                                          */
     int64_t logits_stride;

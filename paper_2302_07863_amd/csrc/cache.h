@@ -45,7 +45,8 @@ struct CacheRows {
     }
 };
 
-constexpr int kMaxLimit = 16777216;  // of lists and pools: 2^24
+constexpr int kMaxLimit = 16777216;       // of lists and pools: 2^24
+constexpr int kMaxGroups = kMaxLimit - 1;  // workgroups in a direction: their threads are counted in 32 bits
 
 }  // namespace bild
 
@@ -62,13 +63,11 @@ struct bild_cache {
 
 namespace bild {
 
-#ifndef GROUPS
-#define GROUPS 256
-#endif
-constexpr int kAttendGroups = GROUPS;                       // workgroups of a launch, but for one a key head
+constexpr int kAttendGroups = 256;                       // workgroups of a launch, but for one a key head
 inline int attend_groups(int heads) { return (kAttendGroups + heads - 1) / heads; }  // of a key head
 hipError_t attend_init(int d_head);                      // what its kernels need of the current device
 size_t attend_part_floats(int heads, int d_head);        // of bild_cache::part
-inline size_t attend_counts(int heads) { return std::max((size_t)heads * attend_groups(heads), (size_t)512); }
+constexpr int kPromptParts = 512;                        // most workgroups of a launch that shares the keys of tiles of prompts: two a compute unit
+inline size_t attend_counts(int heads) { return std::max((size_t)heads * attend_groups(heads), (size_t)kPromptParts); }
 
 }  // namespace bild

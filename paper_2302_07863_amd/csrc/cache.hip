@@ -20,7 +20,8 @@ using namespace bild;
 namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr float kLimit = 1.329227995784916e36f;  // 2^120: 127 times it is below fp32's largest
+// 2^90: sums over 2^30 values in fp32, times weights of up to 2^8 and the scales of codes (2^2) and weights, stay below its largest
+constexpr float kLimit = 1.2379400392853803e27f;
 
 // Words of a handle that kernels hand on.
 enum : int { W_FITS = 0, W_COPIES, W_USED, W_MOVES, W_COUNT = 16 };
@@ -691,7 +692,7 @@ extern "C" int bild_cache_append(bild_cache* c, const bild_cache_append_call* ca
     if (!k.k || !k.v || k.reserved != 0 || !row_type(k.dtype) || k.layer < 0 || k.layer >= c->view.layers) return BILD_EINVAL;
     if (k.n < 1 || k.n > c->view.sequences || k.rows < 1 || (k.starts && k.tokens < 1)) return BILD_EINVAL;
     const int64_t slots = k.starts ? (k.tokens >> c->view.page_shift) + 2 * (int64_t)k.n : k.n * ((((int64_t)k.rows + c->view.page_tokens - 2) >> c->view.page_shift) + 1);
-    if ((!k.starts && (int64_t)k.n * k.rows > 0x7FFFFFFF) || slots > 0x7FFFFFFF) return BILD_EINVAL;
+    if ((!k.starts && (int64_t)k.n * k.rows > 0x7FFFFFFF) || slots > kMaxGroups) return BILD_EINVAL;
     const AppendArgs a = {c->view, {k.sequences, k.starts, k.n, k.rows, k.starts ? k.tokens : k.n * k.rows}, {k.k, k.v}, {k.k_token, k.v_token}, {k.k_head, k.v_head}, k.layer, c->words};
     const OnDevice on(c->device);
     if (!on.ok) return BILD_EHIP;

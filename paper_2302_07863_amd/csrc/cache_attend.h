@@ -10,7 +10,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-
 constexpr int kBlock = 32;     // keys of a step of the matrix cores' second product: a page has whole ones
 constexpr float kLn2 = 0.6931471805599453f;
 // Weights are powers of two relative to a maximum that is moved only when a score is beyond it by this much: they stay below 2^8, far from fp16's end.
@@ -51,7 +50,6 @@ __device__ __forceinline__ f16x8 eight_of(uint32_t a, uint32_t b) {
 // byte k of two words
 __device__ __forceinline__ f16x2 pair_of(uint32_t a, uint32_t b, int k) { return two(__builtin_amdgcn_perm(b, a, 0x0c000c00u | (unsigned)(4 + k) << 16 | (unsigned)k)); }
 
-
 // Rows of q as fp16 times a power of two that puts the largest magnitude below 2^15 (0, infinities and NaN: 1).
 __device__ __forceinline__ int up_of(float big) {
     int up = 0;
@@ -63,16 +61,13 @@ __device__ __forceinline__ int up_of(float big) {
 }
 
 constexpr int kTile = 16;      // rows of a tile of the kernels for few rows
-#ifndef START
-#define START 16
-#endif
-constexpr int kStart = START;
+constexpr int kStart = 16;     // blocks that could be read while a workgroup gets to a tile and joins what its waves have of it
 
 // A sequence's share of the work.
 struct Seq {
     int s, first, count, length;  // which, its rows, its positions
     int tiles, sink_blocks, low_block, blocks;
-    // what a tile counts for in the line: its blocks, and as many as would be read while a workgroup gets there and joins what its waves have
+    // what a tile counts for in the line
     __device__ int cost() const { return blocks + kStart; }
 };
 __device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
@@ -100,6 +95,5 @@ hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hi
 hipError_t cache_prompt_init(int d_head);
 size_t prompt_part_floats(int d_head);
 constexpr int kPromptRows = 128;   // of a tile of the kernel for prompts
-constexpr int kPromptParts = 512;  // most workgroups of a launch that shares tiles' keys: two a compute unit
 
 }  // namespace bild

@@ -9,7 +9,8 @@
 // scores and to partial sums in fp32.
 //
 // Work is cut where it is: the 32-token blocks of all sequences and row tiles lie in one line, of which each workgroup of a key head takes an equal piece, wherever sequences begin or
-// end (the lengths are in device memory, and a batch's are far apart); a workgroup's four waves take turns over its blocks.  What several workgroups have of a tile the last of them joins, in order.
+// end (the lengths are in device memory, and a batch's are far apart); a workgroup's eight waves take turns over its blocks, or over tiles that are short.  What several workgroups have
+// of a tile the last of them joins, in order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -62,15 +63,11 @@ struct Codes {
     uint32_t v[8][WV];  // eight values, NJ codes of each
 };
 
+// N (2 or 4) floats of a row of partial results.
 template <int N>
 __device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t mem, int off, const float (&o)[N]) {
-    if constexpr (N == 2) {
-        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(o[0]), __float_as_uint(o[1])}, mem, off, 0, kPartAux);
-    } else {
-#pragma unroll
-        for (int t = 0; t < N; t += 4)
-            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[t]), __float_as_uint(o[t + 1]), __float_as_uint(o[t + 2]), __float_as_uint(o[t + 3])}, mem, off + 4 * t, 0, kPartAux);
-    }
+    if constexpr (N == 2) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(o[0]), __float_as_uint(o[1])}, mem, off, 0, kPartAux);
+    else __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3])}, mem, off, 0, kPartAux);
 }
 template <int N>
 __device__ __forceinline__ void get_part(__amdgpu_buffer_rsrc_t mem, int off, float (&o)[N]) {
@@ -79,12 +76,9 @@ __device__ __forceinline__ void get_part(__amdgpu_buffer_rsrc_t mem, int off, fl
         o[0] = __uint_as_float(y[0]);
         o[1] = __uint_as_float(y[1]);
     } else {
+        const auto y = __builtin_amdgcn_raw_buffer_load_b128(mem, off, 0, kPartAux);
 #pragma unroll
-        for (int t = 0; t < N; t += 4) {
-            const auto y = __builtin_amdgcn_raw_buffer_load_b128(mem, off + 4 * t, 0, kPartAux);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) o[t + u] = __uint_as_float(y[u]);
-        }
+        for (int u = 0; u < 4; ++u) o[u] = __uint_as_float(y[u]);
     }
 }
 
@@ -250,14 +244,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
                 const int off = (8 * g + t) * d + min(n16 * NJ, d - NJ);
                 if constexpr (WV == 1) {
                     x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, base, kAux);
-                } else if constexpr (WV == 2) {
+                } else {
                     const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, base, kAux);
                     x.v[t][0] = (uint32_t)y[0];
                     x.v[t][1] = (uint32_t)y[1];
-                } else {
-                    const auto y = __builtin_amdgcn_raw_buffer_load_b128(v, off, base, kAux);
-#pragma unroll
-                    for (int w4 = 0; w4 < 4; ++w4) x.v[t][w4] = (uint32_t)y[w4];
                 }
             }
         };
@@ -454,20 +444,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
             const int cut = max(col / NJ * NJ + NJ - d, 0), dim = col - cut;
             if (col / NJ * NJ < d) {
                 V* out = (V*)a.out + t_at * a.out_token + (int64_t)h * a.out_head + dim;
-                if constexpr (NC >= 4) {
+                RowVec<R, NC> y;
 #pragma unroll
-                    for (int t = 0; t < NC; t += 4) {
-                        RowVec<R, 4> y;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) y.v[u] = R::down(o[t + u] * by);
-                        y.store(out + t);
-                    }
-                } else {
-                    RowVec<R, 2> y;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) y.v[u] = R::down(o[u] * by);
-                    y.store(out);
-                }
+                for (int u = 0; u < NC; ++u) y.v[u] = R::down(o[u] * by);
+                y.store(out);
             }
             if (a.lse && col == 0) a.lse[t_at * a.heads + h] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
         };
@@ -529,6 +509,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 // sequences.  (us, this kernel / that one: 16 rows of 4 heads over 2000 positions, 32 sequences of 8 key heads 95 / 69, 64 rows over 8000, 32 key heads 50 / 53, 20 of 4 over 4000, 8 key heads 23 / 33;
 // 60 of 4 over 2000, 8 sequences 86 / 46; 8 of 4 over 2000, 32 sequences 55 / 70.)
 constexpr int kPromptFrom = 64, kPromptWork = 4096, kMaxSplits = 16;
+constexpr int kLeast = 20;  // of the line that a workgroup takes
 
 constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
 
@@ -588,15 +569,13 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     a.causal = k.causal;
     a.scale = (float)((double)k.scale * 1.4426950408889634 * 512.0 / 127.0);
     a.groups = attend_groups(v.heads);
-#ifndef LEAST
-#define LEAST 20
-#endif
-    a.least = LEAST;
+    a.least = kLeast;
     const int64_t tiles = k.starts ? tokens * a.group / kPromptRows + k.n : k.n * (((int64_t)k.rows * a.group + kPromptRows - 1) / kPromptRows);
-    const bool prompts = (int64_t)k.rows * a.group >= kPromptRows || ((int64_t)k.rows * a.group >= kPromptFrom && tokens * k.heads >= kPromptWork);
-    a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;
     // (fewer tiles than the chip has room for: several workgroups share a tile's keys)
     a.splits = (int)std::min(std::max(kPromptParts / (tiles * v.heads), (int64_t)1), (int64_t)kMaxSplits);
+    const int64_t per_head = (int64_t)k.rows * a.group;
+    const bool prompts = (per_head >= kPromptRows || (per_head >= kPromptFrom && tokens * k.heads >= kPromptWork)) && tiles * v.heads * a.splits <= kMaxGroups;
+    a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;
     a.part = c->part;
     a.arrived = c->arrived;
     const OnDevice on(c->device);

@@ -16,23 +16,11 @@ using namespace bild;
 
 namespace {
 
-#ifndef AHEAD
-#define AHEAD 4
-#endif
-#if AHEAD
-#define SCHED_S { __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0); _Pragma("unroll") for (int i_ = 0; i_ < 2 * QS - AHEAD; ++i_) { __builtin_amdgcn_sched_group_barrier(0x8, TERMS, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); } __builtin_amdgcn_sched_group_barrier(0x8, AHEAD * TERMS, 0); }
-#define SCHED_V { }
-#else
-#define SCHED_S
-#define SCHED_V
-#endif
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256, kKeys = 64;
-#ifndef SPL
-#define SPL 4
-#endif
-constexpr int kSplitLeast = SPL;  // tiles of keys that a workgroup has at least
+constexpr int kAhead = 4;  // operands of the scores' products that are asked for before the first of them
+constexpr int kSplitLeast = 4;  // tiles of keys that a workgroup has at least
 
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float max_xor32(float v) {
@@ -244,7 +232,14 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
 #pragma unroll
                     for (int w = 0; w < TERMS; ++w) z[m] = mma(k, q[w][u], z[m]);
                 }
-            SCHED_S
+            // (the next products' operands come from LDS while these run)
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+            for (int u = 0; u < 2 * QS - kAhead; ++u) {
+                __builtin_amdgcn_sched_group_barrier(0x8, TERMS, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, kAhead * TERMS, 0);
             // (what scores are multiplied by is not 0, so that hidden ones stay -infinity: where it would be, the scores are 0)
             const float by[2] = {fmaxf(ks[0] * row_scale, 1.17549435e-38f), fmaxf(ks[PAGES - 1] * row_scale, 1.17549435e-38f)};
             const bool full = key0 + kKeys - 1 <= first_pos && (!a.window || key0 > last_pos - a.window || key0 + kKeys <= a.sinks) && there[0] && there[PAGES - 1];
@@ -289,7 +284,8 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
                         for (int r = 0; r < 16; ++r) acc[u][r] *= less;
                     unit = now;
                 }
-                const float part = v > 0.f ? v / unit : 1.f, off = __builtin_amdgcn_logf(part) - base;
+                // (not below 2^-60: there its values count for nothing in fp16, but the sum of the weights is taken from the same numbers)
+                const float part = v > 0.f ? fmaxf(v / unit, 8.67361738e-19f) : 8.67361738e-19f, off = __builtin_amdgcn_logf(part) - base;
                 constexpr int ST = 4 / PAGES;
                 f16x8 w[TERMS][ST];
                 float sums[2] = {0.f, 0.f};
@@ -313,7 +309,6 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
 #pragma unroll
                         for (int x = 0; x < TERMS; ++x) acc[u] = mma(y, w[x][st], acc[u]);
                     }
-                SCHED_V
             }
         }
         __builtin_amdgcn_sched_barrier(0);

@@ -8,7 +8,7 @@ import paper_2302_07863_amd as pkg
 from tests.hipmem import DeviceArray
 from tests.rows import BF16, F16, F32, HALF_STEP, U32, unpack
 
-LIMIT = np.float32(2.0 ** 120)
+LIMIT = np.float32(2.0 ** 90)
 GUARD = 256                                            # words before and behind an array that nobody may touch
 
 

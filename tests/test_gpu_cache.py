@@ -7,7 +7,7 @@ import pytest
 import paper_2302_07863_amd as pkg
 from paper_2302_07863_amd import binding as b
 from tests.cached import Held, Oracle, invariants, values
-from tests.hipmem import DeviceArray
+from tests.hipmem import H2D, DeviceArray, hip
 from tests.rows import BF16, F16, F32, Graph, Rows, Stream, close, pack, unpack
 
 pytestmark = pytest.mark.gpu
@@ -464,3 +464,120 @@ def test_calls_that_are_refused():
     bad = b.CacheAppendCall(k=p, v=p, n=1, rows=1, reserved=1)
     assert pkg.lib().bild_cache_append(c.h, C.byref(bad), None) == b.EINVAL
     t.same()
+
+
+# ------------------------------------------------------------------------------------------------ what rows and pages may be like
+@pytest.mark.parametrize("page", [32, 64])
+@pytest.mark.parametrize("by", [3, 20, 60])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_pages_whose_scales_are_far_apart(page, by, dtype):
+    """Each page of the values has a scale of its own, up to 2^(2 by) apart, some 0: for few rows and for prompts."""
+    t, rng = filled(page + by, [333], pages=12, page=page, heads=4, d=64, max_pages=12)
+    n = len(t.o.scales)
+    t.o.scales[:, 0, 1] *= np.exp2(rng.integers(-by, by + 1, (n, 4))).astype(np.float32)
+    t.o.scales[1, 0, 1], t.o.scales[3, 0, 0] = 0, 0
+    t = Held(t.o)
+    attend(t, rng, 0, [3], 2, dtype)
+    attend(t, rng, 0, [300], 8, dtype, causal=False)
+    attend(t, rng, 0, [333], 4, dtype, window=100 if by < 60 else 0, sinks=7)
+
+
+@pytest.mark.parametrize("page", [32, 64])
+@pytest.mark.parametrize("tall,low", [(80, -100), (89, -120)])
+def test_scales_at_both_ends(page, tall, low):
+    """A page of next to nothing counts in the sum of the weights like any other."""
+    t, rng = filled(page, [200], pages=7, page=page, heads=4, d=64, max_pages=12)
+    for order in (0, 1):
+        t.o.scales[:, 0, 1] = np.exp2(float(low))
+        t.o.scales[order::2, 0, 1] = np.exp2(float(tall))
+        t = Held(t.o)
+        attend(t, rng, 0, [2], 2, BF16, causal=False)
+        attend(t, rng, 0, [200], 8, BF16, causal=False)
+
+
+def test_infinities_in_the_values():
+    """They are limited, so that sums over many of them end as finite as they are."""
+    t, rng = cache(40, pages=40, page=64, heads=4, d=64, sequences=2, max_pages=30)
+    extend(t, [1500, 300])
+
+    def spoil(words, x):
+        x[1, ::2, 1] = np.inf
+        x[1, ::3, 2, ::2] = -np.inf
+        x[1, :, 3] = 3e38
+        words[...] = x
+
+    append(t, rng, 0, [1500, 300], spoil=spoil)
+    t.same()
+    assert np.max(t.o.scales) == np.float32(2.0 ** 90)
+    attend(t, rng, 0, [1, 2], 2, F32, size=3.0)
+    out, _ = attend(t, rng, 0, [400, 300], 4, BF16, size=3.0)
+    assert np.all(np.isfinite(out)) and np.max(np.abs(out)) > 2.0 ** 85
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 3, 70])
+def test_rows_with_strides(dtype, rows):
+    """Heads and tokens apart, heads before tokens: keys, values, rows and results in views of larger arrays."""
+    t, rng = cache(50 + rows, pages=20, page=32, heads=3, d=40, sequences=2, max_pages=8)
+    o, tokens, group = t.o, 2 * rows, 2
+    for _ in range(2):
+        extend(t, [rows, rows], uniform=True)
+        words, x = values(rng, (2, 3, tokens, 43), dtype)       # [k or v][head][token][d and some]
+        mem = DeviceArray(words)
+        size, off = words.itemsize, 2
+        k, v = mem.ptr.value + off * size, mem.ptr.value + (3 * tokens * 43 + off) * size
+        t.cache.append(0, dtype, 2, rows, k, v, k_token=43, k_head=43 * tokens, v_token=43, v_head=43 * tokens)
+        rows_of = x[..., off:off + 40].transpose(0, 2, 1, 3)
+        o.append(0, rows_of[0], rows_of[1], [rows, rows])
+        t.same()
+    words, x = values(rng, (6, tokens, 45), dtype)
+    before = pack(np.full((tokens, 7, 51), 9, np.float32), dtype)
+    q, out = DeviceArray(words), DeviceArray(before)
+    t.cache.attend(0, dtype, 2, rows, 6, q.ptr.value + 3 * words.itemsize, out.ptr.value + 5 * words.itemsize, 0.2, q_token=45, q_head=45 * tokens, out_token=7 * 51, out_head=51)
+    want, _, tol, _ = o.attend(0, x[..., 3:43].transpose(1, 0, 2).astype(np.float64), [rows, rows], float(np.float32(0.2)), dtype=dtype)
+    got = unpack(out.to_host(before.dtype, before.size), dtype).reshape(before.shape)
+    close(got[:, :6, 5:45], want, tol)
+    got[:, :6, 5:45] = 9
+    assert np.all(got == 9)                                     # nothing else is written
+
+
+def test_pools_beyond_32_bits():
+    """Pages of 64 MiB, the last of them behind 4 GiB: written, copied, read and moved."""
+    layers, heads, d, page, pages = 64, 64, 128, 64, 70
+    size = layers * 2 * heads * page * d
+    assert size * pages > 1 << 32
+    codes = DeviceArray(nbytes=size * pages)
+    scales = DeviceArray(np.zeros(pages * layers * 2 * heads, np.float32))
+    table, lengths, refs = ints(np.full((3, 2), -1)), ints([0, 0, 0]), np.ones(pages, np.int32)
+    refs[[66, 67, 69]] = 0                                      # (the others are somebody's)
+    held = ints(refs)
+    c = pkg.Cache(pages, page, layers, heads, d, 3, 2, codes=codes.ptr.value, scales=scales.ptr.value, table=table.ptr.value, lengths=lengths.ptr.value, refs=held.ptr.value)
+    rng = np.random.default_rng(5)
+    o = Oracle(3, page, 1, heads, d, 3, 2)                      # pages 0, 1, 2 for 66, 67, 69; one layer, the last
+    for rows, ids in ((40, [0]), (3, [0, 1])):
+        if len(ids) == 2:
+            parents = ints([0, 0, 2])
+            o.fork([0, 0, 2])
+            c.fork(3, parents.ptr.value)
+        words, x = values(rng, (2, rows * len(ids), heads, d), BF16)
+        k, v = DeviceArray(words[0]), DeviceArray(words[1])
+        o.extend([rows] * len(ids), ids)
+        o.append(0, x[0], x[1], [rows] * len(ids), ids)
+        c.extend(len(ids), rows)
+        c.append(layers - 1, BF16, len(ids), rows, k.ptr.value, v.ptr.value)
+        names = np.array([66, 67, 69, -1])
+        assert np.array_equal(table.to_host(np.int32, 6).reshape(3, 2), names[o.table])
+    words, x = values(rng, (2, 2 * heads, d), BF16)
+    q, out = DeviceArray(words), DeviceArray(nbytes=words.nbytes)
+    want, _, tol, _ = o.attend(0, x.astype(np.float64), [1, 1], float(np.float32(0.1)), dtype=BF16)
+    for turn in range(2):
+        c.attend(layers - 1, BF16, 2, 1, 2 * heads, q.ptr.value, out.ptr.value, 0.1)
+        close(unpack(out.to_host(np.uint16, words.size), BF16).reshape(want.shape), want, tol)
+        if turn == 0:
+            freed = np.array(held.to_host(np.int32, pages))
+            freed[[3, 68]] = 0                                  # two in front go: the highest moves into the first
+            assert hip().hipMemcpy(held.ptr, np.ascontiguousarray(freed, np.int32).ctypes.data, 4 * pages, H2D) == 0
+            used = ints([0])
+            c.compact(used=used.ptr.value)
+            assert used.to_host(np.int32, 1)[0] == np.sum(freed > 0)
+            assert np.all(table.to_host(np.int32, 6) < used.to_host(np.int32, 1)[0])
