@@ -18,7 +18,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256, kKeys = 64;
+constexpr int kThreads = 256, kKeys = 64, kUnits = 256;
 constexpr int kAhead = 4;  // operands of the scores' products that are asked for before the first of them
 constexpr int kSplitLeast = 4;  // tiles of keys that a workgroup has at least
 
@@ -33,7 +33,8 @@ __device__ __forceinline__ float max_xor32(float v) {
 template <class R, int DP, int PAGES>
 __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1 : 2) void cache_prompt_kernel(const AttendArgs a) {
     constexpr bool TWO = R::kDtype == BILD_DT_F32;
-    constexpr int TERMS = TWO ? 2 : 1, QS = DP / 16, ND = DP / 32, KC = DP / 64, VI = (DP + 127) / 128, ROWC = DP / 8;
+    constexpr int TERMS = TWO ? 2 : 1, QS = DP / 16, ND = DP / 32, KC = DP / 64, VI = (DP + 127) / 128;
+    constexpr bool SOME = VI * kThreads > 2 * DP;  // of the threads have values on their way
     constexpr int kBuffer = 2 * kKeys * DP;  // fp16 values of a tile's keys and values
     typedef typename R::type V;
     extern __shared__ __attribute__((aligned(16))) _Float16 lds[];  // two buffers: keys [64][DP], values [DP][64]
@@ -41,7 +42,10 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n32 = lane & 31, half = lane >> 5, d = c.d_head;
     __shared__ unsigned share;
     const int head = blockIdx.x % c.heads;  // (dies take workgroups in turn: those of a head have its keys in few L2s)
-    const int place_at = (int)((gridDim.x - 1 - blockIdx.x) / c.heads), split = place_at % a.splits;  // (the last rows, which see most, come first)
+    // The last rows, which see most, come first; those that come second to the compute units the other way round, so that who has much to do shares its unit with who has little
+    // (us, call: 200 rows of 4 heads behind 4000 positions, 8 key heads 52 / 47, 2000 rows behind 3001 198 / 196).
+    const int places = (int)(gridDim.x / c.heads), round = max(kUnits / c.heads, 1), nth = (int)(blockIdx.x / c.heads);
+    const int place_at = places - 1 - (nth >= round && nth < 2 * round ? round + min(places, 2 * round) - 1 - nth : nth), split = place_at % a.splits;
     // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles
     int i, first, count, tile;
     {
@@ -86,6 +90,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
 
     // ---- pages and scales of the next 64 tiles, a lane a tile
     int pages[PAGES];
+    uint32_t where[PAGES][2];  // of the keys' codes
     float k_scale[PAGES], v_scale[PAGES];
     const auto look_up = [&](int t0) {
         const int t = t0 + lane, key0 = tile_at(t) * kKeys;
@@ -96,6 +101,10 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             k_scale[p] = v_scale[p] = 0.f;
             if (t < tiles && k0 < length) pages[p] = c.table[(int64_t)s * c.max_pages + (k0 >> c.page_shift)];
             if (!c.has(pages[p])) pages[p] = -1;
+            // (a page that is not there: any that is in the pool, and no weight)
+            const uint64_t at = (uint64_t)(c.codes + c.plane(max(pages[p], 0), a.layer, 0, head) * c.plane_bytes() + (k0 & (c.page_tokens - 1)) * d);
+            where[p][0] = (uint32_t)at;
+            where[p][1] = (uint32_t)(at >> 32);
             if (pages[p] >= 0) {
                 k_scale[p] = c.scales[c.plane(pages[p], a.layer, 0, head)];
                 v_scale[p] = c.scales[c.plane(pages[p], a.layer, 1, head)] * (512.f / 127.f);
@@ -145,24 +154,24 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4), k0 = 16 * (group >> 1) + 4 * (group & 1);
         v_off[u] = (PAGES == 2 ? k0 & (kBlock - 1) : k0) * d + min(4 * dg, d - 4);
     }
-    const auto request = [&](int t) {  // (looked up; a page that is not there: any that is in the pool, and no weight)
-        const int base = PAGES == 2 ? 0 : (tile_at(t) * kKeys & (c.page_tokens - 1)) * d;
+    const int64_t to_v = (int64_t)c.heads * c.plane_bytes();
+    const auto request = [&](int t) {  // (looked up)
         const auto plane = [&](int which, int half_of) {
-            const int page = max(__builtin_amdgcn_readlane(pages[half_of], (t - t0) & 63), 0);
-            return make_rsrc(c.codes + c.plane(page, a.layer, which, head) * c.plane_bytes(), (size_t)c.plane_bytes());
+            const uint64_t lo = (uint32_t)__builtin_amdgcn_readlane((int)where[half_of][0], (t - t0) & 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)where[half_of][1], (t - t0) & 63);
+            return make_rsrc((const int8_t*)(hi << 32 | lo) + (which ? to_v : 0), (size_t)(kKeys / PAGES * d));
         };
 #pragma unroll
         for (int u = 0; u < KC; ++u) {
             const int first_key = (u * kThreads + wave * 64) / (DP / 16);
-            kc[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(plane(0, PAGES == 2 && first_key >= kBlock ? PAGES - 1 : 0), k_off[u], base, 0));
+            kc[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(plane(0, PAGES == 2 && first_key >= kBlock ? PAGES - 1 : 0), k_off[u], 0, 0));
         }
 #pragma unroll
         for (int u = 0; u < VI; ++u) {
             const int first_group = (u * kThreads + wave * 64) / (DP / 4);
-            if (first_group >= 8) continue;
+            if (SOME && first_group >= 8) continue;
             const auto from = plane(1, PAGES == 2 && first_group >= 4 ? PAGES - 1 : 0);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) vc[u][y] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(from, v_off[u], base + ((y & 3) + 8 * (y >> 2)) * d, 0);
+            for (int y = 0; y < 8; ++y) vc[u][y] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(from, v_off[u], ((y & 3) + 8 * (y >> 2)) * d, 0);
         }
     };
     const auto k_at = [&](int key, int ch) { return key * DP + 8 * (ch ^ (DP == 64 ? (key >> 1) & 7 : key & 15)); };
@@ -180,7 +189,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
 #pragma unroll
         for (int u = 0; u < VI; ++u) {
             const int item = u * kThreads + tid, group = item / (DP / 4), dg = item % (DP / 4);
-            if (group >= 8) continue;
+            if (SOME && group >= 8) continue;
             uint32_t y[8];
 #pragma unroll
             for (int z = 0; z < 8; ++z) y[z] = vc[u][z] ^ 0x80808080u;
@@ -190,7 +199,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         }
     };
 
-    float top = -INFINITY, sum = 0.f, unit = 0.f, most_v = 0.f;  // (the sums over the values are in `unit`s)
+    float top = -INFINITY, sum = 0.f, unit = 0.f, per_unit = 0.f, most_v = 0.f;  // (the sums over the values are in `unit`s)
     f32x16 acc[ND];
 #pragma unroll
     for (int t = 0; t < ND; ++t)
@@ -219,38 +228,61 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         const _Float16* at = lds + (t & 1) * kBuffer;
         const bool seen = key0 <= last_pos && (!a.window || key0 + kKeys - 1 > first_pos - a.window || key0 < a.sinks) && (there[0] || there[PAGES - 1]);
         if (seen) {
-            f32x16 z[2];
+            float part, part_log;
+            const auto scale_of = [&](int p) {
+                // a page's scale goes into its weights, relative to a power of two that the sums are kept in units of
+                const float v = vs[p];
+                if (__builtin_amdgcn_readfirstlane(v > unit || (v > 0.f && v < unit * 0.0625f))) {
+                    most_v = fmaxf(most_v, v);
+                    const float now = fmaxf(__uint_as_float((__float_as_uint(v) + 0x7FFFFFu) & 0x7F800000u), most_v * 8.27180613e-25f), less = unit / now;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                    for (int u = 0; u < ND; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[m][r] = 0.f;
-#pragma unroll
-            for (int u = 0; u < QS; ++u)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const f16x8 k = *(const f16x8*)(at + k_at(32 * m + n32, 2 * u + half));
-#pragma unroll
-                    for (int w = 0; w < TERMS; ++w) z[m] = mma(k, q[w][u], z[m]);
+                        for (int r = 0; r < 16; ++r) acc[u][r] *= less;
+                    unit = now;
+                    per_unit = 1.f / now;
                 }
-            // (the next products' operands come from LDS while these run)
-            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
-#pragma unroll
-            for (int u = 0; u < 2 * QS - kAhead; ++u) {
-                __builtin_amdgcn_sched_group_barrier(0x8, TERMS, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x8, kAhead * TERMS, 0);
+                // (not below 2^-60: there its values count for nothing in fp16, but the sum of the weights is taken from the same numbers)
+                part = fmaxf(v * per_unit, 8.67361738e-19f);
+                part_log = __builtin_amdgcn_logf(part);
+            };
+            scale_of(0);
             // (what scores are multiplied by is not 0, so that hidden ones stay -infinity: where it would be, the scores are 0)
             const float by[2] = {fmaxf(ks[0] * row_scale, 1.17549435e-38f), fmaxf(ks[PAGES - 1] * row_scale, 1.17549435e-38f)};
             const bool full = key0 + kKeys - 1 <= first_pos && (!a.window || key0 > last_pos - a.window || key0 + kKeys <= a.sinks) && there[0] && there[PAGES - 1];
-            if (!full) {
+            // scores begin as -infinity where the row does not see the key
+            f32x16 z[2];
+            const auto scores = [&] {
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int u = 0; u < QS; ++u)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const f16x8 k = *(const f16x8*)(at + k_at(32 * m + n32, 2 * u + half));
+#pragma unroll
+                        for (int w = 0; w < TERMS; ++w) z[m] = mma(k, q[w][u], z[m]);
+                    }
+                // (the next products' operands come from LDS while these run)
+                __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+                for (int u = 0; u < 2 * QS - kAhead; ++u) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, TERMS, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x8, kAhead * TERMS, 0);
+            };
+            if (full) {
+                z[0] = z[1] = f32x16{};
+                scores();
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = key0 + 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
-                        z[m][r] = key <= pos && (key > low || key < a.sinks) && there[m * (PAGES - 1)] ? z[m][r] : -INFINITY;
+                        z[m][r] = (key <= pos) & ((key > low) | (key < a.sinks)) & there[m * (PAGES - 1)] ? 0.f : -INFINITY;
                     }
+                }
+                scores();
             }
             float big = -INFINITY;
 #pragma unroll
@@ -273,19 +305,8 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int p = 0; p < PAGES; ++p) {
-                // a page's scale goes into its weights, relative to a power of two that the sums are kept in units of
-                const float v = vs[p];
-                if (__builtin_amdgcn_readfirstlane(v > unit || (v > 0.f && v < unit * 0.0625f))) {
-                    most_v = fmaxf(most_v, v);
-                    const float now = fmaxf(__uint_as_float((__float_as_uint(v) + 0x7FFFFFu) & 0x7F800000u), most_v * 8.27180613e-25f), less = unit / now;
-#pragma unroll
-                    for (int u = 0; u < ND; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[u][r] *= less;
-                    unit = now;
-                }
-                // (not below 2^-60: there its values count for nothing in fp16, but the sum of the weights is taken from the same numbers)
-                const float part = v > 0.f ? fmaxf(v / unit, 8.67361738e-19f) : 8.67361738e-19f, off = __builtin_amdgcn_logf(part) - base;
+                if (p) scale_of(p);
+                const float off = part_log - base;
                 constexpr int ST = 4 / PAGES;
                 f16x8 w[TERMS][ST];
                 float sums[2] = {0.f, 0.f};
@@ -300,7 +321,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
                         if (TWO) w[TERMS - 1][st][u] = (_Float16)(e - (float)w[0][st][u]);
                     }
                 }
-                sum = __builtin_fmaf(sums[0] + sums[1], 1.f / part, sum);
+                sum = __builtin_fmaf(sums[0] + sums[1], __builtin_amdgcn_rcpf(part), sum);
 #pragma unroll
                 for (int st = 0; st < ST; ++st)
 #pragma unroll
