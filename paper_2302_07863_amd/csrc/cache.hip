@@ -477,9 +477,10 @@ struct AppendArgs {
 __device__ __forceinline__ float bounded(float x) { return __builtin_amdgcn_fmed3f(x != x ? 0.f : x, -kLimit, kLimit); }
 
 // A workgroup has the new positions of one page, of keys or values of a head: their largest magnitude, then their codes.
-template <class R, int THREADS>
+// KEPT: pieces of eight values that a thread keeps from the first pass for the second.
+template <class R, int THREADS, int KEPT>
 __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs a) {
-    constexpr int E = 8, KEPT = 4;  // values of a piece; pieces a thread keeps from the first pass for the second
+    constexpr int E = 8;
     typedef typename R::type V;
     __shared__ float tops[THREADS / 64];
     const CacheView& c = a.c;
@@ -529,14 +530,25 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
         return x + (int64_t)row * a.token[which] + (u - row * per_row) * E;
     };
     float top = 0.f;
+    {
+        int row = tid / per_row, piece = tid - row * per_row;
+        const int rows_on = THREADS / per_row, pieces_on = THREADS - rows_on * per_row;
 #pragma unroll
-    for (int k = 0; k < KEPT; ++k)
-        if (k * THREADS + tid < pieces) {
-            if (!one) kept[k].load(at(k * THREADS + tid));
-        } else {
+        for (int k = 0; k < KEPT; ++k) {
+            if (k * THREADS + tid < pieces) {
+                if (!one) kept[k].load(x + (int64_t)row * a.token[which] + piece * E);
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) kept[k].v[e] = 0;
+                for (int e = 0; e < E; ++e) kept[k].v[e] = 0;
+            }
+            row += rows_on;
+            piece += pieces_on;
+            if (piece >= per_row) {
+                piece -= per_row;
+                ++row;
+            }
         }
+    }
     const auto largest = [&](const RowVec<R, E>& q) {
 #pragma unroll
         for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(bounded(R::up(q.v[e]))));
@@ -568,10 +580,21 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
             *(uint2*)(codes + 8 * u) = q;
         }
     }
+    // A product with 1 / scale is within 3 * 2^-24 of the quotient, so within 2^-15 of it: where that leaves no doubt about the nearest whole number, it is enough.
+    const float per_scale = 1.f / scale;
     const auto put = [&](const RowVec<R, E>& q, int u) {
         int8_t v[8];
+        bool sure = true;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = scale > 0.f ? (int8_t)rintf(bounded(R::up(q.v[e])) * 127.f / scale) : (int8_t)0;
+        for (int e = 0; e < E; ++e) {
+            const float y = bounded(R::up(q.v[e])) * 127.f * per_scale, whole = rintf(y);
+            sure &= fabsf(y - whole) < 0.5f - 3.0517578125e-5f;  // (not if it is NaN: a scale of 0, or whose reciprocal is beyond fp32)
+            v[e] = (int8_t)whole;
+        }
+        if (__any(!sure)) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = scale > 0.f ? (int8_t)rintf(bounded(R::up(q.v[e])) * 127.f / scale) : (int8_t)0;
+        }
         uint2 w;
         __builtin_memcpy(&w, v, 8);
         *(uint2*)(codes + (int64_t)before * d + 8 * u) = w;
@@ -587,9 +610,14 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
     if (tid == 0) c.scales[plane] = scale;
 }
 
+// A page's threads: as many as keep its pieces, four each (us, a call: 4001 rows of 16 heads of 80, pages of 32, 128 / 256 threads 12.9 / 14.6; 2000 of 8 heads of 128, pages of 64 12.5 / 8.2;
+// 4000 of the same in fp32, pages of 128, 256 threads with four / eight 13.2 / 12.0).  few: rows of a decoding step.
 template <class R>
 hipError_t launch_append(const AppendArgs& a, dim3 grid, bool few, hipStream_t st) {
-    return few ? launch_on(cache_append_kernel<R, 64>, grid, dim3(64), 0, st, a) : launch_on(cache_append_kernel<R, 256>, grid, dim3(256), 0, st, a);
+    const int pieces = a.c.plane_bytes() / 8;
+    if (few) return launch_on(cache_append_kernel<R, 64, 4>, grid, dim3(64), 0, st, a);
+    if (pieces <= 4 * 128) return launch_on(cache_append_kernel<R, 128, 4>, grid, dim3(128), 0, st, a);
+    return pieces <= 4 * 256 ? launch_on(cache_append_kernel<R, 256, 4>, grid, dim3(256), 0, st, a) : launch_on(cache_append_kernel<R, 256, 8>, grid, dim3(256), 0, st, a);
 }
 
 bool config_ok(const bild_cache_config& g) {

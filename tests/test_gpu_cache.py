@@ -208,6 +208,22 @@ def test_a_growing_scale_rounds_what_is_there_again():
     assert k == np.max(t.o.scales)  or k > 1.2 ** 25
 
 
+@pytest.mark.parametrize("top", [127.0, 100.0, 3.3e-3, 1e-37, 3e-40, 5e26])
+def test_values_on_the_border_between_codes(top):
+    """Halves, and the neighbours of halves, in the last bit: codes are those of the quotient, whatever it is computed by."""
+    t, rng = cache(3, d=64, heads=2)
+
+    def spoil(words, x):
+        y = ((rng.integers(-127, 127, x.shape) + np.float32(0.5)) * np.float64(top) / 127).astype(np.float32)
+        x[...] = np.nextafter(y, np.float32(np.inf) * rng.choice([-1, 1], x.shape).astype(np.float32), where=rng.random(x.shape) < 0.6, out=y.copy())
+        x[:, 0] = np.float32(top)
+        words[...] = x
+
+    extend(t, [30, 9, 1, 32])
+    append(t, rng, 0, [30, 9, 1, 32], F32, spoil=spoil)
+    t.same()
+
+
 def test_values_at_the_ends_of_fp32():
     t, rng = cache(2, d=16, heads=2)
 
