@@ -27,7 +27,7 @@ struct AttendArgs {
     float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
     int prompt_from;      // rows of a sequence, times `group`, from which on it is the kernel for prompts'
     int groups, least;  // workgroups of a key head; what one takes at least
-    int splits;         // of a prompt tile's keys
+    int splits;         // of a prompt tile's keys; most
     float* part;
     unsigned* arrived;
 };
@@ -63,6 +63,17 @@ __device__ __forceinline__ int up_of(float big) {
 constexpr int kTile = 16;      // rows of a tile of the kernels for few rows
 constexpr int kStart = 16;     // blocks that could be read while a workgroup gets to a tile and joins what its waves have of it
 
+// Inclusive prefix sums of a wave: within rows of 16 lanes, then the rows before.
+__device__ __forceinline__ int prefix_sum(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast31 into rows 2 and 3
+    return v;
+}
+
 // A sequence's share of the work.
 struct Seq {
     int s, first, count, length;  // which, its rows, its positions
@@ -91,9 +102,10 @@ __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __built
 
 hipError_t launch_cache_attend_tall(const AttendArgs& a, int dtype, hipStream_t st);  // heads above 128
 hipError_t cache_attend_tall_init();
-hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st);
+hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t places, hipStream_t st);
 hipError_t cache_prompt_init(int d_head);
 size_t prompt_part_floats(int d_head);
-constexpr int kPromptRows = 128;   // of a tile of the kernel for prompts
+constexpr int kPromptRows = 128;  // of a tile of the kernel for prompts
+constexpr int kMaxSplits = 16;    // pieces of a tile's keys
 
 }  // namespace bild

@@ -32,17 +32,6 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
     return a < (1ll << 32) && b < (1ll << 32) ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// Inclusive prefix sums of a wave: within rows of 16 lanes, then the rows before.
-__device__ __forceinline__ int prefix_sum(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast15 into rows 1 and 3
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast31 into rows 2 and 3
-    return v;
-}
-
 // What each workgroup takes of a line: equal pieces, none less than `least` unless it is all there is.
 __device__ __forceinline__ long long piece_of(long long line, int groups, int least) {
     const long long pieces = min(max(quotient(line, least), 1ll), (long long)groups);
@@ -508,7 +497,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 // Rows (times query heads of a key head) of a sequence from which on they take the kernel for prompts: a whole tile of it, or half a one where there is much of it, rows times query heads of all
 // sequences.  (us, this kernel / that one: 16 rows of 4 heads over 2000 positions, 32 sequences of 8 key heads 95 / 69, 64 rows over 8000, 32 key heads 50 / 53, 20 of 4 over 4000, 8 key heads 23 / 33;
 // 60 of 4 over 2000, 8 sequences 86 / 46; 8 of 4 over 2000, 32 sequences 55 / 70.)
-constexpr int kPromptFrom = 64, kPromptWork = 4096, kMaxSplits = 16;
+constexpr int kPromptFrom = 64, kPromptWork = 4096;
 constexpr int kLeast = 20;  // of the line that a workgroup takes
 
 constexpr size_t lds_bytes(int DP) { return sizeof(float) * kWaves * kTile * (DP + 4); }
@@ -571,17 +560,19 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     a.groups = attend_groups(v.heads);
     a.least = kLeast;
     const int64_t tiles = k.starts ? tokens * a.group / kPromptRows + k.n : k.n * (((int64_t)k.rows * a.group + kPromptRows - 1) / kPromptRows);
-    // (fewer tiles than the chip has room for: several workgroups share a tile's keys)
+    // Places for workgroups: fewer tiles than the chip has room for share their keys between several.  Up to 64 sequences that goes by each one's length, which the kernel finds out: at most
+    // kPromptParts are pieces of tiles.
     a.splits = (int)std::min(std::max(kPromptParts / (tiles * v.heads), (int64_t)1), (int64_t)kMaxSplits);
+    const int64_t most = kPromptParts / v.heads, places = k.n > 64 ? tiles * a.splits : k.n > 1 ? tiles + std::min(most, tiles * (kMaxSplits - 1)) : std::max(tiles, std::min(most, tiles * kMaxSplits));
     const int64_t per_head = (int64_t)k.rows * a.group;
-    const bool prompts = (per_head >= kPromptRows || (per_head >= kPromptFrom && tokens * k.heads >= kPromptWork)) && tiles * v.heads * a.splits <= kMaxGroups;
+    const bool prompts = (per_head >= kPromptRows || (per_head >= kPromptFrom && tokens * k.heads >= kPromptWork)) && places * v.heads <= kMaxGroups;
     a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;
     a.part = c->part;
     a.arrived = c->arrived;
     const OnDevice on(c->device);
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (prompts && launch_cache_prompt(a, k.dtype, tiles, st) != hipSuccess) return BILD_EHIP;
+    if (prompts && launch_cache_prompt(a, k.dtype, places, st) != hipSuccess) return BILD_EHIP;
     if (prompts && !k.starts) return BILD_OK;  // (all are prompts; with starts, how many rows a sequence has is known to the kernels alone)
     if (v.d_head > 128) return launch_cache_attend_tall(a, k.dtype, st) == hipSuccess ? BILD_OK : BILD_EHIP;
     const hipError_t err = k.dtype == BILD_DT_F32 ? launch<RowF32>(a, st) : k.dtype == BILD_DT_BF16 ? launch<RowBf16>(a, st) : launch<RowF16>(a, st);

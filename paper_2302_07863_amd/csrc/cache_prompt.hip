@@ -42,14 +42,44 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n32 = lane & 31, half = lane >> 5, d = c.d_head;
     __shared__ unsigned share;
     const int head = blockIdx.x % c.heads;  // (dies take workgroups in turn: those of a head have its keys in few L2s)
-    // The last rows, which see most, come first; those that come second to the compute units the other way round, so that who has much to do shares its unit with who has little
-    // (us, call: 200 rows of 4 heads behind 4000 positions, 8 key heads 52 / 47, 2000 rows behind 3001 198 / 196).
-    const int places = (int)(gridDim.x / c.heads), round = max(kUnits / c.heads, 1), nth = (int)(blockIdx.x / c.heads);
-    const int place_at = places - 1 - (nth >= round && nth < 2 * round ? round + min(places, 2 * round) - 1 - nth : nth), split = place_at % a.splits;
-    // ---- which tile of which sequence: entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles
-    int i, first, count, tile;
-    {
-        const int slot = place_at / a.splits;
+    // ---- which tile of which sequence, and which piece of its keys.  Places are in the order of sequences, rows and keys; the last rows, which see most, come first, those that come second to
+    // the compute units the other way round, so that who has much to do shares its unit with who has little (us, call: 200 rows of 4 heads behind 4000 positions, 8 key heads 52 / 47).
+    const auto place_of = [&](int places) {
+        const int round = max(kUnits / c.heads, 1), nth = (int)(blockIdx.x / c.heads);
+        return places - 1 - (nth >= round && nth < 2 * round ? round + min(places, 2 * round) - 1 - nth : nth);
+    };
+    int s, first, count, tile, length, split, pieces, part_at, flag_at;
+    if (a.r.n <= 64) {
+        // a lane a sequence: its tiles, the keys of one, and as many pieces of these as its share of the whole work is, of kPromptParts at most
+        int mine_s = a.r.sequence(min(lane, a.r.n - 1), c.sequences), mine_first, mine_count;
+        a.r.span(min(lane, a.r.n - 1), mine_first, mine_count);
+        const int mine_rows = mine_count * a.group, mine_tiles = lane < a.r.n && mine_s >= 0 && mine_rows >= a.prompt_from ? (mine_rows + kPromptRows - 1) / kPromptRows : 0;
+        const int mine_length = mine_s < 0 ? 0 : min(max(c.lengths[mine_s], 0), c.cap());
+        int keys = (mine_length + kKeys - 1) / kKeys;
+        if (a.window) keys = (int)min((int64_t)keys, ((int64_t)a.sinks + kKeys - 1) / kKeys + ((int64_t)a.window + kPromptRows / a.group) / kKeys + 2);
+        const float work = wave_sum((float)mine_tiles * (float)keys);
+        const int mine_pieces = min((int)((float)keys * (0.999f * kPromptParts / c.heads) / fmaxf(work, 1.f)), min(kMaxSplits, keys / kSplitLeast));
+        const int mine = max(mine_pieces, 1) * mine_tiles, parts = mine_pieces > 1 ? mine : 0, flags = mine_pieces > 1 ? mine_tiles : 0;
+        const int upto = prefix_sum(mine), parts_upto = prefix_sum(parts), flags_upto = prefix_sum(flags), places = __builtin_amdgcn_readlane(upto, 63);
+        if ((int)(blockIdx.x / c.heads) >= places) return;
+        const int place = place_of(places), at = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(place < upto))), local = place - __builtin_amdgcn_readlane(upto - mine, at);
+        pieces = max(__builtin_amdgcn_readlane(mine_pieces, at), 1);
+        tile = local / pieces;
+        split = local - tile * pieces;
+        part_at = __builtin_amdgcn_readlane(parts_upto - parts, at) + local - split;
+        flag_at = __builtin_amdgcn_readlane(flags_upto - flags, at) + tile;
+        s = __builtin_amdgcn_readlane(mine_s, at);
+        first = __builtin_amdgcn_readlane(mine_first, at);
+        count = __builtin_amdgcn_readlane(mine_count, at);
+        length = __builtin_amdgcn_readlane(mine_length, at);
+    } else {
+        // entry i of the list has the slots floor(first row * group / 128) + i and those behind, as many as it can have tiles
+        const int place = place_of((int)(gridDim.x / c.heads)), slot = place / a.splits;
+        int i;
+        pieces = a.splits;
+        split = place - slot * pieces;
+        flag_at = slot;
+        part_at = slot * pieces;
         if (a.r.starts) {
             int lo = 0, hi = a.r.n;
             while (hi - lo > 1) {
@@ -66,12 +96,12 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             tile = slot - i * per;
             a.r.span(i, first, count);
         }
+        if (tile < 0 || tile * kPromptRows >= count * a.group || count * a.group < a.prompt_from) return;
+        s = a.r.sequence(i, c.sequences);
+        if (s < 0) return;
+        length = min(max(c.lengths[s], 0), c.cap());
     }
     const int rows = count * a.group;
-    if (tile < 0 || tile * kPromptRows >= rows || rows < a.prompt_from) return;
-    const int s = a.r.sequence(i, c.sequences);
-    if (s < 0) return;
-    const int length = min(max(c.lengths[s], 0), c.cap());
     const int idx0 = tile * kPromptRows + wave * 32, idx = min(idx0 + n32, rows - 1), j = idx / a.group, e = idx - j * a.group;
     const auto pos_of = [&](int at) { return a.causal ? length - count + at : length - 1; };
     const int pos = pos_of(j), low = a.window ? pos - a.window : -1;
@@ -80,8 +110,8 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     const int low_tile = a.window ? max(wg_first - a.window + 1, 0) / kKeys : 0;
     const int sink_tiles = a.window ? min((int)(((int64_t)a.sinks + kKeys - 1) / kKeys), low_tile) : 0;
     const int all_tiles = sink_tiles + max((min(wg_last + 1, length) + kKeys - 1) / kKeys - low_tile, 0);
-    // where there are few tiles of rows, several workgroups share a tile's keys
-    const int splits = min(a.splits, max(all_tiles / kSplitLeast, 1));
+    // (the first rows of a sequence may see too few keys for as many pieces)
+    const int splits = min(pieces, max(all_tiles / kSplitLeast, 1));
     if (split >= splits) return;
     const int t0 = all_tiles * split / splits, tiles = all_tiles * (split + 1) / splits;
     const auto tile_at = [&](int t) { return t < sink_tiles ? t : t - sink_tiles + low_tile; };
@@ -347,8 +377,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     if (splits > 1) {
         // a lane's values lie in memory as it has them, 1 KiB a store of a wave: the last of the tile's workgroups has the same lanes
         constexpr int kPart = kPromptRows * (DP + 4);  // floats: see prompt_part_floats
-        const int64_t tile_at = (int64_t)(place_at / a.splits) * c.heads + head;
-        const auto place = [&](int sp) { return make_rsrc(a.part + (tile_at * a.splits + sp) * kPart, sizeof(float) * kPart); };
+        const auto place = [&](int sp) { return make_rsrc(a.part + ((int64_t)(part_at + sp) * c.heads + head) * kPart, sizeof(float) * kPart); };
         const auto mine = place(split);
 #pragma unroll
         for (int u = 0; u < ND; ++u)
@@ -357,7 +386,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
                 __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[u][4 * r]), __float_as_uint(acc[u][4 * r + 1]), __float_as_uint(acc[u][4 * r + 2]), __float_as_uint(acc[u][4 * r + 3])},
                                                        mine, (((wave * ND + u) * 4 + r) * 64 + lane) * 16, 0, kPartAux);
         if (half == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(top), __float_as_uint(sum)}, mine, (kPromptRows * DP + 2 * (wave * 32 + n32)) * 4, 0, kPartAux);
-        if (!last_in(a.arrived + tile_at, (unsigned)splits, &share)) return;
+        if (!last_in(a.arrived + (int64_t)flag_at * c.heads + head, (unsigned)splits, &share)) return;
         float m = -INFINITY, l = 0.f;
         for (int sp = 0; sp < splits; ++sp) {
             const auto ml = __builtin_amdgcn_raw_buffer_load_b64(place(sp), (kPromptRows * DP + 2 * (wave * 32 + n32)) * 4, 0, kPartAux);
@@ -428,8 +457,8 @@ hipError_t cache_prompt_init(int d_head) {
 
 size_t prompt_part_floats(int d_head) { return (size_t)kPromptParts * kPromptRows * ((d_head <= 64 ? 64 : d_head <= 128 ? 128 : 256) + 4); }
 
-hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t tiles, hipStream_t st) {
-    const dim3 grid((unsigned)(a.c.heads * tiles * a.splits));
+hipError_t launch_cache_prompt(const AttendArgs& a, int dtype, int64_t places, hipStream_t st) {
+    const dim3 grid((unsigned)(a.c.heads * places));
     return dtype == BILD_DT_F32 ? launch<RowF32>(a, grid, st) : dtype == BILD_DT_BF16 ? launch<RowBf16>(a, grid, st) : launch<RowF16>(a, grid, st);
 }
 

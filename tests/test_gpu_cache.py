@@ -68,7 +68,8 @@ def attend(t, rng, layer, rows, group=1, dtype=F32, sequences=None, uniform=Fals
     want, want_lse, tol, ltol = o.attend(layer, x.astype(np.float64).reshape(tokens, hq, o.d), rows, float(np.float32(scale)), sequences, dtype=dtype,
                                          **{k: v for k, v in kw.items() if k in ("window", "sinks", "causal")})
     alive = np.isfinite(want_lse)
-    assert np.all(got_lse[~alive] == -np.inf) and np.all(got[~alive] == 0)
+    over = np.repeat([not 0 <= s < len(o.lengths) for s in (range(len(rows)) if sequences is None else sequences)], rows)    # (rows of sequences that are passed over stay what they were)
+    assert np.all(got_lse[over] == 77) and np.all(got_lse[~over][~alive[~over]] == -np.inf) and np.all(got[~alive] == 0)
     close(got_lse[alive], want_lse[alive], ltol[alive])
     close(got, want, tol)
     return got, got_lse
@@ -597,3 +598,23 @@ def test_pools_beyond_32_bits():
             c.compact(used=used.ptr.value)
             assert used.to_host(np.int32, 1)[0] == np.sum(freed > 0)
             assert np.all(table.to_host(np.int32, 6) < used.to_host(np.int32, 1)[0])
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 40)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompts_behind_lengths_far_apart(window, sinks, dtype):
+    """Keys of long sequences are shared between workgroups, those of short ones are not; sequences that are passed over, without rows, without keys."""
+    lengths = [2900, 130, 129, 0, 700, 64, 5, 260]
+    t, rng = filled(60, lengths, pages=90, page=64, heads=1, d=64, max_pages=50)
+    ids = [5, 0, -1, 3, 1, 7, 4, 6]
+    attend(t, rng, 0, [64, 130, 3, 20, 129, 0, 33, 9], 7, dtype, sequences=ids, window=window, sinks=sinks)
+
+
+def test_prompts_of_more_sequences_than_a_wave():
+    lengths = [int(x) for x in np.random.default_rng(8).integers(0, 90, 80)]
+    lengths[7], lengths[70] = 1500, 640
+    t, rng = filled(61, lengths, pages=200, page=64, heads=2, d=16, max_pages=30)
+    rows = [min(x, 70) if i % 3 else 1 for i, x in enumerate(lengths)]
+    rows[7], rows[70] = 130, 600
+    attend(t, rng, 0, rows, 4, BF16)
+    attend(t, rng, 0, [50] * 80, 4, F16, uniform=True)
