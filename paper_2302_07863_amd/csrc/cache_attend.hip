@@ -1,16 +1,19 @@
-// Attention over the cache in 8 bits (bild_cache_attend), all keys or a sliding window with sinks.
+// Attention over the cache in 8 bits (bild_cache_attend), all keys or a sliding window with sinks: the kernel for a few rows a sequence, heads up to 128, and the choice between this one, the one for
+// prompts (cache_prompt.hip) and the one for larger heads (cache_attend_tall.hip).
 //
 //   out = sum_j p_j s_v[j] cv_j / 127,  p = softmax_j(scale s_k[j] q ck_j / 127)
 //
-// Bound, for a few rows a sequence: HBM, a byte a value, each key and value read once for all rows and query heads of its key head.  Sixteen such rows are one operand of the matrix
-// cores.  Scores come out transposed, S^T = K Q^T, so that a lane has eight consecutive keys of one row, which is what the second product, O^T = V^T P^T, takes from it: weights
-// go from one to the other in registers.  Codes become fp16 by a byte permutation and a packed product and sum (cache_attend.h),
-// with the values' transposition into the bargain: the pairs that the permutation joins are two tokens' codes.  A page's scale is applied to
-// scores and to partial sums in fp32.
+// Bound: HBM, a byte a value, each key and value read once for all rows and query heads of its key head (up to 16: a tile).  The tile's rows are one operand of the matrix cores.  Scores come out
+// transposed, S^T = K Q^T, so that a lane has eight consecutive keys of one row, which is what the second product, O^T = V^T P^T, takes from it: weights go from one to the other in
+// registers.  Codes become fp16 by a byte permutation and a packed product and sum (cache_attend.h), with the values' transposition into the bargain: the pairs that the permutation joins are two
+// tokens' codes.  A page's scale is applied to scores and to partial sums in fp32.
 //
 // Work is cut where it is: the 32-token blocks of all sequences and row tiles lie in one line, of which each workgroup of a key head takes an equal piece, wherever sequences begin or
 // end (the lengths are in device memory, and a batch's are far apart); a workgroup's eight waves take turns over its blocks, or over tiles that are short.  What several workgroups have
 // of a tile the last of them joins, in order.
+//
+// Measured: 32 heads of 128 over 65537 positions, fp16, 91 us, 5.9 TB/s (reads alone reach 6.1).  64 sequences of up to 16384, 8 key heads: 60 us, 4.0 TB/s: a workgroup gets to two or three
+// tiles, each behind table, scales and codes, one load after the other (some 3 us).  One sequence of 513 positions 7.6 us: launch, lengths, table, scales, codes, and two meetings.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

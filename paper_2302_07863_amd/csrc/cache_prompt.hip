@@ -1,9 +1,17 @@
 // Attention of prompts over the cache in 8 bits (bild_cache_attend): sequences with many rows.
 //
-// Bound: the matrix cores, and beside them the exponentials.  A workgroup has 128 rows (rows times the query heads of a key head) of a sequence and walks over its keys, 64 at a time: their codes
-// come from memory into registers while the tile before is multiplied, become fp16 on their way into LDS (once for all rows), the values transposed.  A wave has 32 rows; scores come out as
-// S^T = K Q^T, so that weights stay in registers as the operand of O^T = V^T P^T: lane l has row l % 32 and of each 16 keys the eight of its half, and the values lie in LDS in that order of keys.
-// Chunks of 16 bytes are swapped within a row of LDS by the row's number, so that neither product's reads meet in a bank.
+//   out = sum_j p_j s_v[j] cv_j / 127,  p = softmax_j(scale s_k[j] q ck_j / 127), a running maximum and sum, rescaled where a tile's maximum is 2^8 beyond it
+//
+// A workgroup has 128 rows (rows times the query heads of a key head) of a sequence and walks over its keys, 64 at a time: their codes come from memory into registers while the tile before is
+// multiplied, become fp16 on their way into LDS (once for all rows), the values transposed.  A wave has 32 rows; scores come out as S^T = K Q^T, so that weights stay in registers as the operand
+// of O^T = V^T P^T: lane l has row l % 32 and of each 16 keys the eight of its half, and the values lie in LDS in that order of keys.  Chunks of 16 bytes are swapped within a row of LDS by the
+// row's number, so that neither product's reads meet in a bank.  Scores of keys that a row does not see begin as -infinity.  A page's scale of the values goes into the exponent of its weights (one
+// sum, no product a value), relative to a power of two that the results are in units of.
+//
+// Bound: issue slots and the matrix cores, which work by turns more than side by side.  2000 rows of 32 heads of 128, 8 key heads, behind 3001 positions (131 GFLOP): 158 us back to back, at 2.0 GHz,
+// some 830 TFLOP/s where a large product reaches 1191; a tile of a wave is some 410 slots (32 products, 34 of four slots) and 1024 cycles of the matrix cores, and takes 2560.  Left out in
+// turn, exponentials save 2 us, taking codes apart 12, all products 36.  What did not help: the next tile's scores beside a tile's exponentials (5 to 10 % slower, at 256 registers), waves'
+// priorities, four waves a unit more at 128 registers (spills, 60 % slower).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
