@@ -189,6 +189,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         const auto block_at = [&](int b) { return b < sq.sink_blocks ? b : b - sq.sink_blocks + sq.low_block; };
         // ---- a page and its scales for each of the next 64 blocks of this wave, a lane a block
         int pages = -1;
+        uint32_t where[2] = {0, 0};  // of the block's keys
         float k_scale = 0.f, v_scale = 0.f;
         // a tile that is no more than a wave's share of the piece is one wave's alone, the next one the next wave's
         const bool whole = c0 == 0 && c1 == cost, alone = whole && sq.blocks <= max(chunk / kWaves, 2ll);
@@ -204,6 +205,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
                 pages = c.table[(int64_t)sq.s * c.max_pages + (p0 >> c.page_shift)];
             if (!c.has(pages)) pages = -1;
             if (pages >= 0) {
+                const uint64_t codes = (uint64_t)(c.codes + c.plane(pages, a.layer, 0, head) * c.plane_bytes() + (p0 & (c.page_tokens - 1)) * d);
+                where[0] = (uint32_t)codes;
+                where[1] = (uint32_t)(codes >> 32);
                 k_scale = c.scales[c.plane(pages, a.layer, 0, head)];
                 v_scale = c.scales[c.plane(pages, a.layer, 1, head)] * (512.f / 127.f);
             }
@@ -218,26 +222,25 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 #pragma unroll
         for (int t = 0; t < NJ; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+        const int64_t to_v = (int64_t)c.heads * c.plane_bytes();
         const int key = (n16 >> 2) * 8 + (n16 & 3);  // the lane's row of the first operand, in two halves: tokens key and key + 4
-        const auto load = [&](Codes<DP>& x, int page, int blk) {
-            const int in_page = blk * kBlock & (c.page_tokens - 1);
-            const auto k = make_rsrc(c.codes + c.plane(page, a.layer, 0, head) * c.plane_bytes(), (size_t)c.plane_bytes());
-            const auto v = make_rsrc(c.codes + c.plane(page, a.layer, 1, head) * c.plane_bytes(), (size_t)c.plane_bytes());
-            const int base = in_page * d;
+        const auto load = [&](Codes<DP>& x, uint32_t lo, uint32_t hi) {
+            const int8_t* codes = (const int8_t*)((uint64_t)hi << 32 | lo);
+            const auto k = make_rsrc(codes, (size_t)(kBlock * d)), v = make_rsrc(codes + to_v, (size_t)(kBlock * d));
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int t = 0; t < NK; ++t) {
                     // (rows begin at multiples of 8 bytes)
-                    x.k[h][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, (key + 4 * h) * d + min(64 * t + 16 * g, d - 16), base, kAux));
+                    x.k[h][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, (key + 4 * h) * d + min(64 * t + 16 * g, d - 16), 0, kAux));
                 }
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const int off = (8 * g + t) * d + min(n16 * NJ, d - NJ);
                 if constexpr (WV == 1) {
-                    x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, base, kAux);
+                    x.v[t][0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(v, off, 0, kAux);
                 } else {
-                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, base, kAux);
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(v, off, 0, kAux);
                     x.v[t][0] = (uint32_t)y[0];
                     x.v[t][1] = (uint32_t)y[1];
                 }
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const int at_pos = p0 + t;
-                const bool sees = at_pos <= pos && (at_pos > low || at_pos < a.sinks);
+                const bool sees = (at_pos <= pos) & ((at_pos > low) | (at_pos < a.sinks));
                 p[t] = sees ? z[t >> 2][t & 3] * by : -INFINITY;
                 big = fmaxf(big, p[t]);
             }
@@ -323,7 +326,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
                 const int page = __builtin_amdgcn_readlane(pages, nth), was = nth++;
                 if (page >= 0) {
                     r.blk = block_at(b);
-                    load(x, page, r.blk);
+                    load(x, (uint32_t)__builtin_amdgcn_readlane((int)where[0], was), (uint32_t)__builtin_amdgcn_readlane((int)where[1], was));
                     // (the scales were asked for before: whoever waits for them does not wait for these codes)
                     r.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), was));
                     r.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), was));
