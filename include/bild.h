@@ -460,7 +460,7 @@ typedef struct bild_cache_config {
     int32_t max_pages;   /* of a sequence; max_pages * page_tokens <= 2^30, sequences * max_pages <= 2^28 */
     int32_t reserved;    /* 0                                                                    */
 } bild_cache_config;
-typedef struct bild_cache bild_cache; /* the geometry, and device memory for what the calls' kernels hand on */
+typedef struct bild_cache bild_cache; /* the geometry, and device memory for what the calls' kernels hand on: 18, 35, 69 MB for d_head up to 64, 128, 256, and 4 x (sequences x (max_pages + 7) + 6 x pages) bytes */
 int bild_cache_create(const bild_cache_config* cfg, bild_cache** out);
 int bild_cache_destroy(bild_cache* c); /* nothing that uses it may still run */
 
