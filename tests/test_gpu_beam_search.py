@@ -5,8 +5,8 @@ import pytest
 
 import paper_2302_07863_amd as pkg
 from tests.cached import Held, Oracle, invariants
-from tests.hipmem import DeviceArray
-from tests.rows import F16, F32, U32, close, ruled, scales_of, turned, weights
+from tests.hipmem import H2D, DeviceArray, hip
+from tests.rows import F16, F32, U32, Graph, Stream, close, ruled, scales_of, turned, weights
 from tests.test_gpu_beams import choose
 
 pytestmark = pytest.mark.gpu
@@ -165,3 +165,57 @@ def test_reviews_of_drafts():
         p.cache.cache.extend(2, 0, sequences=ids.ptr.value, cut=cut.ptr.value)
         p.cache.same()
         assert list(o.lengths[[1, 4]]) == list(keep)
+
+
+@pytest.mark.parametrize("beams,max_pages,pages", [(4, 40, 120), (3, 6000, 90)])
+def test_captured_steps(beams, max_pages, pages):
+    """Choice, fork, growth and packing in one graph: parents go from kernel to kernel, and every replay meets other logits and other pages."""
+    rng = np.random.default_rng(23)
+    batch, vocab = 3, 300
+    n = batch * beams
+    t = Held(Oracle(pages, 32, 2, 1, 16, n, max_pages))
+    chooser = pkg.Beams(vocab, batch, beams)
+    start = np.array([40 + 7 * s for s in range(n)], np.int32)
+    assert t.o.extend(start)
+    starts = DeviceArray(np.concatenate(([0], np.cumsum(start))).astype(np.int32))
+    t.cache.extend(n, starts=starts.ptr.value)
+    logits, scores = DeviceArray(nbytes=4 * n * vocab), DeviceArray(np.zeros(n, np.float32))
+    new, parents, tokens, granted, used = (DeviceArray(nbytes=4 * n) for _ in range(5))
+    st = Stream()
+
+    def step(stream):
+        chooser.select(logits.ptr.value, F32, batch, beams, scores.ptr.value, new.ptr.value, parents.ptr.value, tokens.ptr.value, stream=stream)
+        t.cache.fork(n, parents.ptr.value, group=beams, stream=stream)
+        t.cache.extend(n, 1, granted=granted.ptr.value, stream=stream)
+        t.cache.compact(used=used.ptr.value, stream=stream)
+
+    def put(mem, a):
+        assert hip().hipMemcpy(mem.ptr, np.ascontiguousarray(a).ctypes.data, a.nbytes, H2D) == 0
+
+    g = Graph(st, step)
+    moved = 0
+    for replay in range(8):
+        z, s = (3 * rng.standard_normal((n, vocab))).astype(np.float32), rng.standard_normal(n).astype(np.float32)
+        put(logits, z)
+        put(scores, s)
+        g.replay()
+        st.sync()
+        got = parents.to_host(np.int32, n)
+        for b in range(batch):
+            at = slice(b * beams, (b + 1) * beams)
+            want = choose(z[at].astype(np.float64), s[at], beams, np.zeros(beams, np.int32), np.zeros(beams, np.int32), -1, 0, 0.0, np.zeros((beams, 0), np.int32))
+            assert np.array_equal(got[at], want["parents"]) and np.array_equal(tokens.to_host(np.int32, n)[at], want["tokens"])
+        t.o.fork(got, None, beams)
+        assert t.o.extend([1] * n) and granted.to_host(np.int32, 1)[0] == 1
+        before = t.o.table.copy()
+        assert used.to_host(np.int32, 1)[0] == t.o.compact()
+        moved += int(np.any(before != t.o.table))
+        t.same()
+        invariants(t.o)
+        if replay % 3 == 2:                                     # eager work between replays
+            cut = np.maximum(t.o.lengths - 30, 1).astype(np.int32)
+            mem = DeviceArray(cut)
+            t.o.extend([0] * n, None, cut)
+            t.cache.extend(n, 0, cut=mem.ptr.value)
+            t.same()
+    assert moved > 0
