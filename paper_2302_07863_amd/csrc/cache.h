@@ -63,8 +63,10 @@ struct bild_cache {
 
 namespace bild {
 
-constexpr int kAttendGroups = 256;                       // workgroups of a launch, but for one a key head
-inline int attend_groups(int heads) { return (kAttendGroups + heads - 1) / heads; }  // of a key head
+// Workgroups of a launch: one a compute unit, and one a key head at least.  One more than there are units and it would take twice the time (us, call, 264 / 252 of them: 16 sequences of 3000
+// positions, 12 key heads of 128 61 / 43; 280 / 240: 4 of 8000, 40 key heads 101 / 72).
+constexpr int kAttendGroups = 256;
+inline int attend_groups(int heads) { return std::max(kAttendGroups / heads, 1); }  // of a key head
 hipError_t attend_init(int d_head);                      // what its kernels need of the current device
 size_t attend_part_floats(int heads, int d_head);        // of bild_cache::part
 constexpr int kPromptParts = 512;                        // most workgroups of a launch that shares the keys of tiles of prompts: two a compute unit

@@ -618,3 +618,10 @@ def test_prompts_of_more_sequences_than_a_wave():
     rows[7], rows[70] = 130, 600
     attend(t, rng, 0, rows, 4, BF16)
     attend(t, rng, 0, [50] * 80, 4, F16, uniform=True)
+
+
+@pytest.mark.parametrize("heads", [5, 12, 40, 300])
+def test_head_counts_that_share_the_chip_unevenly(heads):
+    t, rng = filled(heads, [200, 31], pages=12, page=32, heads=heads, d=16, max_pages=8)
+    attend(t, rng, 0, [1, 1], 2, BF16, uniform=True)
+    attend(t, rng, 0, [40, 2], 2, F32)
