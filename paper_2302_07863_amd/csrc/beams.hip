@@ -148,46 +148,55 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
 #pragma unroll
         for (int k = 0; k < KEPT; ++k) kept[k] = tops[min(b * chunks + c0 + 64 * k, all - 1)];
     }
-    // ---- what each beam's logits are ranked by: a wave has a beam's statistics, another one what its length counts for
-    for (int item = wave; item < 2 * a.beams; item += kPickWaves) {
-        const int b = item < a.beams ? item : item - a.beams;
-        const bool ended = a.finished && a.finished[row0 + b] != 0;
-        if (item >= a.beams) {
-            const int length = a.lengths ? a.lengths[row0 + b] : 0;
-            const double to = a.penalty == 0.f ? 1.0 : exp((double)a.penalty * log((double)max(ended ? length : length + 1, 1)));
-            if (lane == 0) {
-                over[b] = to;
-                by_f[b] = (float)(1.0 / to);
-                if (!ended && !(to < 1e30 && to > 1e-30)) far = 1;  // (beyond what fp32 can sort)
-            }
-            continue;
-        }
-        const float2* part = a.sums + (row0 + b) * a.parts * kWaves;
+    // ---- what each beam's logits are ranked by: a wave a beam for the sums, then a lane a beam; one wave has what their lengths count for, a lane a beam
+    if (wave == kPickWaves - 1 && lane < a.beams) {
+        const bool ended = a.finished && a.finished[row0 + lane] != 0;
+        const int length = a.lengths ? a.lengths[row0 + lane] : 0;
+        const double to = a.penalty == 0.f ? 1.0 : exp((double)a.penalty * log((double)max(ended ? length : length + 1, 1)));
+        over[lane] = to;
+        by_f[lane] = (float)(1.0 / to);
+        if (!ended && !(to < 1e30 && to > 1e-30)) far = 1;  // (beyond what fp32 can sort)
+    }
+    {
         const int n = a.parts * kWaves;
-        const float score = a.scores[row0 + b];
+        const auto part_of = [&](int b) { return a.sums + (row0 + b) * a.parts * kWaves; };
         float2 x[KEPT];
+        const auto load = [&](int b) {
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k) x[k] = part[min(lane + 64 * k, n - 1)];
-        float m = -INFINITY;
+            for (int k = 0; k < KEPT; ++k) x[k] = part_of(b)[min(lane + 64 * k, n - 1)];
+        };
+        if (wave < a.beams) load(wave);
+        for (int b = wave; b < a.beams; b += kPickWaves) {
+            const float2* part = part_of(b);
+            float m = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k) m = fmaxf(m, x[k].x);
-        for (int p = lane + 64 * KEPT; p < n; p += 64) m = fmaxf(m, part[p].x);
-        m = wave_max(m);
-        const float from = m == -INFINITY ? 0.f : m;
-        double s = 0.0;
+            for (int k = 0; k < KEPT; ++k) m = fmaxf(m, x[k].x);
+            for (int p = lane + 64 * KEPT; p < n; p += 64) m = fmaxf(m, part[p].x);
+            m = wave_max(m);
+            const float from = m == -INFINITY ? 0.f : m;
+            double s = 0.0;
 #pragma unroll
-        for (int k = 0; k < KEPT; ++k)
-            if (lane + 64 * k < n) s += (double)(x[k].y * fexp_full(x[k].x - from));
-        for (int p = lane + 64 * KEPT; p < n; p += 64) s += (double)(part[p].y * fexp_full(part[p].x - from));
+            for (int k = 0; k < KEPT; ++k)
+                if (lane + 64 * k < n) s += (double)(x[k].y * fexp_full(x[k].x - from));
+            for (int p = lane + 64 * KEPT; p < n; p += 64) s += (double)(part[p].y * fexp_full(part[p].x - from));
+            if (b + kPickWaves < a.beams) load(b + kPickWaves);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-        const double at = (double)score - ((double)m + log(s));
-        if (lane == 0) {
-            const bool live = !ended && fabs(at) < INFINITY;
-            base[b] = live ? at : NAN;  // (NaN: this beam's logits offer nothing)
-            base_f[b] = live ? (float)at : NAN;
-            if (live && !(fabs(at) < 1e30)) far = 1;
+            for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+            if (lane == 0) {
+                base_f[b] = m;
+                base[b] = s;
+            }
         }
+    }
+    const float score = wave == 0 && lane < a.beams ? a.scores[row0 + lane] : 0.f;
+    const bool goes_on = wave == 0 && lane < a.beams && !(a.finished && a.finished[row0 + lane] != 0);
+    lds_barrier();
+    if (wave == 0 && lane < a.beams) {
+        const double at = (double)score - ((double)base_f[lane] + log(base[lane]));
+        const bool live = goes_on && fabs(at) < INFINITY;
+        base[lane] = live ? at : NAN;  // (NaN: this beam's logits offer nothing)
+        base_f[lane] = live ? (float)at : NAN;
+        if (live && !(fabs(at) < 1e30)) far = 1;
     }
     lds_barrier();
     const auto rank_of = [&](int b, float z) { return (base[b] + (double)z) / over[b]; };

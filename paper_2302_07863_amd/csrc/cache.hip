@@ -711,7 +711,10 @@ extern "C" int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
     if (launch_on(cache_compact_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) != hipSuccess) return BILD_EHIP;
-    return launch_on(cache_move_kernel, dim3(kMoveGroups), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
+    // (at most half of the pages move; a table a workgroup)
+    const CacheView& v = c->view;
+    const int64_t pieces = ((int64_t)v.layers * 2 * v.heads * v.plane_bytes() + kPiece - 1) / kPiece, groups = std::min<int64_t>(std::max<int64_t>(v.pages / 2 * pieces, v.sequences), kMoveGroups);
+    return launch_on(cache_move_kernel, dim3((unsigned)groups), dim3(256), 0, st, a) == hipSuccess ? BILD_OK : BILD_EHIP;
 }
 
 extern "C" int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* hip_stream) {
