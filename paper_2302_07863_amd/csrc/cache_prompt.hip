@@ -61,12 +61,26 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         // a lane a sequence: its tiles, the keys of one, and as many pieces of these as its share of the whole work is, of kPromptParts at most
         int mine_s = a.r.sequence(min(lane, a.r.n - 1), c.sequences), mine_first, mine_count;
         a.r.span(min(lane, a.r.n - 1), mine_first, mine_count);
-        const int mine_rows = mine_count * a.group, mine_tiles = lane < a.r.n && mine_s >= 0 && mine_rows >= a.prompt_from ? (mine_rows + kPromptRows - 1) / kPromptRows : 0;
+        const int mine_rows = mine_count * a.group;
+        int mine_tiles = lane < a.r.n && mine_s >= 0 && mine_rows >= a.prompt_from ? (mine_rows + kPromptRows - 1) / kPromptRows : 0;
         const int mine_length = mine_s < 0 ? 0 : min(max(c.lengths[mine_s], 0), c.cap());
         int keys = (mine_length + kKeys - 1) / kKeys;
         if (a.window) keys = (int)min((int64_t)keys, ((int64_t)a.sinks + kKeys - 1) / kKeys + ((int64_t)a.window + kPromptRows / a.group) / kKeys + 2);
         const float work = wave_sum((float)mine_tiles * (float)keys);
         const int mine_pieces = min((int)((float)keys * (0.999f * kPromptParts / c.heads) / fmaxf(work, 1.f)), min(kMaxSplits, keys / kSplitLeast));
+        // One sequence whose first tiles see few keys and whose last ones see many: the last ones, which have at least two shares, are cut into `high` pieces (us, call: 2500 rows of 8 heads of an
+        // empty cache, 2 key heads 75 / 66).
+        int low_tiles = mine_tiles, high = 0;
+        if (a.r.n == 1 && a.causal && !a.window && mine_pieces <= 1 && mine_tiles > 0) {
+            const int seen = max(mine_length - mine_count + min(kPromptRows, mine_rows) / a.group, 0) / kKeys + 1;  // tiles of keys that the first rows see
+            const float share = fmaxf((float)mine_tiles * 0.5f * (float)(seen + keys) * (float)c.heads / kPromptParts, (float)kSplitLeast);
+            high = min((int)((float)keys / share), kMaxSplits);
+            if (high > 1 && keys > seen) {
+                low_tiles = min(max((int)ceilf((float)mine_tiles * (2.f * share - (float)seen) / (float)(keys - seen)), 0), mine_tiles);
+                low_tiles = max(low_tiles, mine_tiles - kPromptParts / (c.heads * high));
+            }
+        }
+        if (lane == 0 && low_tiles < mine_tiles) mine_tiles = low_tiles + (mine_tiles - low_tiles) * high;  // (from here on: places)
         const int mine = max(mine_pieces, 1) * mine_tiles, parts = mine_pieces > 1 ? mine : 0, flags = mine_pieces > 1 ? mine_tiles : 0;
         const int upto = prefix_sum(mine), parts_upto = prefix_sum(parts), flags_upto = prefix_sum(flags), places = __builtin_amdgcn_readlane(upto, 63);
         if ((int)(blockIdx.x / c.heads) >= places) return;
@@ -76,6 +90,14 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         split = local - tile * pieces;
         part_at = __builtin_amdgcn_readlane(parts_upto - parts, at) + local - split;
         flag_at = __builtin_amdgcn_readlane(flags_upto - flags, at) + tile;
+        low_tiles = __builtin_amdgcn_readlane(low_tiles, 0);
+        if (a.r.n == 1 && place >= low_tiles && __builtin_amdgcn_readlane(mine_tiles, 0) > low_tiles) {
+            pieces = __builtin_amdgcn_readlane(high, 0);
+            flag_at = (place - low_tiles) / pieces;
+            split = place - low_tiles - flag_at * pieces;
+            part_at = flag_at * pieces;
+            tile = low_tiles + flag_at;
+        }
         s = __builtin_amdgcn_readlane(mine_s, at);
         first = __builtin_amdgcn_readlane(mine_first, at);
         count = __builtin_amdgcn_readlane(mine_count, at);

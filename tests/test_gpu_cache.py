@@ -625,3 +625,10 @@ def test_head_counts_that_share_the_chip_unevenly(heads):
     t, rng = filled(heads, [200, 31], pages=12, page=32, heads=heads, d=16, max_pages=8)
     attend(t, rng, 0, [1, 1], 2, BF16, uniform=True)
     attend(t, rng, 0, [40, 2], 2, F32)
+
+
+@pytest.mark.parametrize("page,rows,length", [(64, 700, 700), (32, 640, 705)])
+def test_a_prompt_whose_last_rows_see_most(page, rows, length):
+    """Fewer tiles than workgroups have room, and keys from none to all: the last tiles are shared, the first are not."""
+    t, rng = filled(page, [length], pages=26, page=page, heads=4, d=16, max_pages=26)
+    attend(t, rng, 0, [rows], 16, BF16, uniform=True)
