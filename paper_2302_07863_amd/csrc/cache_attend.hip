@@ -569,7 +569,7 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     // Places for workgroups: fewer tiles than the chip has room for share their keys between several.  Up to 64 sequences that goes by each one's length, which the kernel finds out: at most
     // kPromptParts are pieces of tiles.
     a.splits = (int)std::min(std::max(kPromptParts / (tiles * v.heads), (int64_t)1), (int64_t)kMaxSplits);
-    const int64_t most = kPromptParts / v.heads, places = k.n > 64 ? tiles * a.splits : k.n == 1 && tiles >= most ? tiles : tiles + std::min(most, tiles * (kMaxSplits - 1));
+    const int64_t most = kPromptParts / v.heads, places = k.n > 64 ? tiles * a.splits : k.n > 1 ? tiles + std::min(most, tiles * (kMaxSplits - 1)) : std::max(tiles, std::min(most, tiles * kMaxSplits));
     const int64_t per_head = (int64_t)k.rows * a.group;
     const bool prompts = (per_head >= kPromptRows || (per_head >= kPromptFrom && tokens * k.heads >= kPromptWork)) && places * v.heads <= kMaxGroups;
     a.prompt_from = prompts ? kPromptFrom : 0x7FFFFFFF;

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
             high = min((int)((float)keys / share), kMaxSplits);
             if (high > 1 && keys > seen) {
                 low_tiles = min(max((int)ceilf((float)mine_tiles * (2.f * share - (float)seen) / (float)(keys - seen)), 0), mine_tiles);
-                low_tiles = max(low_tiles, mine_tiles - kPromptParts / (c.heads * high));
+                low_tiles = max(low_tiles, mine_tiles - max(kPromptParts / c.heads - mine_tiles, 0) / (high - 1));  // (no more places than the launch has, and parts)
             }
         }
         if (lane == 0 && low_tiles < mine_tiles) mine_tiles = low_tiles + (mine_tiles - low_tiles) * high;  // (from here on: places)
