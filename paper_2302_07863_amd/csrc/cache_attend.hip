@@ -12,8 +12,10 @@
 // end (the lengths are in device memory, and a batch's are far apart); a workgroup's eight waves take turns over its blocks, or over tiles that are short.  What several workgroups have
 // of a tile the last of them joins, in order.
 //
-// Measured: 32 heads of 128 over 65537 positions, fp16, 91 us, 5.9 TB/s (reads alone reach 6.1).  64 sequences of up to 16384, 8 key heads: 60 us, 4.0 TB/s: a workgroup gets to two or three
-// tiles, each behind table, scales and codes, one load after the other (some 3 us).  One sequence of 513 positions 7.6 us: launch, lengths, table, scales, codes, and two meetings.
+// Measured: 32 heads of 128 over 65537 positions, fp16, 92 us, 5.8 TB/s (reads alone reach 6.1).  64 sequences of up to 16384, 8 key heads: 59 us, 4.0 TB/s: a workgroup gets to two to four
+// tiles, and from the beginning of one to its meeting are some 10 us beside its blocks: lengths 1, table and scales 2, first codes 2.4, joining waves 3, meeting and joining parts 3.
+// One sequence of 513 positions 7.7 us: the same chain.  What did not help: codes of two blocks on their way (the same to 3 % slower), a piece of the line a wave instead of a workgroup (batches of
+// short sequences 5 to 15 % faster, all else 3 to 10 % slower).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
