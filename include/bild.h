@@ -535,7 +535,7 @@ int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* call, void* h
 /* ---- beams ----
  * The best continuations of each of `batch` groups of `beams` rows.  A beam that has not ended goes on with any id v: its sum is scores + logit - lse of its row (lse in fp32, sums in 64 bits from there),
  * its length one more.  One that has ended goes on with `pad` alone, sum and length unchanged.  The `choices` best by sum / max(length, 1)^penalty come out in that order, of equals the lower beam and id first.  Beams
- * whose score is -infinity or NaN, rows without finite lse and ids of logit -infinity offer nothing; choices that nobody offers: parent and token -1, score -infinity, length 0, ended.
+ * whose score is -infinity or NaN (that have not ended: no finite number), rows without finite lse and ids of logit -infinity offer nothing; choices that nobody offers: parent and token -1, score -infinity, length 0, ended.
  * Nothing that is written may overlap what is read. */
 typedef struct bild_beams_call {
     const void* logits;        /* [batch * beams][vocab]                                          */
