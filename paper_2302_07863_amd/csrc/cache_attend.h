@@ -61,7 +61,9 @@ __device__ __forceinline__ int up_of(float big) {
 }
 
 constexpr int kTile = 16;      // rows of a tile of the kernels for few rows
-constexpr int kStart = 16;     // blocks that could be read while a workgroup gets to a tile and joins what its waves have of it
+// Blocks that could be read while a workgroup gets to a tile and joins what its waves have of it (us, call, of 16 / 32 / 48: 64 sequences of up to 16384 positions 63.2 / 65.5 / 69.6, 64 of 500
+// 28.3 / 28.3 / 32.2, one of 513 12.9 / 14.5 / 14.2).
+constexpr int kStart = 16;
 
 // Inclusive prefix sums of a wave: within rows of 16 lanes, then the rows before.
 __device__ __forceinline__ int prefix_sum(int v) {
