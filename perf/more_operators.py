@@ -394,9 +394,9 @@ def _plain_pages(s, c):
     hole, mover = (refs == 0) & (place < used), (refs > 0) & (place >= used)
     to = torch.argsort((~hole).to(torch.int32), stable=True)  # the holes first, lowest first
     moved = torch.where(mover, to[(torch.cumsum(mover, 0) - 1).clamp(min=0)], place)
-    # the pages that come to lie in each place: itself, or the one that moves there
-    source = place.clone().scatter_(0, moved, torch.where(mover, place, moved))
-    source = torch.where(place < used, source, place)
+    # the page that comes to lie in each place: the one that moves there (movers alone write, each into a hole of its own), else itself
+    source = place.clone()
+    source[moved[mover]] = place[mover]
     for name in ("codes", "scales"):
         s[name].copy_(s[name][source])
     refs.copy_(torch.where(place < used, refs[source], 0))
