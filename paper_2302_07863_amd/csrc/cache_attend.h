@@ -23,7 +23,7 @@ struct AttendArgs {
     float* lse;
     int64_t q_token, q_head, out_token, out_head;
     int layer, heads, group;
-    int window, sinks, causal;
+    int window, sinks, causal;  // (no window is wider than a sequence can be long: up to 2^30)
     float scale;    // of scores, in powers of two, with what codes and scales are short of: log2 e * 2^9 / 127
     int prompt_from;      // rows of a sequence, times `group`, from which on it is the kernel for prompts'
     int groups, least;  // workgroups of a key head; what one takes at least
@@ -80,6 +80,8 @@ __device__ __forceinline__ int prefix_sum(int v) {
 struct Seq {
     int s, first, count, length;  // which, its rows, its positions
     int tiles, sink_blocks, low_block, blocks;
+    // of its row j.  (Rows from before its beginning see nothing: all of them are at -1, so that a window can be taken off in 32 bits.)
+    __device__ int position(int j, int causal) const { return causal ? max(length - count + j, -1) : length - 1; }
     // what a tile counts for in the line
     __device__ int cost() const { return blocks + kStart; }
 };
@@ -91,7 +93,7 @@ __device__ __forceinline__ Seq sequence_at(const AttendArgs& a, int i) {
     q.length = q.s < 0 ? 0 : min(max(a.c.lengths[q.s], 0), a.c.cap());
     const int64_t rows = (int64_t)q.count * a.group;
     q.tiles = rows < a.prompt_from ? (int)((rows + kTile - 1) / kTile) : 0;
-    q.low_block = a.window ? max(q.length - q.count - a.window + 1, 0) / kBlock : 0;
+    q.low_block = a.window ? max(max(q.length - q.count, 0) - a.window + 1, 0) / kBlock : 0;
     q.sink_blocks = a.window ? min((int)(((int64_t)a.sinks + kBlock - 1) / kBlock), q.low_block) : 0;
     q.blocks = max(q.sink_blocks + (q.length + kBlock - 1) / kBlock - q.low_block, 1);  // (one that has none is written all the same)
     return q;

@@ -184,10 +184,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(const AttendA
         const int b0 = block_of(c0), b1 = block_of(c1);
         // ---- rows
         const int rows = sq.count * a.group, idx = tile * kTile + n16, mine = min(idx, rows - 1), j = mine / a.group, e = mine - j * a.group;
-        const int pos = a.causal ? sq.length - sq.count + j : sq.length - 1, low = a.window ? pos - a.window : -1;
+        const int pos = sq.position(j, a.causal), low = a.window ? pos - a.window : -1;
         // the positions that the tile's rows see
         const int j0 = tile * kTile / a.group, j1 = min((tile * kTile + kTile - 1) / a.group, sq.count - 1);
-        const int first_pos = a.causal ? sq.length - sq.count + j0 : sq.length - 1, last_pos = a.causal ? sq.length - sq.count + j1 : sq.length - 1;
+        const int first_pos = sq.position(j0, a.causal), last_pos = sq.position(j1, a.causal);
         const auto block_at = [&](int b) { return b < sq.sink_blocks ? b : b - sq.sink_blocks + sq.low_block; };
         // ---- a page and its scales for each of the next 64 blocks of this wave, a lane a block
         int pages = -1;
@@ -562,7 +562,7 @@ extern "C" int bild_cache_attend(bild_cache* c, const bild_cache_attend_call* ca
     a.layer = k.layer;
     a.heads = k.heads;
     a.group = k.heads / v.heads;
-    a.window = k.window;
+    a.window = std::min(k.window, v.cap());  // (a wider one hides no more)
     a.sinks = k.window ? k.sinks : 0;
     a.causal = k.causal;
     a.scale = (float)((double)k.scale * 1.4426950408889634 * 512.0 / 127.0);

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
         int mine_s = a.r.sequence(min(lane, a.r.n - 1), c.sequences), mine_first, mine_count;
         a.r.span(min(lane, a.r.n - 1), mine_first, mine_count);
         const int mine_rows = mine_count * a.group;
-        int mine_tiles = lane < a.r.n && mine_s >= 0 && mine_rows >= a.prompt_from ? (mine_rows + kPromptRows - 1) / kPromptRows : 0;
+        int mine_tiles = lane < a.r.n && mine_s >= 0 && mine_rows >= a.prompt_from ? (mine_rows - 1) / kPromptRows + 1 : 0;
         const int mine_length = mine_s < 0 ? 0 : min(max(c.lengths[mine_s], 0), c.cap());
         int keys = (mine_length + kKeys - 1) / kKeys;
         if (a.window) keys = (int)min((int64_t)keys, ((int64_t)a.sinks + kKeys - 1) / kKeys + ((int64_t)a.window + kPromptRows / a.group) / kKeys + 2);
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kThreads, R::kDtype == BILD_DT_F32 || DP == 256 ? 1
     }
     const int rows = count * a.group;
     const int idx0 = tile * kPromptRows + wave * 32, idx = min(idx0 + n32, rows - 1), j = idx / a.group, e = idx - j * a.group;
-    const auto pos_of = [&](int at) { return a.causal ? length - count + at : length - 1; };
+    const auto pos_of = [&](int at) { return a.causal ? max(length - count + at, -1) : length - 1; };  // (see Seq::position)
     const int pos = pos_of(j), low = a.window ? pos - a.window : -1;
     // ---- the keys that any row of the tile sees, in tiles
     const int wg_first = pos_of(tile * kPromptRows / a.group), wg_last = pos_of(min(tile * kPromptRows + kPromptRows - 1, rows - 1) / a.group);

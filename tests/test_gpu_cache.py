@@ -632,3 +632,16 @@ def test_a_prompt_whose_last_rows_see_most(page, rows, length):
     """Fewer tiles than workgroups have room, and keys from none to all: the last tiles are shared, the first are not."""
     t, rng = filled(page, [length], pages=26, page=page, heads=4, d=16, max_pages=26)
     attend(t, rng, 0, [rows], 16, BF16, uniform=True)
+
+
+@pytest.mark.parametrize("window,sinks", [((1 << 31) - 1, 0), ((1 << 31) - 1, 3), ((1 << 31) - 1, (1 << 31) - 1), ((1 << 31) - 9, 0), (1 << 30, 0), (97, 0)])
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, F32), (256, F16)])
+def test_windows_that_hide_nothing(window, sinks, d, dtype):
+    """Up to the end of their range, where a sequence has more rows than positions: those from before its beginning see nothing, the others all that is in front of them."""
+    t, rng = filled(d, [3, 40, 97, 0], pages=10, page=32, heads=2, d=d, max_pages=4)
+    attend(t, rng, 0, [8, 1, 2, 5], 2, dtype, window=window, sinks=sinks)       # few rows
+    got, lse = attend(t, rng, 0, [130, 90, 97, 70], 2, dtype, window=window, sinks=sinks)  # prompts
+    again, lse_again = attend(t, np.random.default_rng(1), 0, [8], 1, dtype, window=window, sinks=sinks)
+    open_, lse_open = attend(t, np.random.default_rng(1), 0, [8], 1, dtype)
+    assert np.array_equal(lse_again, lse_open) and np.array_equal(again, open_)
+    assert np.all(lse[:127] == -np.inf) and np.all(np.isfinite(lse[127:130]))
