@@ -31,7 +31,8 @@ struct ExtendArgs {
     CacheRows r;
     const int* cut;
     int* granted;
-    int window, sinks;
+    int window, sinks;     // (0: nothing is given back behind a window)
+    int pieces;            // of a table, each looked through by a wave (see slide)
     int *plan;             // [sequences][4], 16-byte aligned: entries
     int *fresh;            // [pages]: the free pages that are given away, lowest first
     int *asked, *latest;   // [pages], zero between launches: how many of a shared page's holders want to write into it, the last of these + 1
@@ -69,19 +70,43 @@ __device__ __forceinline__ int scan(int v, int& total, int* sums) {
     return before + x - v;
 }
 
-// Pages [from, to) of a sequence are given back, by the whole wave.  up_to_none: from the last on, and no further than 64 entries that have none.
-__device__ __forceinline__ void give_back(const CacheView& c, int64_t row, int from, int to, bool up_to_none) {
+// Pages [from, to) of a sequence are given back, by the whole wave, EACH x 64 entries at a time.  Whether there were any.
+template <int EACH>
+__device__ __forceinline__ bool give_back(const CacheView& c, int64_t row, int from, int to) {
     const int lane = threadIdx.x & 63;
-    for (int last = to; last > from; last -= 64) {
-        const int b = last - 1 - lane;
-        int p = -1;
-        if (b >= from) {
-            p = c.table[row + b];
-            if (p != -1) c.table[row + b] = -1;
-            if (c.has(p)) atomicSub(&c.refs[p], 1);
+    bool any = false;
+    for (int b0 = from; b0 < to; b0 += 64 * EACH) {
+        int p[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int b = b0 + 64 * e + lane;
+            p[e] = b < to ? c.table[row + b] : -1;
         }
-        if (up_to_none && !__any(p != -1)) break;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            if (p[e] != -1) c.table[row + b0 + 64 * e + lane] = -1;
+            if (c.has(p[e])) atomicSub(&c.refs[p[e]], 1);
+            any |= p[e] != -1;
+        }
     }
+    return any;
+}
+
+// Positions that entry i's sequence s keeps.
+__device__ __forceinline__ int kept(const ExtendArgs& a, int i, int s) {
+    const int length = min(max(a.c.lengths[s], 0), a.c.cap());
+    return a.cut ? min(max(a.cut[i], 0), length) : length;
+}
+
+// What the window of entry u / pieces has left behind, in piece u % pieces of its table, is given back, by the whole wave.  All of it is looked through each time: calls with fewer sinks or
+// another window than those before leave pages anywhere in it, and nothing but the table, which is the caller's, says where.
+constexpr int kSlideEach = 8;
+__device__ __forceinline__ bool slide(const ExtendArgs& a, int u, int pieces) {
+    const CacheView& c = a.c;
+    const int i = u / pieces, from = (u - i * pieces) * 64 * kSlideEach, s = a.r.sequence(i, c.sequences);
+    if (s < 0) return false;
+    const int end = max(kept(a, i, s) - a.window + 1, 0) >> c.page_shift, sinks = (int)(((int64_t)a.sinks + c.page_tokens - 1) >> c.page_shift);
+    return give_back<kSlideEach>(c, (int64_t)s * c.max_pages, max(from, sinks), min(from + 64 * kSlideEach, end));
 }
 
 // One workgroup, as who gets which page is a matter of order: needs are summed over the list, free pages over the pool, both by prefix sums.  Bound: launch and a chain of loads - length, table, count of
@@ -98,6 +123,9 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
 #pragma unroll
     for (int e = 0; e < 8; ++e) counts[e] = 8 * tid + e < c.pages ? seen(&c.refs[8 * tid + e]) : 1;
     __syncthreads();
+    if (a.window > 0)
+        for (int u = tid >> 6; u < n * a.pieces; u += kPlanWaves)
+            if (slide(a, u, a.pieces)) freed = 1;
     // (a thread's first entry stays in registers, further ones of long lists go through memory)
     Entry mine = {0, 0, 0, -1, -1};
     const auto entry = [&](int i) {
@@ -109,34 +137,28 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
         if (i < kPlanThreads) mine = q;
         else *(int4*)(a.plan + 4 * (int64_t)i) = make_int4(q.keep, q.add, q.before, q.shared);
     };
-    // the cut, and what a window has left behind
+    // the cut
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid, s = i < n ? a.r.sequence(i, c.sequences) : -1;
-        int length = 0, keep = 0, add = 0, slide0 = 0, slide1 = 0;
+        int length = 0, keep = 0, add = 0;
         if (s >= 0) {
             int first;
             length = min(max(c.lengths[s], 0), c.cap());
-            keep = a.cut ? min(max(a.cut[i], 0), length) : length;
+            keep = kept(a, i, s);
             if (a.r.starts) {
                 first = a.r.starts[i];
                 add = (int)min(max((int64_t)a.r.starts[i + 1] - first, (int64_t)0), (int64_t)c.cap() + 1);
             } else {
                 add = a.r.rows;
             }
-            if (a.window > 0) {
-                slide0 = (int)(((int64_t)a.sinks + mask) >> shift);
-                slide1 = max(keep - a.window + 1, 0) >> shift;
-            }
             if (keep != length) c.lengths[s] = keep;
         }
         if (i < n) put(i, {keep, s >= 0 ? add : 0, 0, -1, s});
         const int cut0 = (keep + mask) >> shift, cut1 = (length + mask) >> shift;
-        if (cut1 > cut0 || slide1 > slide0) freed = 1;
-        for (unsigned long long todo = __ballot(cut1 > cut0 || slide1 > slide0); todo; todo &= todo - 1) {
+        if (cut1 > cut0) freed = 1;
+        for (unsigned long long todo = __ballot(cut1 > cut0); todo; todo &= todo - 1) {
             const int l = (int)__builtin_ctzll(todo);
-            const int64_t row = (int64_t)__shfl(s, l, 64) * c.max_pages;
-            give_back(c, row, __shfl(cut0, l, 64), __shfl(cut1, l, 64), false);
-            give_back(c, row, __shfl(slide0, l, 64), min(__shfl(slide1, l, 64), __shfl(cut0, l, 64)), true);
+            give_back<1>(c, (int64_t)__shfl(s, l, 64) * c.max_pages, __shfl(cut0, l, 64), __shfl(cut1, l, 64));
         }
     }
     __syncthreads();
@@ -273,6 +295,14 @@ __global__ __launch_bounds__(kPlanThreads) void cache_extend_kernel(const Extend
         a.words[W_COPIES] = copies;
         if (a.granted) *a.granted = fits;
     }
+}
+
+// The same of long lists and tables, by more than one workgroup, in front of cache_extend_kernel (us, a call, in front of it / in it: one sequence of 200000 positions, pages of 32 9.9 / 8.7; 16 of
+// 50001, pages of 64 8.7 / 8.9; 64 of 2000 8.8 / 10.7; 64 of 50001, pages of 32 11.7 / 28.6; 64 of 2^20, pages of 64 41 / 190).
+constexpr int kSlideHere = 32, kSlideGroups = 1024;
+__global__ __launch_bounds__(256) void cache_slide_kernel(const ExtendArgs a) {
+    const int64_t items = (int64_t)a.r.n * a.pieces;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < items; u += (int64_t)gridDim.x * 4) slide(a, (int)u, a.pieces);
 }
 
 // The first positions of pages, a wave a layer, half and head (pieces of a few KiB: enough of them for every compute unit).  Bound: memory; 91 MB read and written 20 us, 4.5 TB/s of 5.41.
@@ -686,11 +716,16 @@ extern "C" int bild_cache_extend(bild_cache* c, const bild_cache_extend_call* ca
     if (!c || !call) return BILD_EINVAL;
     const bild_cache_extend_call& k = *call;
     if (k.n < 1 || k.n > c->view.sequences || k.rows < 0 || k.window < 0 || k.sinks < 0) return BILD_EINVAL;
-    const ExtendArgs a = {c->view, {k.sequences, k.starts, k.n, std::min(k.rows, c->view.cap() + 1), 0}, k.cut, k.granted, k.window, k.sinks, c->plan, c->fresh, c->asked, c->latest,
-                          c->plan + 4 * (size_t)c->view.sequences, c->words};
+    const int pieces = (c->view.max_pages + 64 * kSlideEach - 1) / (64 * kSlideEach);
+    ExtendArgs a = {c->view, {k.sequences, k.starts, k.n, std::min(k.rows, c->view.cap() + 1), 0}, k.cut, k.granted, k.window, k.sinks, pieces, c->plan, c->fresh, c->asked, c->latest,
+                    c->plan + 4 * (size_t)c->view.sequences, c->words};
     const OnDevice on(c->device);
     if (!on.ok) return BILD_EHIP;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (const int64_t items = (int64_t)k.n * pieces; k.window && items > kSlideHere) {
+        if (launch_on(cache_slide_kernel, dim3((unsigned)std::min<int64_t>((items + 3) / 4, kSlideGroups)), dim3(256), 0, st, a) != hipSuccess) return BILD_EHIP;
+        a.window = 0;
+    }
     if (launch_on(cache_extend_kernel, dim3(1), dim3(kPlanThreads), 0, st, a) != hipSuccess) return BILD_EHIP;
     if (!k.starts && k.rows == 0) return BILD_OK;  // (nothing is copied)
     const int64_t planes = (int64_t)c->view.layers * 2 * c->view.heads, groups = std::min<int64_t>((k.n * planes + 3) / 4, 2048);

@@ -645,3 +645,29 @@ def test_windows_that_hide_nothing(window, sinks, d, dtype):
     open_, lse_open = attend(t, np.random.default_rng(1), 0, [8], 1, dtype)
     assert np.array_equal(lse_again, lse_open) and np.array_equal(again, open_)
     assert np.all(lse[:127] == -np.inf) and np.all(np.isfinite(lse[127:130]))
+
+
+@pytest.mark.parametrize("sequences", [3, 40])
+def test_fewer_sinks_give_back_what_more_have_kept(sequences):
+    """What no row from the cut on sees is given back, whatever earlier calls had for sinks and windows: pages in front of a long stretch without any, and in the middle of one."""
+    t, rng = cache(62, pages=260, page=32, heads=1, d=16, sequences=sequences, max_pages=700)
+
+    def grow(rows, times, **kw):
+        rows = [rows, rows // 2] + [0] * (sequences - 2)
+        for _ in range(times):
+            assert extend(t, rows, **kw)
+            append(t, rng, 0, rows)
+        t.same()
+        invariants(t.o)
+
+    grow(600, 10, window=100, sinks=1280)
+    assert np.sum(t.o.table[0] >= 0) >= 40
+    grow(1, 2, window=100, sinks=4)                             # 39 pages behind a hundred and more that are gone
+    assert np.sum(t.o.table[0] >= 0) <= 1 + 6
+    grow(600, 5, window=1000, sinks=6100)                       # (the window's pages become sinks)
+    grow(300, 20, window=1000, sinks=6100)
+    held = np.flatnonzero(t.o.table[0] >= 0)
+    assert np.any((held > 2) & (held < 191)) and np.max(np.diff(held)) > 64
+    grow(1, 1, window=1000)                                     # from the middle, and from the beginning
+    assert np.sum(t.o.table[0] >= 0) <= 34
+    attend(t, rng, 0, [1] * sequences, window=1000)
