@@ -181,3 +181,27 @@ def test_calls_that_are_refused():
         assert e.value.code == code, kw
     bad = b.BeamsCall(logits=p, scores=p, out_scores=p, out_parents=p, out_tokens=p, batch=1, choices=1, reserved=1)
     assert pkg.lib().bild_beams_select(s.h, C.byref(bad), None) == b.EINVAL
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("beams,choices,vocab,living", [(8, 16, 250112, 1), (16, 16, 32128, 1), (32, 64, 32128, 4), (64, 64, 5001, 2), (12, 12, 1000, 1), (8, 16, 9000, 3)])
+def test_few_living_beams(beams, choices, vocab, living, dtype):
+    """A first step, where one beam has a score, and last ones, where most have ended: fewer chunks than usual to take a threshold from."""
+    rng = np.random.default_rng(beams + living)
+    words = pack(2.5 * rng.standard_normal((beams, vocab)), dtype)
+    at = rng.permutation(beams)[:living]
+    scores = np.full(beams, -np.inf)
+    scores[at] = -rng.random(living)
+    select(words, dtype, 1, beams, choices, scores)
+    finished = np.ones(beams, np.int32)
+    finished[at] = 0
+    lengths = rng.integers(3, 30, beams).astype(np.int32)
+    select(words, dtype, 1, beams, choices, -lengths * (0.5 + rng.random(beams)), lengths, finished, pad=1, penalty=0.6)
+
+
+def test_beams_whose_scores_are_far_apart():
+    """Most of what is chosen goes on from the best beam, whose groups alone are too few."""
+    rng = np.random.default_rng(12)
+    words = pack(2.5 * rng.standard_normal((32, 32128)), BF16)
+    select(words, BF16, 1, 32, 64, -0.7 * np.arange(32))
+    select(words, BF16, 1, 32, 64, -3.0 * np.arange(32)[::-1])

@@ -671,3 +671,41 @@ def test_fewer_sinks_give_back_what_more_have_kept(sequences):
     grow(1, 1, window=1000)                                     # from the middle, and from the beginning
     assert np.sum(t.o.table[0] >= 0) <= 34
     attend(t, rng, 0, [1] * sequences, window=1000)
+
+
+def test_codes_in_a_large_pool():
+    """More pages than a workgroup looks at in one turn: what is copied, written and packed there, code by code."""
+    t, rng = cache(63, pages=9000, page=32, layers=1, heads=1, d=16, sequences=60, max_pages=300)
+    t.o.codes[...] = rng.integers(-127, 128, t.o.codes.shape)
+    t.o.scales[...] = rng.random(t.o.scales.shape)
+    t = Held(t.o)
+    assert extend(t, [273 * 32] * 30, list(range(30, 60)))      # (8190 pages in front)
+    ids = list(range(30))
+    rows = rng.integers(1, 900, 30)
+    assert extend(t, rows, ids)
+    append(t, rng, 0, rows, sequences=ids)
+    t.same()
+    fork(t, rng.integers(0, 15, 30), ids)
+    assert extend(t, [3] * 30, ids)
+    append(t, rng, 0, [3] * 30, sequences=ids)
+    t.same()
+    assert np.max(t.o.table) > 8192
+    assert extend(t, [0] * 6, [3, 4, 5, 31, 40, 59], cut=[0] * 6)
+    t.o.compact()
+    t.cache.compact()
+    t.same()
+    invariants(t.o)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_tens_of_thousands_of_positions(dtype):
+    t, rng = cache(64, pages=700, page=64, heads=2, d=64, sequences=2, max_pages=640)
+    t.o.lengths[:] = 40001, 130
+    t.o.table[0, :626], t.o.table[1, :3] = rng.permutation(697)[:626], [697, 698, 699]
+    t.o.refs[t.o.table[t.o.table >= 0]] = 1
+    t.o.codes[...] = rng.integers(-127, 128, t.o.codes.shape)
+    t.o.scales[...] = 0.2 + rng.random(t.o.scales.shape)
+    t = Held(t.o)
+    attend(t, rng, 0, [1, 1], 4, dtype, uniform=True)
+    attend(t, rng, 0, [5, 2], 4, dtype, window=33000, sinks=700)
+    attend(t, rng, 0, [40, 1], 4, dtype)                        # a prompt
