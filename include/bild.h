@@ -487,9 +487,9 @@ int bild_cache_fork(bild_cache* c, const int32_t* sequences /* [n], nullable */,
  * nullable): how many there are. */
 int bild_cache_compact(bild_cache* c, int32_t* used, void* hip_stream);
 
-/* Writes keys and values of one layer for the last rows of each sequence, which bild_cache_extend has made room for.  A page's scale becomes the largest magnitude among its positions, of which
- * those that were there are rounded once more if it grows: codes are the nearest to 127 x / scale (fp32), with scale, the products and quotients in fp32.  Magnitudes beyond 2^90 are limited to it, NaN counts as 0.
- * Pages that several sequences hold are not written. */
+/* Writes keys and values of one layer for the last rows of each sequence, which bild_cache_extend has made room for.  A page's scale grows to the largest magnitude that it has held (a cut does not
+ * lower it, a page that is given away anew begins at 0); the positions that were there are rounded once more if it does: codes are the nearest to 127 x / scale (fp32), with scale, the products and quotients in fp32.
+ * Magnitudes beyond 2^90 are limited to it, NaN counts as 0.  Pages that several sequences hold are not written. */
 typedef struct bild_cache_append_call {
     const void* k;            /* head h of row t at k + t * k_token + h * k_head, its d_head values side by side */
     const void* v;
@@ -510,8 +510,9 @@ int bild_cache_append(bild_cache* c, const bild_cache_append_call* call, void* h
  *   out[t][h] = sum over j of p_j v_j,  p = softmax of scale * q[t][h] k_j,  lse = ln of the sum of e^(scale * q k_j)
  * Query head h has the key head h / (heads / key heads).  A row that sees nothing: out 0, lse -infinity.  Products are those of q as fp16, times a power of two that puts the largest of its row below 2^15
  * (fp32: two fp16 parts), with the codes themselves; weights of the values, for many rows with the ratio of their page's scale to others, are fp16 (fp32 rows: two parts); sums are fp32; out is
- * rounded once.  Where a sequence has many rows, values of a page may count as 0 whose scale is 2^80 times smaller than that of another of its pages.  A row whose q has an infinity or NaN, or
- * whose products go beyond fp32, has no finite result and leaves the others alone.  out may not overlap q. */
+ * rounded once.  Where a sequence has many rows, values of a page may count as 0 whose scale is 2^80 times smaller than that of another of its pages.  Weights (times that ratio)
+ * below 2^-25 of a row's largest may count as 0 for the values, not for lse.  What a row gives whose q has an infinity or NaN, or whose products go beyond fp32, is not defined (as a rule NaN); it
+ * leaves the others alone.  out may not overlap q. */
 typedef struct bild_cache_attend_call {
     const void* q;            /* head h of row t at q + t * q_token + h * q_head                  */
     void* out;
@@ -561,7 +562,7 @@ typedef struct bild_beams_call {
     float penalty;             /* 0: by sums                                                      */
     int32_t reserved;          /* 0 */
 } bild_beams_call;
-typedef struct bild_beams bild_beams; /* device memory for the statistics of rows that several workgroups share */
+typedef struct bild_beams bild_beams; /* device memory for the statistics of rows that several workgroups share; its calls have to follow each other (one stream, or ordered by the caller) */
 int bild_beams_create(int vocab /* up to 2^24 */, int max_batch, int beams /* 1 .. 64; max_batch * beams up to 65535 */, bild_beams** out);
 int bild_beams_destroy(bild_beams* b);
 int bild_beams_select(bild_beams* b, const bild_beams_call* call, void* hip_stream);

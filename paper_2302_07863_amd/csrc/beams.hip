@@ -5,7 +5,10 @@
 // Bound: memory, every logit read once.  The first kernel reads them: for the softmax's sum, and for the largest of each chunk of 64 consecutive 16-byte pieces.  The k best
 // lie in chunks whose maxima are among the k best maxima, so the second kernel, a workgroup a group of beams, looks at some thousand maxima and reads few chunks again.
 // What is chosen is decided in 64 bits (of the fp32 sums): a threshold that k maxima reach is taken in fp32, to which ranks are rounded monotonically, so that it loses
-// nobody; who reaches it is listed and each counts how many are better.  Lists that are too long (flat logits, where thousands are equal) are left for a walk in the order of the ids.
+// nobody; who reaches it is listed and each counts how many are better.  Lists that are too long are left for a walk in the order of the ids, one workgroup an entry of the batch: right, and slow.
+// They are too long where thousands of ranks are equal (flat logits), and where the threshold is low because maxima are taken in groups, each of one beam: where few beams live (a search's first step;
+// with fewer than 2 of 8 beams for 16 choices, 4 of 32 for 64, there are not as many groups as choices and no threshold), or most of what is chosen goes on from few beams.  us, a call: 8 beams of 250112
+// ids, 16 choices 15, with one living beam 234; 32 beams, 64 choices with scores 0.7 apart from beam to beam 156, with four living 779; of 32128 ids 13, 110, 53, 327.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -136,8 +139,8 @@ __global__ __launch_bounds__(kPickThreads) void beams_pick_kernel(const BeamsArg
     const float* tops = a.tops + row0 * chunks;
     if (tid == 0) n_chunks = n_list = far = 0;
     lds_barrier();
-    // Groups of 16 or 4 lanes: four times as many as choices at least, or the threshold would be among the low ones of their maxima.  A wave looks at the maxima of a slice of a beam's
-    // chunks, neighbours in groups apart.
+    // Groups of 16 or 4 lanes: four times as many as choices at least, or the threshold would be among the low ones of their maxima (of beams that offer nothing they are empty: see the top).  A wave
+    // looks at the maxima of a slice of a beam's chunks, neighbours in groups apart.
     const int width = a.choices <= 16 ? 16 : 4, groups = kPickThreads / width;
     const int slices = (kPickWaves + a.beams - 1) / a.beams, pairs = a.beams * slices, per = (chunks + slices - 1) / slices, swapped = lane / width + 64 / width * (lane & (width - 1));
     const auto each = [&](int pair, auto&& f) {  // f(beam, chunk of it)

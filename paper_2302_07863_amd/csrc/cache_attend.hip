@@ -16,6 +16,9 @@
 // tiles, and from the beginning of one to its meeting are some 10 us beside its blocks: lengths 1, table and scales 2, first codes 2.4, joining waves 3, meeting and joining parts 3.
 // One sequence of 513 positions 7.7 us: the same chain.  What did not help: codes of two blocks on their way (the same to 3 % slower), a piece of the line a wave instead of a workgroup (batches of
 // short sequences 5 to 15 % faster, all else 3 to 10 % slower).
+//
+// Not for heads above 128: an instantiation for 256 of the form before this one, whose line of work the compiler did not know to be the same in all lanes, ended in a memory fault, and its cause was not
+// found.  (Instantiations hold some hundred scalar registers in lanes of vector registers; none goes to memory.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

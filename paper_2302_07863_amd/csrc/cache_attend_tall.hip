@@ -1,5 +1,5 @@
 // Attention over the cache in 8 bits (bild_cache_attend) of few rows a sequence, heads above 128: cache_attend.hip's walk over the keys in its first form, with four waves a
-// workgroup.  (The present form, with eight, is not built for these heads: an instantiation for heads of 256 ended in a memory fault whose cause was not found.)
+// workgroup.  (The form with eight is not built for these heads: an instantiation for heads of 256 ended in a memory fault whose cause was not found.)
 // Bound: HBM for long sequences; 16 heads of 256 over 65536 positions 108 us a call, 5.0 TB/s; 8 over 4000 24.8 us, which was not taken apart.
 #include <hip/hip_runtime.h>
 

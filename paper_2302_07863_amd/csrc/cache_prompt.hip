@@ -8,10 +8,10 @@
 // row's number, so that neither product's reads meet in a bank.  Scores of keys that a row does not see begin as -infinity.  A page's scale of the values goes into the exponent of its weights (one
 // sum, no product a value), relative to a power of two that the results are in units of.
 //
-// Bound: issue slots and the matrix cores, which work by turns more than side by side.  2000 rows of 32 heads of 128, 8 key heads, behind 3001 positions (131 GFLOP): some 155 us among other calls, 178
+// Bound: issue slots and the matrix cores, which work by turns more than side by side (busy 51 and 35 % of the time, by counters; LDS 35 %, of which conflicts are a quarter).  2000 rows of 32 heads of 128, 8 key heads, behind 3001 positions (131 GFLOP): some 155 us among other calls, 178
 // back to back at the 1.9 to 2.0 GHz that the chip then keeps, 740 to 850 TFLOP/s where a large product reaches 1191; a tile of a wave is some 410 slots (32 products, 34 of four slots) and 1024 cycles of the matrix cores, and takes 2560.  Left out in
 // turn, in the form before the loop was cleared of copies of registers (195 us a call), exponentials saved 2 us, taking codes apart 12, all products 36.  What did not help: the next tile's scores beside a tile's exponentials (5 to 10 % slower, at 256 registers), waves'
-// priorities, four waves a unit more at 128 registers (spills, 60 % slower).
+// priorities, four waves a unit more at 128 registers (spills, 60 % slower).  fp32 rows of heads above 128 keep 55 to 63 registers of a lane in memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
